@@ -357,7 +357,8 @@ const char* ris_status_string(int status);
  * ris_mask_desc; 2.1 added the row-range build and the decode step; 2.2 the
  * host-model layers (RMSNorm, SwiGLU); 2.3 the strided rotation
  * ris_rope_from; 2.4 changed the draws' round function (the same descriptor
- * now yields different, equally distributed sets). */
+ * now yields different, equally distributed sets); 2.5 the serving operators of
+ * ris_serve.h. */
 int ris_version(void);
 
 #ifdef __cplusplus

@@ -137,9 +137,52 @@ constexpr float kAutoDensity = 0.05f;
 
 }  // namespace
 
+// Rotary frequencies of a descriptor; window: the positions it has to cover.
+namespace ris {
+int make_rope_table(const ris_rope_desc* desc, int32_t D, int64_t window, RopeTable* tab) {
+    if (desc->kind < RIS_ROPE_PLAIN || desc->kind > RIS_ROPE_YARN) return RIS_E_ARG;
+    if (!(desc->base > 1.0) || !isfinite(desc->base)) return RIS_E_ARG;
+    if (!(desc->factor >= 0.0) || !isfinite(desc->factor)) return RIS_E_ARG;
+    if (!(desc->beta_slow >= 0.0) || !(desc->beta_fast >= 0.0)) return RIS_E_ARG;
+    if (desc->kind != RIS_ROPE_PLAIN && desc->orig_max_pos < 1) return RIS_E_ARG;
+
+    // Factor: requested window / native limit (at least 1) unless given.
+    double s = desc->factor;
+    if (desc->kind != RIS_ROPE_PLAIN && !(s > 0.0)) {
+        s = (double)window / (double)desc->orig_max_pos;
+        if (s < 1.0) s = 1.0;
+    }
+    const int half = D / 2;
+    const double base = desc->base;
+    for (int i = 0; i < half; ++i) {
+        const double plain = 1.0 / pow(base, 2.0 * i / D);
+        double f = plain;
+        if (desc->kind == RIS_ROPE_LINEAR) {
+            f = plain / s;
+        } else if (desc->kind == RIS_ROPE_YARN) {
+            const double b_slow = desc->beta_slow > 0.0 ? desc->beta_slow : 1.0;
+            const double b_fast = desc->beta_fast > 0.0 ? desc->beta_fast : 32.0;
+            const double L0 = (double)desc->orig_max_pos;
+            const double c_fast = D * log(L0 / (b_fast * 2.0 * M_PI)) / (2.0 * log(base));
+            const double c_slow = D * log(L0 / (b_slow * 2.0 * M_PI)) / (2.0 * log(base));
+            double lo = floor(c_fast), hi = ceil(c_slow);
+            if (lo < 0.0) lo = 0.0;
+            if (hi > D - 1) hi = D - 1;
+            if (lo == hi) hi += 0.001;
+            double t = (i - lo) / (hi - lo);
+            t = t < 0.0 ? 0.0 : (t > 1.0 ? 1.0 : t);
+            f = t * (plain / s) + (1.0 - t) * plain;
+        }
+        tab->inv_freq[i] = f;
+    }
+    tab->mscale = (desc->kind == RIS_ROPE_YARN && s > 1.0) ? 0.1 * log(s) + 1.0 : 1.0;
+    return RIS_OK;
+}
+}  // namespace ris
+
 extern "C" {
 
-int ris_version(void) { return (2 << 16) | 4; }
+int ris_version(void) { return (2 << 16) | 5; }
 
 const char* ris_status_string(int status) {
     switch (status) {
@@ -207,44 +250,11 @@ int ris_rope_from(const void* src, int64_t head_stride, int64_t token_stride, vo
     if (dtype != RIS_F32 && dtype != RIS_BF16) return RIS_E_DTYPE;
     if (heads < 1 || N < 1 || pos0 < 0) return RIS_E_ARG;
     if (D < 2 || (D & 1) || D / 2 > ris::kMaxRopeHalf) return RIS_E_SHAPE;
-    if (desc->kind < RIS_ROPE_PLAIN || desc->kind > RIS_ROPE_YARN) return RIS_E_ARG;
-    if (!(desc->base > 1.0) || !isfinite(desc->base)) return RIS_E_ARG;
-    if (!(desc->factor >= 0.0) || !isfinite(desc->factor)) return RIS_E_ARG;
-    if (!(desc->beta_slow >= 0.0) || !(desc->beta_fast >= 0.0)) return RIS_E_ARG;
-    if (desc->kind != RIS_ROPE_PLAIN && desc->orig_max_pos < 1) return RIS_E_ARG;
     if (N > (1ll << 32) || pos0 > (1ll << 52)) return RIS_E_ARG;
 
-    // Factor: requested window / native limit (at least 1) unless given.
-    double s = desc->factor;
-    if (desc->kind != RIS_ROPE_PLAIN && !(s > 0.0)) {
-        s = (double)(pos0 + N) / (double)desc->orig_max_pos;
-        if (s < 1.0) s = 1.0;
-    }
     ris::RopeTable tab;
-    const int half = D / 2;
-    const double base = desc->base;
-    for (int i = 0; i < half; ++i) {
-        const double plain = 1.0 / pow(base, 2.0 * i / D);
-        double f = plain;
-        if (desc->kind == RIS_ROPE_LINEAR) {
-            f = plain / s;
-        } else if (desc->kind == RIS_ROPE_YARN) {
-            const double b_slow = desc->beta_slow > 0.0 ? desc->beta_slow : 1.0;
-            const double b_fast = desc->beta_fast > 0.0 ? desc->beta_fast : 32.0;
-            const double L0 = (double)desc->orig_max_pos;
-            const double c_fast = D * log(L0 / (b_fast * 2.0 * M_PI)) / (2.0 * log(base));
-            const double c_slow = D * log(L0 / (b_slow * 2.0 * M_PI)) / (2.0 * log(base));
-            double lo = floor(c_fast), hi = ceil(c_slow);
-            if (lo < 0.0) lo = 0.0;
-            if (hi > D - 1) hi = D - 1;
-            if (lo == hi) hi += 0.001;
-            double t = (i - lo) / (hi - lo);
-            t = t < 0.0 ? 0.0 : (t > 1.0 ? 1.0 : t);
-            f = t * (plain / s) + (1.0 - t) * plain;
-        }
-        tab.inv_freq[i] = f;
-    }
-    tab.mscale = (desc->kind == RIS_ROPE_YARN && s > 1.0) ? 0.1 * log(s) + 1.0 : 1.0;
+    const int st = ris::make_rope_table(desc, D, pos0 + N, &tab);
+    if (st != RIS_OK) return st;
     return hip_status(ris::launch_rope(src, head_stride, token_stride, x, dtype == RIS_BF16, heads, N, D, pos0,
                                        tab, static_cast<hipStream_t>(stream)));
 }
@@ -452,6 +462,7 @@ int ris_decode_attn(const void* Q, const void* K, const void* V, const int64_t* 
     p.B = d.batch; p.Hq = d.Hq; p.Hkv = d.Hkv; p.G = d.Hq / d.Hkv; p.D = d.D;
     p.out_bf16 = d.dtype_out == RIS_BF16;
     p.window = d.window; p.sink = d.sink;
+    p.keep_nan = 0;
     p.parts = (int32_t)decode_waves(d);
     // a row holds max_len keys at most: no overflow for any descriptor
     const int64_t keys = decode_keys(d) < d.max_len ? decode_keys(d) : d.max_len;

@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "ris_serve.h"
+
 namespace ris {
 
 // Resolved geometry parameters (block already fixed for Structural mode).
@@ -110,6 +112,7 @@ struct DecodeParams {
     int32_t B, Hq, Hkv, G, D;
     int32_t out_bf16;
     int32_t window, sink;
+    int32_t keep_nan;             // 1: a row whose weights sum to NaN is NaN, 0: zeros
     int64_t kv_bytes;             // K and V bytes of a step, estimated as for `parts`
     int32_t parts;                // waves per row (a multiple of kDecodeWaves)
     float scale;
@@ -120,5 +123,63 @@ hipError_t launch_decode(const DecodeParams& p, hipStream_t st);
 hipError_t launch_rmsnorm(const void* x, void* residual, const void* w, void* out, int64_t rows,
                           int64_t cols, float eps, int bf16, hipStream_t st);
 hipError_t launch_swiglu(const void* gu, void* out, int64_t rows, int64_t inter, int bf16, hipStream_t st);
+
+// Packed prompts.
+int make_rope_table(const ris_rope_desc* desc, int32_t D, int64_t window, RopeTable* tab);
+hipError_t launch_rope_packed(const void* src, int64_t head_stride, int64_t token_stride, void* dst, int dtype_bf16,
+                              int heads, int64_t T, int D, const int64_t* cu, const int64_t* start, int batch,
+                              const RopeTable& tab, hipStream_t st);
+
+struct PromptParams {
+    const void* Q;
+    const void* K;
+    const void* V;
+    const int64_t* cu;            // [batch + 1]
+    void* out;
+    int64_t T;
+    int64_t q_head, q_token, k_head, k_token, v_head, v_token, o_head, o_token;
+    int32_t Hq, Hkv, G, D;
+    int32_t batch, causal;
+    int32_t in_bf16, out_bf16;
+    float c;                      // score scale in the log2 domain
+    float slack;                  // scores above the reference maximum before it moves
+};
+int64_t prompt_blocks(int64_t T, int batch, int Hkv, int G, int in_bf16);   // workgroups of a launch
+hipError_t launch_prompt_attn(const PromptParams& p, hipStream_t st);
+
+// 4-bit key/value cache.
+struct Kv4Params {
+    void* K;                      // rows, strided
+    void* V;
+    uint8_t* K4;                  // [batch, Hkv, max_len, D / 2]
+    uint8_t* V4;
+    uint8_t* S;                   // [batch, Hkv, max_len, 2, D / 32]
+    const int64_t* cu;            // [batch + 1]
+    const int64_t* start;         // [batch] or null
+    int64_t T, max_len;
+    int64_t k_head, k_token, v_head, v_token;
+    int32_t Hkv, D, batch;
+    int32_t bf16;
+};
+hipError_t launch_kv4_store(const Kv4Params& p, hipStream_t st);
+hipError_t launch_kv4_load(const Kv4Params& p, hipStream_t st);
+hipError_t launch_kv4_decode(const DecodeParams& p, const uint8_t* S, hipStream_t st);
+
+// Log probabilities.
+struct LogprobParams {
+    const void* logits;
+    const int64_t* targets;       // [rows, n_targets]
+    float* logprob;
+    float* entropy;               // may be null
+    int64_t* top_ids;             // [rows, top_k]
+    float* top_logprob;
+    float* part;                  // workspace: [rows, parts] states, then their lists
+    int64_t rows, vocab, row_stride;
+    int32_t n_targets, top_k, bf16;
+    int32_t parts;                // workgroups per row
+};
+int32_t logprob_parts(int64_t rows, int64_t vocab);
+int64_t logprob_workspace(int64_t rows, int32_t parts, int32_t top_k);
+hipError_t launch_logprobs(const LogprobParams& p, hipStream_t st);
 
 }  // namespace ris

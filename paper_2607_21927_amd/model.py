@@ -16,12 +16,17 @@ BLAS, weights kept [out, in] contiguous: activations times transposed
 weights is the layout the library's bf16 GEMMs run fastest in, 13-16% ahead
 of pre-transposed [in, out] weights at these shapes); every other step runs
 in the library's kernels.  The stack
-returns the final normalised hidden states (no LM head).
+returns the final normalised hidden states.
+
+Around that pass (``serve``): ``prefill_packed`` runs prompts of different
+lengths through the stack at full density, the paper's dense baseline, and can
+fill a 4-bit key/value cache; ``decode_step`` generates over that cache; ``score``
+and ``score_prompts`` give log probabilities of tokens under the LM head.
 """
 import torch
 import torch.nn.functional as F
 
-from . import ris
+from . import ris, serve
 
 
 class PrefillModel:
@@ -30,7 +35,9 @@ class PrefillModel:
     cfg: a model configuration with fields hidden, heads, kv_heads, head_dim,
     inter, layers, eps, qkv_bias, vocab.  weights: the dict layout of
     ``synth.model_weights`` (numpy arrays or tensors; linear weights
-    [out, in]); they are copied to the device in ``dtype``.
+    [out, in]); they are copied to the device in ``dtype``.  The LM head is
+    ``weights["lm_head"]`` [vocab, hidden], or the embedding where the weights tie
+    the two.
     """
 
     def __init__(self, cfg, weights, device="cuda", dtype=torch.bfloat16):
@@ -42,6 +49,7 @@ class PrefillModel:
             return torch.as_tensor(a).to(device=self.device, dtype=dtype).contiguous()
 
         self.embed = t(weights["embed"])
+        self.lm_head = t(weights["lm_head"]) if "lm_head" in weights else self.embed
         self.layers = []
         for L in weights["layers"]:
             layer = {
@@ -125,3 +133,142 @@ class PrefillModel:
             if timers:
                 timers.mark("proj")
         return h
+
+    # ---- packed prompts, generation over the 4-bit cache, scoring
+
+    def kv4_cache(self, batch, max_len):
+        """A 4-bit key/value cache for ``batch`` sequences of up to ``max_len``
+        tokens, one (K4, V4, S) per layer, with what the steps over it reuse."""
+        return KV4Cache(self, batch, max_len)
+
+    def _packed_qkv(self, h, layer, cu_seqlens, rope_desc, start):
+        """Rotated Q [Hq, T, D] and K [Hkv, T, D], and V as a view of the projection."""
+        cfg = self.cfg
+        T, D, Hq, Hkv = h.shape[0], cfg.head_dim, cfg.heads, cfg.kv_heads
+        qkv = F.linear(h, layer["wqkv"], layer["bqkv"]).view(T, Hq + 2 * Hkv, D).transpose(0, 1)
+        qk = qkv[:Hq + Hkv]
+        if rope_desc is not None:
+            qk = serve.rope_packed(qk, torch.empty(Hq + Hkv, T, D, dtype=qkv.dtype, device=qkv.device), cu_seqlens,
+                                   rope_desc, start=start)
+        return qk[:Hq], qk[Hq:], qkv[Hq + Hkv:]
+
+    def _stack(self, ids, attention, timers=None):
+        """The decoder stack around ``attention(l, layer, h)`` [T, Hq D]."""
+        cfg = self.cfg
+        res = self.embed[ids].contiguous()
+        h = torch.empty_like(res)
+        ris.rmsnorm(res, self.layers[0]["ln1"], h, cfg.eps)
+        for l, layer in enumerate(self.layers):
+            a = F.linear(attention(l, layer, h), layer["wo"])
+            ris.rmsnorm(a, layer["ln2"], h, cfg.eps, residual=res)
+            m = self.mlp(h, layer)
+            nxt = self.layers[l + 1]["ln1"] if l + 1 < len(self.layers) else self.norm
+            ris.rmsnorm(m, nxt, h, cfg.eps, residual=res)
+            if timers:
+                timers.mark("proj")
+        return h
+
+    def prefill_packed(self, ids, cu_seqlens, rope_desc=None, cache=None, timers=None):
+        """Final hidden states [T, hidden] of prompts packed into ``ids`` [T], with
+        dense causal attention within each prompt and positions from 0.
+
+        cu_seqlens: device int64 offsets [batch + 1].  rope_desc: as in ``prefill``,
+        with the factor given for linear and YaRN.  cache: a ``kv4_cache`` of as
+        many sequences, which receives the prompts' keys and values.  Rows of
+        tokens outside every prompt hold nothing of use.
+        """
+        cfg = self.cfg
+        T, D, Hq = ids.shape[0], cfg.head_dim, cfg.heads
+
+        def attention(l, layer, h):
+            q, k, v = self._packed_qkv(h, layer, cu_seqlens, rope_desc, None)
+            if timers:
+                timers.mark("rope")
+            if cache is not None:
+                serve.kv4_store(k, v, cu_seqlens, *cache.layers[l])
+            a = torch.empty(T, Hq * D, dtype=h.dtype, device=h.device)
+            out = a.view(T, Hq, D).transpose(0, 1)
+            serve.prompt_attn(q, k, v, cu_seqlens, out, serve.prompt_desc(q, k, v, out, cu_seqlens))
+            if timers:
+                timers.mark("attention")
+            return a
+
+        return self._stack(ids, attention, timers)
+
+    def decode_step(self, ids, pos, cache, rope_desc=None, anchors=None, window=None, sink=0):
+        """Final hidden states [batch, hidden] of one new token a sequence: ids
+        [batch] at positions pos [batch] (device int64), whose keys and values join
+        the cache before the step attends to it.
+
+        window None attends to every token of the cache.  anchors: per layer the
+        (anchor_ptr, anchor_idx) that ``ris.mask_build_rows`` wrote for the sequences
+        (anchor_idx [batch, stride]), with the local window and initial tokens of the
+        Hybrid Anchor.  bf16 models only.
+        """
+        cfg = self.cfg
+        B, D, Hq = ids.shape[0], cfg.head_dim, cfg.heads
+
+        def attention(l, layer, h):
+            q, k, v = self._packed_qkv(h, layer, cache.cu, rope_desc, pos)
+            serve.kv4_store(k, v, cache.cu, *cache.layers[l], start=pos)
+            ptr, idx = anchors[l] if anchors is not None else (None, None)
+            q = q.transpose(0, 1).contiguous()
+            out = torch.empty(B, Hq, D, dtype=h.dtype, device=h.device)
+            desc = serve.kv4_decode_desc(q, cache.layers[l][0], out, idx.shape[1] if idx is not None else 0,
+                                         window=cache.max_len if window is None else window, sink=sink)
+            serve.kv4_decode_attn(q, *cache.layers[l], pos, ptr, idx, out, cache.workspace(desc), desc)
+            return out.view(B, Hq * D)
+
+        return self._stack(ids, attention)
+
+    def score(self, h, targets=None, top_k=0, rows=2048):
+        """Log probabilities under the LM head at hidden states h [n, hidden]: of
+        the tokens ``targets`` [n, m] (negative: padding, 0), with the entropy and
+        the ``top_k`` likeliest tokens.  Logits exist for ``rows`` states at a time.
+        Returns dict(logprob [n, m], entropy [n], top_ids, top_logprob [n, top_k])."""
+        n, m = h.shape[0], 0 if targets is None else targets.shape[1]
+        out = dict(logprob=torch.empty(n, m, dtype=torch.float32, device=h.device),
+                   entropy=torch.empty(n, dtype=torch.float32, device=h.device),
+                   top_ids=torch.empty(n, top_k, dtype=torch.int64, device=h.device),
+                   top_logprob=torch.empty(n, top_k, dtype=torch.float32, device=h.device))
+        if targets is not None:
+            targets = targets.contiguous()
+        for r in range(0, n, rows):
+            logits = F.linear(h[r:r + rows], self.lm_head)
+            desc = serve.logprob_desc(logits, m, top_k)
+            ws = torch.empty(serve.logprobs_workspace_bytes(desc), dtype=torch.uint8, device=h.device)
+            serve.logprobs(logits, targets[r:r + rows] if m else None, *(out[x][r:r + rows] for x in (
+                "logprob", "entropy", "top_ids", "top_logprob")), ws, desc)
+        return out
+
+    def score_prompts(self, ids, cu_seqlens, rope_desc=None, top_k=0):
+        """``score`` of every next token of packed prompts: entry t is about the token
+        after ids[t] in its prompt; a prompt's last token has none (log probability
+        0), so a sum over a prompt's entries is the prompt's log probability."""
+        T = ids.shape[0]
+        at = torch.arange(1, T + 1, device=ids.device)
+        ends = torch.zeros(T + 1, dtype=torch.bool, device=ids.device)
+        ends[cu_seqlens] = True
+        none = ends[1:] | (at <= cu_seqlens[0]) | (at > cu_seqlens[-1])
+        targets = torch.where(none, -1, ids.roll(-1))
+        return self.score(self.prefill_packed(ids, cu_seqlens, rope_desc), targets[:, None], top_k)
+
+
+class KV4Cache:
+    """The layers' 4-bit caches of a batch of sequences (``PrefillModel.kv4_cache``)."""
+
+    def __init__(self, model, batch, max_len):
+        cfg = model.cfg
+        self.max_len = max_len
+        self.layers = [serve.kv4_cache(batch, cfg.kv_heads, max_len, cfg.head_dim, model.device) for _ in model.layers]
+        self.cu = torch.arange(batch + 1, dtype=torch.int64, device=model.device)   # one token a sequence
+        self._ws = {}
+
+    def workspace(self, desc):
+        """Device scratch of the decode step: steps of one cache follow each other and
+        share it, one buffer a size, none of which moves while a captured step may
+        hold its address."""
+        n = serve.kv4_decode_workspace_bytes(desc)
+        if n not in self._ws:
+            self._ws[n] = torch.empty(n, dtype=torch.uint8, device=self.cu.device)
+        return self._ws[n]

@@ -1,0 +1,282 @@
+"""Python binding of the serving operators of libris.so (``include/ris_serve.h``).
+
+Argument checks and marshalling only, as in ``ris``: every step runs in the HIP
+library, the caller owns every tensor, and the work goes to torch's current HIP
+stream of the tensors' device unless a stream is given.
+"""
+import contextlib
+import ctypes
+
+from . import ris
+from .ris import _check, _dtype_code, _ptr
+
+MAX_TOP = 64
+KV4_BLOCK = 32          # dimensions that share a scale in the 4-bit cache
+
+
+class PromptDesc(ctypes.Structure):
+    _fields_ = [("dtype_in", ctypes.c_int32), ("dtype_out", ctypes.c_int32),
+                ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("batch", ctypes.c_int32), ("T", ctypes.c_int64), ("causal", ctypes.c_int32),
+                ("scale", ctypes.c_float),
+                ("q_head", ctypes.c_int64), ("q_token", ctypes.c_int64),
+                ("k_head", ctypes.c_int64), ("k_token", ctypes.c_int64),
+                ("v_head", ctypes.c_int64), ("v_token", ctypes.c_int64),
+                ("o_head", ctypes.c_int64), ("o_token", ctypes.c_int64)]
+
+
+class Kv4Desc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("batch", ctypes.c_int32), ("T", ctypes.c_int64), ("max_len", ctypes.c_int64),
+                ("k_head", ctypes.c_int64), ("k_token", ctypes.c_int64),
+                ("v_head", ctypes.c_int64), ("v_token", ctypes.c_int64)]
+
+
+class LogprobDesc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("n_targets", ctypes.c_int32), ("top_k", ctypes.c_int32),
+                ("rows", ctypes.c_int64), ("vocab", ctypes.c_int64), ("row_stride", ctypes.c_int64)]
+
+
+EXPORTS = ("ris_rope_packed", "ris_prompt_attn", "ris_kv4_store", "ris_kv4_load",
+           "ris_kv4_decode_workspace_bytes", "ris_kv4_decode_attn", "ris_logprobs_workspace_bytes",
+           "ris_logprobs")
+
+_lib = None
+
+
+def lib():
+    """``ris.lib()`` with the prototypes of this module's entry points."""
+    global _lib
+    if _lib is None:
+        L = ris.lib()
+        vp, i32, i64, ptr = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.POINTER
+        L.ris_rope_packed.argtypes = [vp, i64, i64, vp, i32, i32, i64, i32, vp, vp, i32, ptr(ris.RopeDesc), vp]
+        L.ris_prompt_attn.argtypes = [vp, vp, vp, vp, vp, ptr(PromptDesc), vp]
+        L.ris_kv4_store.argtypes = [vp] * 7 + [ptr(Kv4Desc), vp]
+        L.ris_kv4_load.argtypes = [vp] * 7 + [ptr(Kv4Desc), vp]
+        L.ris_kv4_decode_workspace_bytes.argtypes = [ptr(ris.DecodeDesc)]
+        L.ris_kv4_decode_attn.argtypes = [vp] * 9 + [i64, ptr(ris.DecodeDesc), vp]
+        L.ris_logprobs_workspace_bytes.argtypes = [ptr(LogprobDesc)]
+        L.ris_logprobs.argtypes = [vp] * 7 + [i64, ptr(LogprobDesc), vp]
+        for name in EXPORTS:
+            getattr(L, name).restype = i64 if name.endswith("_bytes") else ctypes.c_int
+        _lib = L
+    return _lib
+
+
+def _one_device(*ts):
+    """The GPU that holds all of the tensors."""
+    devices = {t.device for t in ts if t is not None}
+    if len(devices) != 1 or next(iter(devices)).type != "cuda":
+        raise ValueError("tensors must be on one GPU")
+    return next(iter(devices))
+
+
+def _need_dense(*ts):
+    for t in ts:
+        if t is not None and not t.is_contiguous():
+            raise ValueError("tensors must be contiguous")
+
+
+def _need_rows(shape, *ts):
+    """[heads, T, D] views whose rows 16-byte accesses can walk; a dimension of
+    one element may have any stride."""
+    for t in ts:
+        if tuple(t.shape) != shape:
+            raise ValueError(f"expected a {shape} view, got {tuple(t.shape)}")
+        if t.stride(2) != 1 or t.data_ptr() % 16 or any(s * t.element_size() % 16 for s in _strides(t)):
+            raise ValueError("rows must be contiguous, bases and strides multiples of 16 bytes")
+
+
+def _strides(t):
+    """Head and token stride of a [heads, T, D] view."""
+    return (t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0)
+
+
+def _bounds(cu_seqlens, start=None):
+    import torch
+    for t in (cu_seqlens, start):
+        if t is not None and (t.dtype != torch.int64 or t.dim() != 1 or not t.is_contiguous()):
+            raise TypeError("cu_seqlens and start must be contiguous int64 vectors")
+    batch = cu_seqlens.numel() - 1
+    if batch < 1 or (start is not None and start.numel() != batch):
+        raise ValueError("cu_seqlens must hold batch + 1 offsets and start one position a sequence")
+    return batch
+
+
+def _call(device, stream, name, *args):
+    """Launch on `stream` (torch's current one of `device`) with `device` current."""
+    import torch
+    other = torch.cuda.current_device() != device.index
+    with torch.cuda.device(device) if other else contextlib.nullcontext():
+        handle = ris._stream(stream)
+        _check(getattr(lib(), name)(*args, handle), name)
+
+
+def rope_packed(src, out, cu_seqlens, desc, start=None, stream=None):
+    """ris_rope_packed: src is a [heads, T, D] view (unit stride along D), out
+    [heads, T, D] contiguous; token i of sequence b is rotated to position
+    start[b] + i (start None: i)."""
+    device = _one_device(src, out, cu_seqlens, start)
+    _need_dense(out)
+    H, T, D = out.shape
+    if tuple(src.shape) != (H, T, D) or src.stride(2) != 1 or src.dtype != out.dtype:
+        raise ValueError("src must be a [heads, T, D] view of out's dtype with unit stride along D")
+    batch = _bounds(cu_seqlens, start)
+    _call(device, stream, "ris_rope_packed", _ptr(src), src.stride(0), src.stride(1), _ptr(out), _dtype_code(out),
+          H, T, D, _ptr(cu_seqlens), _ptr(start), batch, ctypes.byref(desc))
+    return out
+
+
+def prompt_desc(Q, K, V, out, cu_seqlens, causal=1, scale=0.0):
+    """Descriptor from views Q, out [Hq, T, D] and K, V [Hkv, T, D]."""
+    Hq, T, D = Q.shape
+    return PromptDesc(_dtype_code(Q), _dtype_code(out), Hq, K.shape[0], D, cu_seqlens.numel() - 1, T, causal, scale,
+                      *_strides(Q), *_strides(K), *_strides(V), *_strides(out))
+
+
+def prompt_attn(Q, K, V, cu_seqlens, out, desc, stream=None):
+    """ris_prompt_attn: dense attention of packed prompts.  Q, out [Hq, T, D] and
+    K, V [Hkv, T, D] are views of any head and token strides that are multiples of
+    16 bytes (head columns of a token-major projection output, for instance)."""
+    device = _one_device(Q, K, V, cu_seqlens, out)
+    if not (Q.dtype == K.dtype == V.dtype):
+        raise TypeError("Q, K, V must share a dtype")
+    if _dtype_code(Q) != desc.dtype_in or _dtype_code(out) != desc.dtype_out:
+        raise TypeError("Q and out dtypes must match the descriptor")
+    _need_rows((desc.Hq, desc.T, desc.D), Q, out)
+    _need_rows((desc.Hkv, desc.T, desc.D), K, V)
+    strides = (*_strides(Q), *_strides(K), *_strides(V), *_strides(out))
+    if strides != tuple(getattr(desc, f"{x}_{y}") for x in "qkvo" for y in ("head", "token")):
+        raise ValueError("strides must match the descriptor")
+    if _bounds(cu_seqlens) != desc.batch:
+        raise ValueError("cu_seqlens must hold the descriptor's batch + 1 offsets")
+    _call(device, stream, "ris_prompt_attn", _ptr(Q), _ptr(K), _ptr(V), _ptr(cu_seqlens), _ptr(out), ctypes.byref(desc))
+    return out
+
+
+def kv4_cache(batch, Hkv, max_len, D, device="cuda"):
+    """Empty 4-bit cache: codes K4, V4 [batch, Hkv, max_len, D / 2] and scales S
+    [batch, Hkv, max_len, 2, D / 32], uint8."""
+    import torch
+    codes = [torch.zeros(batch, Hkv, max_len, D // 2, dtype=torch.uint8, device=device) for _ in range(2)]
+    return codes[0], codes[1], torch.zeros(batch, Hkv, max_len, 2, D // KV4_BLOCK, dtype=torch.uint8, device=device)
+
+
+def _need_cache(K4, V4, S, batch, Hkv, D):
+    import torch
+    if not (K4.dtype == V4.dtype == S.dtype == torch.uint8):
+        raise TypeError("K4, V4 and S must be uint8")
+    _need_dense(K4, V4, S)
+    max_len = K4.shape[2] if K4.dim() == 4 else 0
+    if (tuple(K4.shape) != (batch, Hkv, max_len, D // 2) or V4.shape != K4.shape
+            or tuple(S.shape) != (batch, Hkv, max_len, 2, D // KV4_BLOCK)):
+        raise ValueError("K4 and V4 must be [batch, Hkv, max_len, D / 2] and S [batch, Hkv, max_len, 2, D / 32]")
+    return max_len
+
+
+def _kv4(K, V, cu_seqlens, K4, V4, S, start):
+    device = _one_device(K, V, cu_seqlens, K4, V4, S, start)
+    if K.dtype != V.dtype:
+        raise TypeError("K and V must share a dtype")
+    Hkv, T, D = K.shape
+    _need_rows((Hkv, T, D), K, V)
+    batch = _bounds(cu_seqlens, start)
+    max_len = _need_cache(K4, V4, S, batch, Hkv, D)
+    return device, Kv4Desc(_dtype_code(K), Hkv, D, batch, T, max_len, *_strides(K), *_strides(V))
+
+
+def kv4_store(K, V, cu_seqlens, K4, V4, S, start=None, stream=None):
+    """ris_kv4_store: rows K, V [Hkv, T, D] (views as in ``prompt_attn``) quantised
+    into the cache, token i of sequence b at position start[b] + i (start None: i)."""
+    device, d = _kv4(K, V, cu_seqlens, K4, V4, S, start)
+    _call(device, stream, "ris_kv4_store", _ptr(K), _ptr(V), _ptr(cu_seqlens), _ptr(start), _ptr(K4), _ptr(V4),
+          _ptr(S), ctypes.byref(d))
+
+
+def kv4_load(K4, V4, S, cu_seqlens, K, V, start=None, stream=None):
+    """ris_kv4_load: the cache's values at those positions into K, V [Hkv, T, D]."""
+    device, d = _kv4(K, V, cu_seqlens, K4, V4, S, start)
+    _call(device, stream, "ris_kv4_load", _ptr(K4), _ptr(V4), _ptr(S), _ptr(cu_seqlens), _ptr(start), _ptr(K),
+          _ptr(V), ctypes.byref(d))
+
+
+def kv4_decode_desc(Q, K4, out, anchor_stride=0, window=0, sink=0, scale=0.0):
+    """Descriptor from Q [B, Hq, D], the codes K4 [B, Hkv, max_len, D / 2] and out."""
+    B, Hq, D = Q.shape
+    return ris.DecodeDesc(_dtype_code(Q), _dtype_code(out), B, Hq, K4.shape[1], D, K4.shape[2], anchor_stride, window,
+                          sink, scale)
+
+
+def kv4_decode_workspace_bytes(desc):
+    v = lib().ris_kv4_decode_workspace_bytes(ctypes.byref(desc))
+    if v < 0:
+        raise ris.RisError(int(v), "ris_kv4_decode_workspace_bytes")
+    return int(v)
+
+
+def kv4_decode_attn(Q, K4, V4, S, pos, anchor_ptr, anchor_idx, out, workspace, desc, stream=None):
+    """ris_kv4_decode_attn; workspace is a device uint8 tensor of at least
+    kv4_decode_workspace_bytes(desc) bytes.  anchor_ptr and anchor_idx may be None
+    where the descriptor's anchor_stride is 0."""
+    import torch
+    device = _one_device(Q, K4, V4, S, pos, anchor_ptr, anchor_idx, out, workspace)
+    _need_dense(Q, pos, anchor_ptr, anchor_idx, out, workspace)
+    if pos.dtype != torch.int64 or pos.numel() != desc.batch:
+        raise ValueError("pos must be int64 and hold B entries")
+    if desc.anchor_stride > 0:
+        if anchor_ptr is None or anchor_idx is None:
+            raise ValueError("anchor_ptr and anchor_idx are needed where anchor_stride > 0")
+        if anchor_ptr.dtype != torch.int64 or anchor_idx.dtype != torch.int32:
+            raise TypeError("anchor_ptr must be int64, anchor_idx int32")
+        if anchor_ptr.numel() != desc.batch * (desc.Hkv + 1) or anchor_idx.numel() < desc.batch * desc.anchor_stride:
+            raise ValueError("anchor_ptr must hold B * (Hkv + 1) entries and anchor_idx B * anchor_stride")
+    if _dtype_code(Q) != desc.dtype_in or _dtype_code(out) != desc.dtype_out:
+        raise TypeError("Q and out dtypes must match the descriptor")
+    if tuple(Q.shape) != (desc.batch, desc.Hq, desc.D) or out.shape != Q.shape:
+        raise ValueError("Q and out must be [B, Hq, D] as in the descriptor")
+    if _need_cache(K4, V4, S, desc.batch, desc.Hkv, desc.D) != desc.max_len:
+        raise ValueError("the cache's max_len must match the descriptor")
+    nbytes = workspace.numel() * workspace.element_size()
+    _call(device, stream, "ris_kv4_decode_attn", _ptr(Q), _ptr(K4), _ptr(V4), _ptr(S), _ptr(pos), _ptr(anchor_ptr),
+          _ptr(anchor_idx), _ptr(out), _ptr(workspace), nbytes, ctypes.byref(desc))
+    return out
+
+
+def logprob_desc(logits, n_targets=1, top_k=0):
+    """Descriptor from logits [rows, vocab] (unit stride along vocab)."""
+    rows, vocab = logits.shape
+    return LogprobDesc(_dtype_code(logits), n_targets, top_k, rows, vocab, max(logits.stride(0), vocab) if rows > 1 else vocab)
+
+
+def logprobs_workspace_bytes(desc):
+    v = lib().ris_logprobs_workspace_bytes(ctypes.byref(desc))
+    if v < 0:
+        raise ris.RisError(int(v), "ris_logprobs_workspace_bytes")
+    return int(v)
+
+
+def logprobs(logits, targets, logprob, entropy, top_ids, top_logprob, workspace, desc, stream=None):
+    """ris_logprobs: rows of logits [rows, vocab] scored.  targets int64 and
+    logprob float32 [rows, n_targets], entropy float32 [rows] or None, top_ids
+    int64 and top_logprob float32 [rows, top_k]; what the descriptor counts 0 of
+    may be None.  workspace: at least logprobs_workspace_bytes(desc) bytes."""
+    import torch
+    device = _one_device(logits, targets, logprob, entropy, top_ids, top_logprob, workspace)
+    if tuple(logits.shape) != (desc.rows, desc.vocab) or logits.stride(1) != 1 and desc.vocab > 1:
+        raise ValueError("logits must be [rows, vocab] as in the descriptor, unit stride along vocab")
+    if desc.rows > 1 and logits.stride(0) != desc.row_stride or _dtype_code(logits) != desc.dtype:
+        raise ValueError("the logits' row stride and dtype must match the descriptor")
+    _need_dense(targets, logprob, entropy, top_ids, top_logprob, workspace)
+    wanted = ((targets, (desc.rows, desc.n_targets), torch.int64), (logprob, (desc.rows, desc.n_targets), torch.float32),
+              (top_ids, (desc.rows, desc.top_k), torch.int64), (top_logprob, (desc.rows, desc.top_k), torch.float32))
+    for t, shape, dtype in wanted:
+        if shape[1] and t is None or t is not None and (tuple(t.shape) != shape or t.dtype != dtype):
+            raise ValueError("targets and logprob must be [rows, n_targets], top_ids and top_logprob [rows, top_k] "
+                             "(ids int64, the others float32)")
+    if entropy is not None and (tuple(entropy.shape) != (desc.rows,) or entropy.dtype != torch.float32):
+        raise ValueError("entropy must be float32 [rows]")
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _call(device, stream, "ris_logprobs", _ptr(logits), _ptr(targets), _ptr(logprob), _ptr(entropy), _ptr(top_ids),
+          _ptr(top_logprob), _ptr(workspace), nbytes, ctypes.byref(desc))
+    return logprob

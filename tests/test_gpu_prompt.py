@@ -1,0 +1,273 @@
+"""Packed RoPE and packed prompt attention on the GPU vs the oracle."""
+import numpy as np
+import pytest
+
+from gpu_common import say, torch
+from oracle import rope as o_rope
+from oracle import serve as o_srv
+from serve_common import attn_bar, bounds, head_view, need_serve, replay_checked
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def inputs(Hq, Hkv, T, D, dtype, seed=0, std=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return [(torch.randn(h, T, D, generator=g) * std).to(dtype).cuda() for h in (Hq, Hkv, Hkv)]
+
+
+def run(serve, q, k, v, cu, out_dtype=None, causal=1, scale=0.0, out=None):
+    if out is None:
+        out = torch.empty(q.shape, dtype=out_dtype or q.dtype, device="cuda")
+    return serve.prompt_attn(q, k, v, cu, out, serve.prompt_desc(q, k, v, out, cu, causal=causal, scale=scale))
+
+
+def check(got, q, k, v, lens, causal, scale, first=0):
+    cu = np.cumsum([first] + list(lens))
+    want = o_srv.packed_attention(*(x.double().cpu().numpy() for x in (q, k, v)), cu, scale, causal)
+    for a, b in zip(cu[:-1], cu[1:]):
+        if a == b:
+            continue
+        bar = attn_bar(q[:, a:b], k[:, a:b], v[:, a:b], b - a, scale, want[:, a:b], q.dtype, got.dtype)
+        err = np.abs(got[:, a:b].double().cpu().numpy() - want[:, a:b])
+        say(f"  {a}..{b}: {float((err / bar).max()):.3f} of the bar")
+        assert (err <= bar).all()
+
+
+LENS = [[1], [2, 1, 1], [31, 32, 33], [64, 63, 65], [127, 128, 129], [0, 5, 0, 0, 200, 0], [255, 257], [300, 7, 512]]
+
+
+@pytest.mark.parametrize("lens", LENS, ids=str)
+@pytest.mark.parametrize("dtype,out_dtype,Hq,Hkv,D,causal", [
+    (BF16, F32, 6, 1, 128, 1), (BF16, BF16, 4, 2, 64, 1), (BF16, BF16, 3, 3, 128, 0), (F32, F32, 4, 2, 64, 1),
+    (F32, F32, 2, 1, 128, 0), (F32, BF16, 2, 2, 128, 1)])
+def test_prompt_attention_matches_the_oracle(lens, dtype, out_dtype, Hq, Hkv, D, causal):
+    serve = need_serve()
+    say(f"prompt {lens} {dtype} {out_dtype} {Hq}/{Hkv} D={D} causal={causal}")
+    q, k, v = inputs(Hq, Hkv, sum(lens), D, dtype, seed=sum(lens))
+    got = run(serve, q, k, v, bounds(lens), out_dtype, causal)
+    check(got, q, k, v, lens, causal, D**-0.5)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", [(12, 2, 128), (32, 4, 64), (24, 2, 64), (5, 5, 128), (7, 1, 64)])
+def test_prompt_group_sizes(Hq, Hkv, D):
+    serve = need_serve()
+    lens = [70, 130]
+    q, k, v = inputs(Hq, Hkv, 200, D, BF16, seed=Hq)
+    check(run(serve, q, k, v, bounds(lens), F32), q, k, v, lens, 1, D**-0.5)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_prompt_views_of_a_projection(dtype):
+    """Q, K, V as head columns of one token-major buffer, out token-major: the bits
+    of contiguous tensors; what lies between and behind the rows stays."""
+    serve = need_serve()
+    Hq, Hkv, D, lens = 6, 2, 128, [90, 1, 77]
+    T = sum(lens) + 9                                   # nine tokens of no sequence
+    buf = torch.randn(T, (Hq + 2 * Hkv) * D + 8, generator=torch.Generator().manual_seed(1)).to(dtype).cuda()
+    q, k, v = (head_view(buf, a, n, D) for a, n in ((0, Hq), (Hq, Hkv), (Hq + Hkv, Hkv)))
+    keep = torch.full((T, Hq * D + 16), 7.0, dtype=dtype, device="cuda")
+    got = run(serve, q, k, v, bounds(lens), out=head_view(keep, 0, Hq, D))
+    same = run(serve, q.contiguous(), k.contiguous(), v.contiguous(), bounds(lens))
+    assert torch.equal(got[:, :sum(lens)], same[:, :sum(lens)])
+    assert (keep[sum(lens):] == 7).all() and (keep[:, Hq * D:] == 7).all()
+    check(got, q, k, v, lens, 1, D**-0.5)
+
+
+def test_prompt_one_token_views_and_shared_heads():
+    """T = 1 with odd strides on its only row; one K and V for all heads (stride 0)."""
+    serve = need_serve()
+    q, k, v = inputs(4, 1, 1, 64, BF16, seed=2)
+    odd = torch.empty(4, 3, 64, dtype=BF16, device="cuda")[:, 1:2]
+    assert torch.equal(run(serve, q, k, v, bounds([1]), out=odd).float(), v.float().expand(4, 1, 64))
+    q, k, v = inputs(6, 1, 150, 64, BF16, seed=3)
+    got = run(serve, q, k.expand(3, 150, 64), v.expand(3, 150, 64), bounds([150]))
+    assert torch.equal(got, run(serve, q, k, v, bounds([150])))
+
+
+@pytest.mark.parametrize("dtype,D", [(BF16, 128), (BF16, 64), (F32, 128), (F32, 64)])
+def test_what_a_token_does_not_attend_to_does_not_reach_it(dtype, D):
+    """Infinities and NaN in the keys and values of later tokens, of the next
+    sequence and of no sequence; the tokens that attend to them get what the
+    formula gives."""
+    serve = need_serve()
+    lens, Hq, Hkv = [100, 60, 200], 2, 1
+    T = 380
+    q, k, v = inputs(Hq, Hkv, T, D, dtype, seed=4)
+    clean = run(serve, q, k, v, bounds(lens))
+    kb, vb = k.clone(), v.clone()
+    kb[:, 150:160], vb[:, 150:160] = float("nan"), float("inf")       # the end of the second sequence
+    vb[:, 290, 3], vb[:, 300, 5] = float("inf"), float("nan")         # two elements in the third
+    vb[:, 310, 3] = float("-inf")
+    kb[:, 360:], vb[:, 360:] = float("inf"), float("nan")             # tokens of no sequence
+    got = run(serve, q, kb, vb, bounds(lens))
+    assert torch.equal(got[:, :150], clean[:, :150]) and torch.equal(got[:, 160:290], clean[:, 160:290])
+    assert got[:, 150:160].isnan().all()
+    third, ref = got[:, 290:360].float(), clean[:, 290:360].float()
+    assert (third[:, :20, 3] == float("inf")).all() and third[:, 20:, 3].isnan().all()      # inf, then inf - inf
+    assert not third[:, :10, 5].isnan().any() and third[:, 10:, 5].isnan().all()
+    others = [d for d in range(D) if d not in (3, 5)]
+    assert torch.equal(third[..., others], ref[..., others])
+
+
+def test_prompt_offsets_outside_the_buffer_are_clipped():
+    serve = need_serve()
+    q, k, v = inputs(2, 1, 100, 64, BF16, seed=5)
+    cu = torch.tensor([-7, 30, 20, 1 << 40], dtype=torch.int64, device="cuda")      # [0, 30), none, [20, 100)
+    out = torch.zeros(2, 100, 64, dtype=BF16, device="cuda")
+    run(serve, q, k, v, cu, out=out)
+    check(out[:, :20], q[:, :20], k[:, :20], v[:, :20], [20], 1, 0.125)
+    check(out[:, 30:], q[:, 30:], k[:, 30:], v[:, 30:], [], 1, 0.125)
+    want = o_srv.packed_attention(*(x.double().cpu().numpy() for x in (q, k, v)), [20, 100], 0.125)
+    bar = attn_bar(q, k, v, 80, 0.125, want, BF16, BF16)
+    assert (np.abs(out.double().cpu().numpy() - want)[:, 30:] <= bar[:, 30:]).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("scale,std", [(0.5, 8.0), (1e-3, 1.0), (0.125, 1e-3)])
+def test_prompt_scales(dtype, scale, std):
+    """Nearly one-hot and nearly uniform softmax rows, an explicit scale."""
+    serve = need_serve()
+    q, k, v = inputs(2, 1, 333, 64, dtype, seed=6, std=std)
+    check(run(serve, q, k, v, bounds([333]), F32, 1, scale), q, k, v, [333], 1, float(np.float32(scale)))
+
+
+def test_prompt_running_maximum_rises_and_falls():
+    """Keys whose scores rise over the sequence, fall, and jump far within a tile."""
+    serve = need_serve()
+    T, D = 700, 128
+    q, k, v = inputs(1, 1, T, D, BF16, seed=7)
+    for shape in (torch.linspace(0, 40, T), torch.linspace(40, 0, T), torch.arange(T) % 97 * 0.5,
+                  -60 + torch.zeros(T), torch.where(torch.arange(T) == 350, 60.0, 0.0)):
+        k2 = k.clone()
+        k2[0, :, 0] = shape.to(BF16).cuda()
+        q2 = q.clone()
+        q2[..., 0] = 11.0
+        check(run(serve, q2, k2, v, bounds([T]), F32), q2, k2, v, [T], 1, D**-0.5)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,lens,causal", [(12, 2, 128, [20011, 1000, 4097], 1), (8, 1, 64, [33000], 1),
+                                                  (2, 1, 128, [9001], 0)])
+def test_prompt_long_sequences(Hq, Hkv, D, lens, causal):
+    """Rows here and there of long prompts, against float64."""
+    serve = need_serve()
+    say(f"long {Hq}/{Hkv} D={D} {lens}")
+    q, k, v = inputs(Hq, Hkv, sum(lens), D, BF16, seed=8)
+    got = run(serve, q, k, v, bounds(lens), F32, causal)
+    rng = np.random.default_rng(0)
+    for a, n in zip(np.cumsum([0] + lens[:-1]), lens):
+        for i in [0, 1, n - 1, n // 2] + list(rng.integers(0, n, 12)):
+            m = i + 1 if causal else n
+            for h in range(Hq):
+                s = (k[h * Hkv // Hq, a:a + m].double() @ q[h, a + i].double()) * D**-0.5
+                want = torch.softmax(s, 0) @ v[h * Hkv // Hq, a:a + m].double()
+                bar = attn_bar(q[h, a:a + n], k[0, a:a + n], v[0, a:a + n], m, D**-0.5, want, BF16, F32)
+                assert ((got[h, a + i].double() - want).abs() <= bar).all(), (n, i, h)
+
+
+def test_prompt_many_sequences():
+    """More sequences than a wave looks at in a step, most of one or two tokens."""
+    serve = need_serve()
+    rng = np.random.default_rng(9)
+    lens = [int(x) for x in rng.choice([0, 1, 1, 2, 3, 150], 300)]
+    q, k, v = inputs(2, 1, sum(lens), 64, BF16, seed=9)
+    got = run(serve, q, k, v, bounds(lens), F32)
+    want = o_srv.packed_attention(*(x.double().cpu().numpy() for x in (q, k, v)), np.cumsum([0] + lens), 0.125)
+    assert (np.abs(got.double().cpu().numpy() - want) <= attn_bar(q, k, v, 150, 0.125, want, BF16, F32)).all()
+
+
+def test_prompt_offsets_beyond_32_bits():
+    """Rows whose byte and element offsets pass 2^32 and 2^31."""
+    serve = need_serve()
+    T, D, wide = 40_000, 64, 65_536
+    big = torch.empty(T, wide, dtype=BF16, device="cuda")              # 5.2 GB
+    q, k, v = inputs(2, 1, T, D, BF16, seed=10)
+    for i, x in enumerate((q[:1], q[1:], k, v)):
+        big[:, i * D:(i + 1) * D] = x[0]
+    qv, kv, vv = head_view(big, 0, 2, D), head_view(big, 2, 1, D), head_view(big, 3, 1, D)
+    lens = [39_000, 1000]
+    got = run(serve, qv, kv, vv, bounds(lens), out=head_view(big, 100, 2, D))
+    assert torch.equal(got, run(serve, q, k, v, bounds(lens)))
+
+
+def test_prompt_is_deterministic_on_another_stream_and_in_a_graph():
+    serve = need_serve()
+    lens, Hq, Hkv, D = [300, 41], 4, 2, 128
+    q, k, v = inputs(Hq, Hkv, 341, D, BF16, seed=11)
+    cu, out = bounds(lens), torch.empty(Hq, 341, D, dtype=BF16, device="cuda")
+    first = run(serve, q, k, v, cu, out=out).clone()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    other = torch.empty_like(out)
+    serve.prompt_attn(q, k, v, cu, other, serve.prompt_desc(q, k, v, other, cu), stream=s)
+    s.synchronize()
+    assert torch.equal(first, other)
+
+    def change(i):
+        q.copy_(inputs(Hq, Hkv, 341, D, BF16, seed=20 + i)[0])
+        cu.copy_(bounds([300 - 37 * i, 41 + 30 * i]))
+    replay_checked(lambda: run(serve, q, k, v, cu, out=out), [out], change)
+
+
+# ---- RoPE on packed sequences
+
+KINDS = [("plain", 0, 1.0), ("linear", 1, 2.0), ("yarn", 2, 2.0)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("kind,code,factor", KINDS)
+@pytest.mark.parametrize("D,lens,start", [(128, [1, 0, 70, 3], None), (64, [5, 40_001], [60_000, 3]), (2, [300, 1], [0, 9]),
+                                          (512, [3, 3], None), (96, [20, 9], [1, 1 << 40])])
+def test_rope_packed_is_rope_from_at_each_sequences_positions(dtype, kind, code, factor, D, lens, start):
+    """The bits of ris_rope_from on every sequence alone, whose own parity with the
+    oracle is held elsewhere; tokens of no sequence stay."""
+    serve = need_serve()
+    from paper_2607_21927_amd import ris
+    say(f"rope {kind} D={D} {lens} {start}")
+    T = sum(lens) + 4
+    desc = ris.rope_desc(code, 1e6, orig_max_pos=32768, factor=factor)
+    buf = torch.randn(T, 3 * D, generator=torch.Generator().manual_seed(D)).to(dtype).cuda()
+    src = head_view(buf, 0, 3, D)
+    out = torch.full((3, T, D), 9.0, dtype=dtype, device="cuda")
+    st = None if start is None else torch.tensor(start, device="cuda")
+    serve.rope_packed(src, out, bounds(lens), desc, start=st)
+    at = 0
+    for b, n in enumerate(lens):
+        if n:
+            want = ris.rope_from(src[:, at:at + n], torch.empty(3, n, D, dtype=dtype, device="cuda"), desc,
+                                 pos0=start[b] if start else 0)
+            assert torch.equal(out[:, at:at + n], want)
+        at += n
+    assert (out[:, at:] == 9).all()
+
+
+def test_rope_packed_matches_the_oracle_and_rotates_in_place():
+    serve = need_serve()
+    from paper_2607_21927_amd import ris
+    x = torch.randn(2, 90, 64, generator=torch.Generator().manual_seed(3)).cuda()
+    lens, start = [40, 50], [7, 65_000]
+    want = np.concatenate([o_rope.apply(x[:, a:b].double().cpu().numpy(), o_rope.YARN, 1e4, p, 4.0, 2048)
+                           for a, b, p in ((0, 40, 7), (40, 90, 65_000))], 1)
+    serve.rope_packed(x, x, bounds(lens), ris.rope_desc(ris.ROPE_YARN, 1e4, orig_max_pos=2048, factor=4.0),
+                      start=torch.tensor(start, device="cuda"))
+    np.testing.assert_allclose(x.cpu().numpy(), want, atol=2e-6)
+
+
+def test_rope_packed_many_sequences_and_graph():
+    serve = need_serve()
+    from paper_2607_21927_amd import ris
+    B, D = 5000, 64
+    desc = ris.rope_desc(ris.ROPE_PLAIN, 1e4)
+    lens = [int(x) for x in np.random.default_rng(1).choice([0, 1, 1, 2], B)]
+    T = sum(lens)
+    src = torch.randn(2, T, D, generator=torch.Generator().manual_seed(4)).cuda()
+    start = torch.arange(B, device="cuda") * 3
+    out = torch.empty_like(src)
+    cu = bounds(lens)
+    serve.rope_packed(src, out, cu, desc, start=start)
+    pos = np.concatenate([np.arange(n) + 3 * b for b, n in enumerate(lens)])
+    c, s = (torch.tensor(x).float().cuda() for x in o_rope.cos_sin(o_rope.PLAIN, D, 1e4, pos))
+    want = torch.cat([src[..., :32] * c - src[..., 32:] * s, src[..., 32:] * c + src[..., :32] * s], -1)
+    assert (out - want).abs().max() <= 8 * 2.0**-24 * src.abs().max()
+    replay_checked(lambda: serve.rope_packed(src, out, cu, desc, start=start), [out], lambda i: start.add_(11 * i))
