@@ -160,27 +160,50 @@ __device__ __forceinline__ void load_codes(const uint8_t* p, uint32_t (&u)[D / 3
     }
 }
 
+// The codes of the 32 keys from virtual position v0 of the row (uniform) on.  Most
+// tiles lie within the anchor or within the window, where a key is one load or none.
 template <int D>
 __device__ __forceinline__ void load_tile(const RowSegs& r, const uint8_t* Kr, const uint8_t* Vr, const uint8_t* Sr,
                                           int64_t v0, int li, int lg, Kv4Tile<D>& T) {
     const int lane = li + 16 * lg;
-    uint32_t vm = 0;
+    const int row4 = lane >> 2, part = lane & 3;
+    uint32_t jk[2], jv[2], vm = 0xFFFFFFFFu;            // max_len <= 2^31: a key fits 32 bits
+    if (v0 >= r.na && v0 + kTileKeys <= r.na + r.nw) {
+        const uint32_t j0 = (uint32_t)(r.w_lo + (v0 - r.na));
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            jk[kb] = j0 + 16 * kb + li;
+            jv[kb] = j0 + 16 * kb + row4;
+        }
+    } else {
+        const bool anchor = v0 + kTileKeys <= r.na;
+        vm = 0;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            int64_t j;
+            if (anchor) {
+                const int a = r.aidx[v0 + 16 * kb + li];
+                j = a >= r.ns && a < r.w_lo ? a : -1;
+            } else {
+                j = key_of(r, v0 + 16 * kb + li);
+            }
+            vm |= (uint32_t)(__ballot(j >= 0) & 0xFFFFull) << (16 * kb);
+            jk[kb] = j >= 0 ? (uint32_t)j : 0u;         // row 0 always exists
+            jv[kb] = (uint32_t)__shfl((int)jk[kb], row4);
+        }
+    }
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
-        const int64_t j = key_of(r, v0 + 16 * kb + li);
-        vm |= (uint32_t)(__ballot(j >= 0) & 0xFFFFull) << (16 * kb);
-        const int64_t jj = j >= 0 ? j : 0;              // row 0 always exists
-        load_codes<D>(Kr + jj * (D / 2) + lg * (D / 8), T.k[kb]);
-        T.ks[kb] = Sr[jj * (D / 16) + lg * D / 128];
-        const int64_t jv = __shfl((int)jj, lane >> 2);  // max_len <= 2^31: a key fits 32 bits
-        load_codes<D>(Vr + jv * (D / 2) + (lane & 3) * (D / 8), T.v[kb]);
-        T.vs[kb] = Sr[jv * (D / 16) + D / 32 + (lane & 3) * D / 128];
+        load_codes<D>(Kr + (uint64_t)jk[kb] * (D / 2) + lg * (D / 8), T.k[kb]);
+        T.ks[kb] = Sr[(uint64_t)jk[kb] * (D / 16) + lg * D / 128];
+        load_codes<D>(Vr + (uint64_t)jv[kb] * (D / 2) + part * (D / 8), T.v[kb]);
+        T.vs[kb] = Sr[(uint64_t)jv[kb] * (D / 16) + D / 32 + part * D / 128];
     }
     T.valid = vm;
 }
 
 template <int D>
-__global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_kv4_decode(DecodeParams p, const uint8_t* S, float c) {
+__global__ __launch_bounds__(64 * kDecodeWaves, 4) void k_kv4_decode(DecodeParams p, const uint8_t* S, float c) {
     constexpr int SL = D / 32;         // k-slices of the score product
     constexpr int DB = D / 16;         // 16-dim blocks of the output
     constexpr int VS = D + 16;         // V row stride in LDS (bf16 elements)
@@ -226,22 +249,6 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_kv4_decode(DecodeParam
         Kv4Tile<D> cur;
         load_tile<D>(r, Kr, Vr, Sr, v_first, li, lg, cur);
         for (int64_t v0 = v_first; v0 < total; v0 += stride) {
-            Kv4Tile<D> nxt;
-            const bool more = v0 + stride < total;
-            if (more) load_tile<D>(r, Kr, Vr, Sr, v0 + stride, li, lg, nxt);
-
-            // V rows as bf16 into this wave's LDS, row-major.  A slot without a key
-            // has weight 0, which times a NaN would be one: its row is 0.
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb) {
-                const bool ok = (cur.valid >> (16 * kb + (lane >> 2))) & 1u;
-                const float sc = scale_of(ok ? cur.vs[kb] : 127u);
-                uint16_t* vr = vw + (16 * kb + (lane >> 2)) * VS + (lane & 3) * (D / 4);
-#pragma unroll
-                for (int s = 0; s < SL; ++s)
-                    *reinterpret_cast<u32x4_t*>(vr + 8 * s) = decode8(ok ? cur.v[kb][s] : 0u, sc);
-            }
-
             // S^T = K Q^T: lane l holds head l % 16 at key slots 16 kb + 4 (l / 16) + i.
             f32x4_t st[2];
 #pragma unroll
@@ -253,6 +260,20 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_kv4_decode(DecodeParam
                     st[kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(decode8(cur.k[kb][s], sc)),
                                                                       as_bf16x8(qf[s]), st[kb], 0, 0, 0);
             }
+            // V rows as bf16 into this wave's LDS, row-major.  A slot without a key
+            // has weight 0, which times a NaN would be one: its row is 0.
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                const bool ok = (cur.valid >> (16 * kb + (lane >> 2))) & 1u;
+                const float sc = scale_of(ok ? cur.vs[kb] : 127u);
+                uint16_t* vr = vw + (16 * kb + (lane >> 2)) * VS + (lane & 3) * (D / 4);
+#pragma unroll
+                for (int s = 0; s < SL; ++s)
+                    *reinterpret_cast<u32x4_t*>(vr + 8 * s) = decode8(ok ? cur.v[kb][s] : 0u, sc);
+            }
+            const uint32_t valid = cur.valid;
+            // the next tile's codes take the registers that these have left
+            if (v0 + stride < total) load_tile<D>(r, Kr, Vr, Sr, v0 + stride, li, lg, cur);
 
             // Online softmax over the tile (scores in the log2 domain).
             float sc[2][4];
@@ -261,32 +282,34 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_kv4_decode(DecodeParam
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const bool ok = (cur.valid >> (16 * kb + 4 * lg + i)) & 1u;
+                    const bool ok = (valid >> (16 * kb + 4 * lg + i)) & 1u;
                     sc[kb][i] = ok ? st[kb][i] * c : -INFINITY;
                     mx = fmaxf(mx, sc[kb][i]);
                 }
             mx = quad_max16(mx);
-            const float m_new = fmaxf(m_run, mx);
-            const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+            // The reference moves, and what was summed is rescaled, only where a score
+            // exceeds it by 2^8 in weight.
+            if (__any(mx > m_run + 8.f)) {
+                const float m_new = fmaxf(m_run, mx);
+                const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+                m_run = m_new;
+                l_run *= alpha;
+                // lane l holds the output of heads 4 (l / 16) + i
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float a = __shfl(alpha, 4 * lg + i);
+#pragma unroll
+                    for (int db = 0; db < DB; ++db) o[db][i] *= a;
+                }
+            }
             float pv[2][4];
-            float ps = 0.f;
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    pv[kb][i] = __builtin_amdgcn_exp2f(sc[kb][i] - m_new);
-                    ps += pv[kb][i];
+                    pv[kb][i] = __builtin_amdgcn_exp2f(sc[kb][i] - m_run);
+                    l_run += pv[kb][i];
                 }
-            l_run = l_run * alpha + ps;
-            m_run = m_new;
-
-            // Rescale the output rows: lane l holds heads 4 (l / 16) + i.
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float a = __shfl(alpha, 4 * lg + i);
-#pragma unroll
-                for (int db = 0; db < DB; ++db) o[db][i] *= a;
-            }
 
             // P as the A operand: head l % 16, k slots 8 (l / 16) + e hold keys
             // 4 (l / 16) + e (e < 4) and 16 + 4 (l / 16) + e - 4 (e >= 4); V as the B
@@ -302,7 +325,6 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_kv4_decode(DecodeParam
                 const u32x4_t vb = {a.x, a.y, e.x, e.y};
                 o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(pk), as_bf16x8(vb), o[db], 0, 0, 0);
             }
-            if (more) cur = nxt;
         }
     }
     merge_waves<D>(p, row, reinterpret_cast<float*>(vlds), m_run, l_run, o);

@@ -83,8 +83,16 @@ int validate_kv4_decode(const ris_decode_desc* d) {
     return RIS_OK;
 }
 
-// Waves per row: the tiles of a typical row (its share of the anchor slice, window and
-// initial tokens) dealt to ~2048 waves over the batch, whole workgroups of them.
+// Waves per row for the tiles of a typical row (its share of the anchor slice, window
+// and initial tokens).  One workgroup, whose output needs no merge in another launch,
+// to kSoloTiles tiles and beyond where rows are many (2 rows of 16 tiles at D = 128:
+// 7.3 us with 4 waves, 8.2 with 8, 7.3 with 16; 24 tiles 9.1, 9.1, 8.1; 128 rows of 32
+// tiles 11.6, 11.2, 11.1, of 64 19.1, 15.8, 14.0; 256 rows of 64 19.5, 19.8, 21.4; 512 rows
+// of 128 48, 53, 54).  Else a wave to a tile up to kWaves in all: rows of one length
+// are fastest with 2048 (64 rows of 65,536 keys 105 us with 2048, 110 with 4096, 111 with
+// 8192), rows of lengths between a quarter and all of that with 8192 (87, 81, 80).  A row
+// takes kMostWaves at most (2 rows of 33,000 keys: 11.9 us, 12.9 with twice as many).
+constexpr int64_t kSoloTiles = 16, kWaves = 4096, kMostWaves = 512;
 int64_t kv4_decode_waves(const ris_decode_desc& d) {
     const int64_t win = d.window < d.max_len ? d.window : d.max_len;
     const int64_t snk = d.sink < d.max_len ? d.sink : d.max_len;
@@ -92,11 +100,11 @@ int64_t kv4_decode_waves(const ris_decode_desc& d) {
     if (keys > d.max_len) keys = d.max_len;
     const int64_t tiles = (keys + ris::kDecodeTileKeys - 1) / ris::kDecodeTileKeys;
     const int64_t rows = (int64_t)d.batch * d.Hkv;
-    int64_t parts = (ris::kDecodeTargetWaves + rows - 1) / rows;
-    if (parts > tiles) parts = tiles;
-    parts = (parts + ris::kDecodeWaves - 1) / ris::kDecodeWaves * ris::kDecodeWaves;
-    if (parts < ris::kDecodeWaves) parts = ris::kDecodeWaves;
-    return parts > ris::kDecodeMaxParts ? ris::kDecodeMaxParts : parts;
+    if (tiles <= kSoloTiles || tiles <= rows / 4) return ris::kDecodeWaves;
+    int64_t waves = (kWaves + rows - 1) / rows;
+    if (waves > tiles) waves = tiles;
+    if (waves > kMostWaves) waves = kMostWaves;
+    return (waves + ris::kDecodeWaves - 1) / ris::kDecodeWaves * ris::kDecodeWaves;
 }
 
 int64_t kv4_decode_workspace(const ris_decode_desc& d) {
