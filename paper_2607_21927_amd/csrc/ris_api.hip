@@ -154,21 +154,24 @@ int make_rope_table(const ris_rope_desc* desc, int32_t D, int64_t window, RopeTa
     }
     const int half = D / 2;
     const double base = desc->base;
+    double lo = 0.0, hi = 1.0;                          // YaRN's band edges
+    if (desc->kind == RIS_ROPE_YARN) {
+        const double b_slow = desc->beta_slow > 0.0 ? desc->beta_slow : 1.0;
+        const double b_fast = desc->beta_fast > 0.0 ? desc->beta_fast : 32.0;
+        const double L0 = (double)desc->orig_max_pos;
+        const double c_fast = D * log(L0 / (b_fast * 2.0 * M_PI)) / (2.0 * log(base));
+        const double c_slow = D * log(L0 / (b_slow * 2.0 * M_PI)) / (2.0 * log(base));
+        lo = floor(c_fast), hi = ceil(c_slow);
+        if (lo < 0.0) lo = 0.0;
+        if (hi > D - 1) hi = D - 1;
+        if (lo == hi) hi += 0.001;
+    }
     for (int i = 0; i < half; ++i) {
         const double plain = 1.0 / pow(base, 2.0 * i / D);
         double f = plain;
         if (desc->kind == RIS_ROPE_LINEAR) {
             f = plain / s;
         } else if (desc->kind == RIS_ROPE_YARN) {
-            const double b_slow = desc->beta_slow > 0.0 ? desc->beta_slow : 1.0;
-            const double b_fast = desc->beta_fast > 0.0 ? desc->beta_fast : 32.0;
-            const double L0 = (double)desc->orig_max_pos;
-            const double c_fast = D * log(L0 / (b_fast * 2.0 * M_PI)) / (2.0 * log(base));
-            const double c_slow = D * log(L0 / (b_slow * 2.0 * M_PI)) / (2.0 * log(base));
-            double lo = floor(c_fast), hi = ceil(c_slow);
-            if (lo < 0.0) lo = 0.0;
-            if (hi > D - 1) hi = D - 1;
-            if (lo == hi) hi += 0.001;
             double t = (i - lo) / (hi - lo);
             t = t < 0.0 ? 0.0 : (t > 1.0 ? 1.0 : t);
             f = t * (plain / s) + (1.0 - t) * plain;
