@@ -8,4 +8,4 @@ operators around it (``include/ris_serve.h``: packed prompts, the 4-bit cache, l
 probabilities) are bound in ``paper_2607_21927_amd.serve``.
 """
 
-from . import ris, serve  # noqa: F401
+from . import ris  # noqa: F401

@@ -4,11 +4,12 @@ Argument checks and marshalling only, as in ``ris``: every step runs in the HIP
 library, the caller owns every tensor, and the work goes to torch's current HIP
 stream of the tensors' device unless a stream is given.
 """
-import contextlib
 import ctypes
 
+import torch
+
 from . import ris
-from .ris import _check, _dtype_code, _ptr
+from .ris import _dtype_code
 
 MAX_TOP = 64
 KV4_BLOCK = 32          # dimensions that share a scale in the 4-bit cache
@@ -64,12 +65,15 @@ def lib():
     return _lib
 
 
-def _one_device(*ts):
-    """The GPU that holds all of the tensors."""
-    devices = {t.device for t in ts if t is not None}
-    if len(devices) != 1 or next(iter(devices)).type != "cuda":
+def _one_gpu(t, *others):
+    """Index of the GPU that holds all of the tensors."""
+    index = t.get_device()
+    for o in others:
+        if o is not None and o.get_device() != index:
+            index = -1
+    if index < 0:
         raise ValueError("tensors must be on one GPU")
-    return next(iter(devices))
+    return index
 
 
 def _need_dense(*ts):
@@ -78,53 +82,65 @@ def _need_dense(*ts):
             raise ValueError("tensors must be contiguous")
 
 
-def _need_rows(shape, *ts):
-    """[heads, T, D] views whose rows 16-byte accesses can walk; a dimension of
-    one element may have any stride."""
-    for t in ts:
-        if tuple(t.shape) != shape:
-            raise ValueError(f"expected a {shape} view, got {tuple(t.shape)}")
-        if t.stride(2) != 1 or t.data_ptr() % 16 or any(s * t.element_size() % 16 for s in _strides(t)):
-            raise ValueError("rows must be contiguous, bases and strides multiples of 16 bytes")
-
-
-def _strides(t):
-    """Head and token stride of a [heads, T, D] view."""
-    return (t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0)
+def _rows(t, shape):
+    """Head and token stride of a [heads, T, D] view whose rows 16-byte accesses can
+    walk; a dimension of one element counts with stride 0."""
+    if t.shape != shape:
+        raise ValueError(f"expected a {shape} view, got {tuple(t.shape)}")
+    head, token, one = t.stride()
+    if shape[0] == 1:
+        head = 0
+    if shape[1] == 1:
+        token = 0
+    per = 16 // t.element_size()
+    if one != 1 or t.data_ptr() % 16 or head % per or token % per:
+        raise ValueError("rows must be contiguous, bases and strides multiples of 16 bytes")
+    return head, token
 
 
 def _bounds(cu_seqlens, start=None):
-    import torch
-    for t in (cu_seqlens, start):
-        if t is not None and (t.dtype != torch.int64 or t.dim() != 1 or not t.is_contiguous()):
-            raise TypeError("cu_seqlens and start must be contiguous int64 vectors")
     batch = cu_seqlens.numel() - 1
-    if batch < 1 or (start is not None and start.numel() != batch):
-        raise ValueError("cu_seqlens must hold batch + 1 offsets and start one position a sequence")
+    if cu_seqlens.dtype != torch.int64 or not cu_seqlens.is_contiguous():
+        raise TypeError("cu_seqlens must be a contiguous int64 vector")
+    if batch < 1:
+        raise ValueError("cu_seqlens must hold batch + 1 offsets")
+    if start is not None:
+        if start.dtype != torch.int64 or not start.is_contiguous():
+            raise TypeError("start must be a contiguous int64 vector")
+        if start.numel() != batch:
+            raise ValueError("start must hold one position a sequence")
     return batch
 
 
-def _call(device, stream, name, *args):
-    """Launch on `stream` (torch's current one of `device`) with `device` current."""
-    import torch
-    other = torch.cuda.current_device() != device.index
-    with torch.cuda.device(device) if other else contextlib.nullcontext():
-        handle = ris._stream(stream)
-        _check(getattr(lib(), name)(*args, handle), name)
+def _at(t):
+    return 0 if t is None else t.data_ptr()
+
+
+def _call(index, stream, name, *args):
+    """Launch on `stream` (torch's current one of GPU `index`) with that GPU current."""
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(index):
+            return _call(index, stream, name, *args)
+    if stream is None:
+        stream = torch.cuda.current_stream(index)
+    status = getattr(lib(), name)(*args, stream if isinstance(stream, int) else stream.cuda_stream)
+    if status != ris.OK:
+        raise ris.RisError(status, name)
 
 
 def rope_packed(src, out, cu_seqlens, desc, start=None, stream=None):
     """ris_rope_packed: src is a [heads, T, D] view (unit stride along D), out
     [heads, T, D] contiguous; token i of sequence b is rotated to position
     start[b] + i (start None: i)."""
-    device = _one_device(src, out, cu_seqlens, start)
+    index = _one_gpu(out, src, cu_seqlens, start)
     _need_dense(out)
     H, T, D = out.shape
-    if tuple(src.shape) != (H, T, D) or src.stride(2) != 1 or src.dtype != out.dtype:
+    head, token, one = src.stride()
+    if src.shape != out.shape or one != 1 or src.dtype != out.dtype:
         raise ValueError("src must be a [heads, T, D] view of out's dtype with unit stride along D")
     batch = _bounds(cu_seqlens, start)
-    _call(device, stream, "ris_rope_packed", _ptr(src), src.stride(0), src.stride(1), _ptr(out), _dtype_code(out),
-          H, T, D, _ptr(cu_seqlens), _ptr(start), batch, ctypes.byref(desc))
+    _call(index, stream, "ris_rope_packed", src.data_ptr(), head, token, out.data_ptr(), _dtype_code(out), H, T, D,
+          cu_seqlens.data_ptr(), _at(start), batch, desc)
     return out
 
 
@@ -132,73 +148,70 @@ def prompt_desc(Q, K, V, out, cu_seqlens, causal=1, scale=0.0):
     """Descriptor from views Q, out [Hq, T, D] and K, V [Hkv, T, D]."""
     Hq, T, D = Q.shape
     return PromptDesc(_dtype_code(Q), _dtype_code(out), Hq, K.shape[0], D, cu_seqlens.numel() - 1, T, causal, scale,
-                      *_strides(Q), *_strides(K), *_strides(V), *_strides(out))
+                      *_rows(Q, Q.shape), *_rows(K, K.shape), *_rows(V, V.shape), *_rows(out, out.shape))
 
 
 def prompt_attn(Q, K, V, cu_seqlens, out, desc, stream=None):
     """ris_prompt_attn: dense attention of packed prompts.  Q, out [Hq, T, D] and
     K, V [Hkv, T, D] are views of any head and token strides that are multiples of
     16 bytes (head columns of a token-major projection output, for instance)."""
-    device = _one_device(Q, K, V, cu_seqlens, out)
+    index = _one_gpu(out, Q, K, V, cu_seqlens)
     if not (Q.dtype == K.dtype == V.dtype):
         raise TypeError("Q, K, V must share a dtype")
     if _dtype_code(Q) != desc.dtype_in or _dtype_code(out) != desc.dtype_out:
         raise TypeError("Q and out dtypes must match the descriptor")
-    _need_rows((desc.Hq, desc.T, desc.D), Q, out)
-    _need_rows((desc.Hkv, desc.T, desc.D), K, V)
-    strides = (*_strides(Q), *_strides(K), *_strides(V), *_strides(out))
-    if strides != tuple(getattr(desc, f"{x}_{y}") for x in "qkvo" for y in ("head", "token")):
+    q, kv = (desc.Hq, desc.T, desc.D), (desc.Hkv, desc.T, desc.D)
+    if (_rows(Q, q) != (desc.q_head, desc.q_token) or _rows(K, kv) != (desc.k_head, desc.k_token)
+            or _rows(V, kv) != (desc.v_head, desc.v_token) or _rows(out, q) != (desc.o_head, desc.o_token)):
         raise ValueError("strides must match the descriptor")
     if _bounds(cu_seqlens) != desc.batch:
         raise ValueError("cu_seqlens must hold the descriptor's batch + 1 offsets")
-    _call(device, stream, "ris_prompt_attn", _ptr(Q), _ptr(K), _ptr(V), _ptr(cu_seqlens), _ptr(out), ctypes.byref(desc))
+    _call(index, stream, "ris_prompt_attn", Q.data_ptr(), K.data_ptr(), V.data_ptr(), cu_seqlens.data_ptr(),
+          out.data_ptr(), desc)
     return out
 
 
 def kv4_cache(batch, Hkv, max_len, D, device="cuda"):
     """Empty 4-bit cache: codes K4, V4 [batch, Hkv, max_len, D / 2] and scales S
     [batch, Hkv, max_len, 2, D / 32], uint8."""
-    import torch
     codes = [torch.zeros(batch, Hkv, max_len, D // 2, dtype=torch.uint8, device=device) for _ in range(2)]
     return codes[0], codes[1], torch.zeros(batch, Hkv, max_len, 2, D // KV4_BLOCK, dtype=torch.uint8, device=device)
 
 
 def _need_cache(K4, V4, S, batch, Hkv, D):
-    import torch
     if not (K4.dtype == V4.dtype == S.dtype == torch.uint8):
         raise TypeError("K4, V4 and S must be uint8")
     _need_dense(K4, V4, S)
     max_len = K4.shape[2] if K4.dim() == 4 else 0
-    if (tuple(K4.shape) != (batch, Hkv, max_len, D // 2) or V4.shape != K4.shape
-            or tuple(S.shape) != (batch, Hkv, max_len, 2, D // KV4_BLOCK)):
+    if (K4.shape != (batch, Hkv, max_len, D // 2) or V4.shape != K4.shape
+            or S.shape != (batch, Hkv, max_len, 2, D // KV4_BLOCK)):
         raise ValueError("K4 and V4 must be [batch, Hkv, max_len, D / 2] and S [batch, Hkv, max_len, 2, D / 32]")
     return max_len
 
 
 def _kv4(K, V, cu_seqlens, K4, V4, S, start):
-    device = _one_device(K, V, cu_seqlens, K4, V4, S, start)
+    index = _one_gpu(K4, K, V, cu_seqlens, V4, S, start)
     if K.dtype != V.dtype:
         raise TypeError("K and V must share a dtype")
-    Hkv, T, D = K.shape
-    _need_rows((Hkv, T, D), K, V)
+    Hkv, T, D = shape = tuple(K.shape)
     batch = _bounds(cu_seqlens, start)
     max_len = _need_cache(K4, V4, S, batch, Hkv, D)
-    return device, Kv4Desc(_dtype_code(K), Hkv, D, batch, T, max_len, *_strides(K), *_strides(V))
+    return index, Kv4Desc(_dtype_code(K), Hkv, D, batch, T, max_len, *_rows(K, shape), *_rows(V, shape))
 
 
 def kv4_store(K, V, cu_seqlens, K4, V4, S, start=None, stream=None):
     """ris_kv4_store: rows K, V [Hkv, T, D] (views as in ``prompt_attn``) quantised
     into the cache, token i of sequence b at position start[b] + i (start None: i)."""
-    device, d = _kv4(K, V, cu_seqlens, K4, V4, S, start)
-    _call(device, stream, "ris_kv4_store", _ptr(K), _ptr(V), _ptr(cu_seqlens), _ptr(start), _ptr(K4), _ptr(V4),
-          _ptr(S), ctypes.byref(d))
+    index, desc = _kv4(K, V, cu_seqlens, K4, V4, S, start)
+    _call(index, stream, "ris_kv4_store", K.data_ptr(), V.data_ptr(), cu_seqlens.data_ptr(), _at(start), K4.data_ptr(),
+          V4.data_ptr(), S.data_ptr(), desc)
 
 
 def kv4_load(K4, V4, S, cu_seqlens, K, V, start=None, stream=None):
     """ris_kv4_load: the cache's values at those positions into K, V [Hkv, T, D]."""
-    device, d = _kv4(K, V, cu_seqlens, K4, V4, S, start)
-    _call(device, stream, "ris_kv4_load", _ptr(K4), _ptr(V4), _ptr(S), _ptr(cu_seqlens), _ptr(start), _ptr(K),
-          _ptr(V), ctypes.byref(d))
+    index, desc = _kv4(K, V, cu_seqlens, K4, V4, S, start)
+    _call(index, stream, "ris_kv4_load", K4.data_ptr(), V4.data_ptr(), S.data_ptr(), cu_seqlens.data_ptr(), _at(start),
+          K.data_ptr(), V.data_ptr(), desc)
 
 
 def kv4_decode_desc(Q, K4, out, anchor_stride=0, window=0, sink=0, scale=0.0):
@@ -219,8 +232,7 @@ def kv4_decode_attn(Q, K4, V4, S, pos, anchor_ptr, anchor_idx, out, workspace, d
     """ris_kv4_decode_attn; workspace is a device uint8 tensor of at least
     kv4_decode_workspace_bytes(desc) bytes.  anchor_ptr and anchor_idx may be None
     where the descriptor's anchor_stride is 0."""
-    import torch
-    device = _one_device(Q, K4, V4, S, pos, anchor_ptr, anchor_idx, out, workspace)
+    index = _one_gpu(out, Q, K4, V4, S, pos, anchor_ptr, anchor_idx, workspace)
     _need_dense(Q, pos, anchor_ptr, anchor_idx, out, workspace)
     if pos.dtype != torch.int64 or pos.numel() != desc.batch:
         raise ValueError("pos must be int64 and hold B entries")
@@ -233,13 +245,13 @@ def kv4_decode_attn(Q, K4, V4, S, pos, anchor_ptr, anchor_idx, out, workspace, d
             raise ValueError("anchor_ptr must hold B * (Hkv + 1) entries and anchor_idx B * anchor_stride")
     if _dtype_code(Q) != desc.dtype_in or _dtype_code(out) != desc.dtype_out:
         raise TypeError("Q and out dtypes must match the descriptor")
-    if tuple(Q.shape) != (desc.batch, desc.Hq, desc.D) or out.shape != Q.shape:
+    if Q.shape != (desc.batch, desc.Hq, desc.D) or out.shape != Q.shape:
         raise ValueError("Q and out must be [B, Hq, D] as in the descriptor")
     if _need_cache(K4, V4, S, desc.batch, desc.Hkv, desc.D) != desc.max_len:
         raise ValueError("the cache's max_len must match the descriptor")
     nbytes = workspace.numel() * workspace.element_size()
-    _call(device, stream, "ris_kv4_decode_attn", _ptr(Q), _ptr(K4), _ptr(V4), _ptr(S), _ptr(pos), _ptr(anchor_ptr),
-          _ptr(anchor_idx), _ptr(out), _ptr(workspace), nbytes, ctypes.byref(desc))
+    _call(index, stream, "ris_kv4_decode_attn", Q.data_ptr(), K4.data_ptr(), V4.data_ptr(), S.data_ptr(), pos.data_ptr(),
+          _at(anchor_ptr), _at(anchor_idx), out.data_ptr(), workspace.data_ptr(), nbytes, desc)
     return out
 
 
@@ -261,22 +273,21 @@ def logprobs(logits, targets, logprob, entropy, top_ids, top_logprob, workspace,
     logprob float32 [rows, n_targets], entropy float32 [rows] or None, top_ids
     int64 and top_logprob float32 [rows, top_k]; what the descriptor counts 0 of
     may be None.  workspace: at least logprobs_workspace_bytes(desc) bytes."""
-    import torch
-    device = _one_device(logits, targets, logprob, entropy, top_ids, top_logprob, workspace)
-    if tuple(logits.shape) != (desc.rows, desc.vocab) or logits.stride(1) != 1 and desc.vocab > 1:
+    index = _one_gpu(logits, targets, logprob, entropy, top_ids, top_logprob, workspace)
+    rows, n, k = desc.rows, desc.n_targets, desc.top_k
+    if logits.shape != (rows, desc.vocab) or logits.stride(1) != 1 and desc.vocab > 1:
         raise ValueError("logits must be [rows, vocab] as in the descriptor, unit stride along vocab")
-    if desc.rows > 1 and logits.stride(0) != desc.row_stride or _dtype_code(logits) != desc.dtype:
+    if rows > 1 and logits.stride(0) != desc.row_stride or _dtype_code(logits) != desc.dtype:
         raise ValueError("the logits' row stride and dtype must match the descriptor")
     _need_dense(targets, logprob, entropy, top_ids, top_logprob, workspace)
-    wanted = ((targets, (desc.rows, desc.n_targets), torch.int64), (logprob, (desc.rows, desc.n_targets), torch.float32),
-              (top_ids, (desc.rows, desc.top_k), torch.int64), (top_logprob, (desc.rows, desc.top_k), torch.float32))
-    for t, shape, dtype in wanted:
-        if shape[1] and t is None or t is not None and (tuple(t.shape) != shape or t.dtype != dtype):
+    for t, count, dtype in ((targets, n, torch.int64), (logprob, n, torch.float32), (top_ids, k, torch.int64),
+                            (top_logprob, k, torch.float32)):
+        if t is None and count or t is not None and (t.shape != (rows, count) or t.dtype != dtype):
             raise ValueError("targets and logprob must be [rows, n_targets], top_ids and top_logprob [rows, top_k] "
                              "(ids int64, the others float32)")
-    if entropy is not None and (tuple(entropy.shape) != (desc.rows,) or entropy.dtype != torch.float32):
+    if entropy is not None and (entropy.shape != (rows,) or entropy.dtype != torch.float32):
         raise ValueError("entropy must be float32 [rows]")
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _call(device, stream, "ris_logprobs", _ptr(logits), _ptr(targets), _ptr(logprob), _ptr(entropy), _ptr(top_ids),
-          _ptr(top_logprob), _ptr(workspace), nbytes, ctypes.byref(desc))
+    _call(index, stream, "ris_logprobs", logits.data_ptr(), _at(targets), _at(logprob), _at(entropy), _at(top_ids),
+          _at(top_logprob), _at(workspace), nbytes, desc)
     return logprob

@@ -203,11 +203,11 @@ def test_binding_refuses_before_any_call(serve):
     with pytest.raises(ValueError):
         serve._bounds(torch.tensor([0]))
     with pytest.raises(ValueError, match="16 bytes"):
-        serve._need_rows((2, 4, 64), torch.zeros(2, 4, 65, dtype=torch.bfloat16)[..., 1:])
+        serve._rows(torch.zeros(2, 4, 65, dtype=torch.bfloat16)[..., 1:], (2, 4, 64))
     with pytest.raises(ValueError, match="16 bytes"):
-        serve._need_rows((2, 4, 32), torch.zeros(2, 4, 64)[..., ::2])
+        serve._rows(torch.zeros(2, 4, 64)[..., ::2], (2, 4, 32))
     with pytest.raises(ValueError, match="view"):
-        serve._need_rows((2, 5, 64), x)
+        serve._rows(x, (2, 5, 64))
     K4, V4, S = serve.kv4_cache(1, 2, 8, 64, "cpu")
     assert serve._need_cache(K4, V4, S, 1, 2, 64) == 8
     for bad in ((K4, V4[:, :, :4], S), (K4, V4, S[..., :1]), (K4[:, :1], V4[:, :1], S)):
