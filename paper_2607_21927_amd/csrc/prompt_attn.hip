@@ -18,6 +18,8 @@
 // a workgroup whose output is not finite goes over its keys once more, with
 // such elements of V taken out of the tiles that the mask cuts and added where
 // they are attended to.
+#include <type_traits>
+
 #include "packed.h"
 #include "ris_internal.h"
 
@@ -41,18 +43,42 @@ __device__ __forceinline__ int swizzle(int r) {
 typedef const __attribute__((address_space(1))) void* gptr_t;
 typedef __attribute__((address_space(3))) void* lptr_t;
 
-// Keys [j0, j0 + 64) of x (rows of the sequence, `tok` elements apart) into LDS;
-// keys from n on repeat the last one.
+// A lane's part in a tile: 16-byte pieces, piece i at place 256 i + thread of the tile
+// in LDS.  Their rows are kStep apart, a multiple of the swizzle's period, so all
+// have one chunk and one offset in the row.
 template <int D>
-__device__ __forceinline__ void load_tile(const uint16_t* x, int64_t tok, int j0, int n, uint16_t* lds) {
-    constexpr int C = D / 8;                            // chunks of a row
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+struct Piece {
+    static constexpr int kCount = kKeys * (D / 8) / (64 * kWaves);
+    static constexpr int kStep = kKeys / kCount;
+    static_assert(kStep % 16 == 0, "the swizzle repeats every 16 rows");
+    int row;            // of piece 0
+    uint32_t chunk;     // bytes into the row
+    __device__ __forceinline__ Piece() : row((int)threadIdx.x / (D / 8)) {
+        chunk = 16u * ((threadIdx.x % (D / 8)) ^ swizzle<D>(row));
+    }
+};
+
+// Keys [j0, j0 + 64) of x (rows of the sequence, `tok` elements apart) into LDS;
+// keys from n on repeat the last one.  (Offsets within a tile fit 32 bits: the host
+// refuses rows farther apart.)
+template <int D>
+__device__ __forceinline__ void load_tile(const Piece<D>& pc, const uint16_t* x, int64_t tok, int j0, int n, uint16_t* lds) {
+    uint16_t* to = lds + (threadIdx.x & ~63u) * 8;      // the wave's places
+    const char* from = reinterpret_cast<const char*>(x + j0 * tok);
+    const uint32_t step = 2u * (uint32_t)tok;
+    if (j0 + kKeys <= n) {
+        const uint32_t off = pc.row * step + pc.chunk;
 #pragma unroll
-    for (int i = 0; i < kKeys * C / (64 * kWaves); ++i) {
-        const int at = (i * kWaves + wave) * 64, e = at + lane;
-        const int r = e / C, c = (e % C) ^ swizzle<D>(r);
-        const int j = j0 + r < n ? j0 + r : n - 1;
-        __builtin_amdgcn_global_load_lds((gptr_t)(x + j * tok + 8 * c), (lptr_t)(lds + 8 * at), 16, 0, 0);
+        for (int i = 0; i < Piece<D>::kCount; ++i)
+            __builtin_amdgcn_global_load_lds((gptr_t)(from + (uint64_t)(i * Piece<D>::kStep) * step + off),
+                                             (lptr_t)(to + 64 * kWaves * 8 * i), 16, 0, 0);
+    } else {
+#pragma unroll
+        for (int i = 0; i < Piece<D>::kCount; ++i) {
+            const int r = pc.row + i * Piece<D>::kStep < n - j0 ? pc.row + i * Piece<D>::kStep : n - 1 - j0;
+            __builtin_amdgcn_global_load_lds((gptr_t)(from + (uint32_t)(r * step + pc.chunk)), (lptr_t)(to + 64 * kWaves * 8 * i),
+                                             16, 0, 0);
+        }
     }
 }
 
@@ -65,8 +91,9 @@ template <int D>
 __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_bf16(PromptParams p) {
     constexpr int SL = D / 16;      // contraction steps of the score product
     constexpr int DB = D / 32;      // 32-dim blocks of the output
-    __shared__ __align__(16) uint16_t kt[2][kKeys * D];
-    __shared__ __align__(16) uint16_t vt[2][kKeys * D];
+    // two tiles of K and of V; arrays of their own, so that a load into one is not
+    // taken for a write to another
+    __shared__ __align__(16) uint16_t k0[kKeys * D], k1[kKeys * D], v0[kKeys * D], v1[kKeys * D];
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int lq = lane & 31, lh = lane >> 5;
@@ -81,6 +108,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_bf16(PromptParams p) 
 
     const uint16_t* K = static_cast<const uint16_t*>(p.K) + g * p.k_head + t.first * p.k_token;
     const uint16_t* V = static_cast<const uint16_t*>(p.V) + g * p.v_head + t.first * p.v_token;
+
+    const Piece<D> pc;
 
     // Q^T as the B operand: lane l holds query l % 32, dims 16 s + 8 (l / 32) ..
     u32x4_t qf[SL];
@@ -98,112 +127,124 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_bf16(PromptParams p) 
     const int tiles = (kend + kKeys - 1) / kKeys;
 
     f32x16_t o[DB];
-    float m, l;
-    for (int safe = 0;; safe = 1) {
+    float m = -INFINITY, mc = 0.f, l = 0.f;      // reference maximum in scores; times c, 0 while there is none; sum
+
+    // One tile of keys: kCut where the mask cuts it, kSafe where V may hold
+    // infinities or NaN under the mask.
+    const auto compute = [&](auto cut, auto safe, const uint16_t* kl, const uint16_t* vl, int j0) __attribute__((always_inline)) {
+        constexpr bool kCut = decltype(cut)::value, kSafe = decltype(safe)::value;
+        // S^T: lane l holds query l % 32 at keys 32 b + 8 (i / 4) + 4 (l / 32) + i % 4.
+        f32x16_t st[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) st[b][i] = 0.f;
+#pragma unroll
+            for (int s = 0; s < SL; ++s) {
+                const u32x4_t a = *reinterpret_cast<const u32x4_t*>(kl + (32 * b + lq) * D + 8 * ((2 * s + lh) ^ swizzle<D>(lq)));
+                st[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(qf[s]), st[b], 0, 0, 0);
+            }
+        }
+        if constexpr (kCut) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (j0 + 32 * b + 8 * (i / 4) + 4 * lh + i % 4 > last) st[b][i] = -INFINITY;
+        }
+        float mx = st[0][0];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, st[b][i]);
+        mx = pair_max32(mx);
+        if (__any(mx > m + p.slack)) {
+            const bool none = m == -INFINITY;                      // nothing summed yet: o and l are 0
+            m = fmaxf(m, mx);
+            const float nc = m == -INFINITY ? 0.f : m * p.c;
+            const float al = none ? 0.f : __builtin_amdgcn_exp2f(mc - nc);
+            mc = nc;
+            l *= al;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] *= al;
+        }
+        u32x4_t pf[4];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                const float x = __builtin_amdgcn_exp2f(fmaf(st[b][i], p.c, -mc));
+                const float y = __builtin_amdgcn_exp2f(fmaf(st[b][i + 1], p.c, -mc));
+                l += x + y;
+                pf[2 * b + i / 8][i % 8 / 2] = pack_bf16x2(x, y);
+            }
+        // O^T += V^T P^T over 16 keys at a time: slot e of lane half lh holds
+        // key 16 u + 4 lh + e (e < 4) or 16 u + 8 + 4 lh + e - 4.
+        const int r0 = 4 * lh + ((lane & 15) >> 2), cq = 2 * (lane >> 4 & 1) + ((lane & 3) >> 1);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int d = 0; d < DB; ++d) {
+                const int c = 4 * d + cq;
+                const uint2 a = lds_read_tr16(vl + (16 * u + r0) * D + 8 * (c ^ swizzle<D>(r0)) + 4 * (lane & 1));
+                const uint2 b = lds_read_tr16(vl + (16 * u + r0 + 8) * D + 8 * (c ^ swizzle<D>(r0 + 8)) + 4 * (lane & 1));
+                u32x4_t v = {a.x, a.y, b.x, b.y};
+                if constexpr (kSafe) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = finite_only(v[i]);
+                }
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v), as_bf16x8(pf[u]), o[d], 0, 0, 0);
+            }
+        if constexpr (kSafe) {
+            for (int r = 0; r < kKeys; ++r)
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int dim = 32 * d + 8 * (i / 4) + 4 * lh + i % 4;
+                        const uint16_t v = vl[r * D + 8 * ((dim >> 3) ^ swizzle<D>(r)) + (dim & 7)];
+                        if (odd_half(v) && j0 + r <= last) o[d][i] += bf16_to_f32(v);
+                    }
+        }
+    };
+    // All keys: tile `it` is computed from one pair of arrays while tile `it` + 1
+    // is on its way into the other.
+    const auto pass = [&](auto safe) __attribute__((always_inline)) {
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-        m = -INFINITY;          // reference maximum, in scores; mc: times c, 0 while there is none
-        float mc = 0.f;
-        l = 0.f;
-        load_tile<D>(K, p.k_token, 0, n, kt[0]);
-        load_tile<D>(V, p.v_token, 0, n, vt[0]);
-        for (int it = 0; it < tiles; ++it) {
+        load_tile<D>(pc, K, p.k_token, 0, n, k0);
+        load_tile<D>(pc, V, p.v_token, 0, n, v0);
+        const auto step = [&](int it, const uint16_t* kl, const uint16_t* vl, uint16_t* kn, uint16_t* vn) __attribute__((always_inline)) {
             const int j0 = it * kKeys;
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
             if (it + 1 < tiles) {
-                load_tile<D>(K, p.k_token, j0 + kKeys, n, kt[(it + 1) & 1]);
-                load_tile<D>(V, p.v_token, j0 + kKeys, n, vt[(it + 1) & 1]);
+                load_tile<D>(pc, K, p.k_token, j0 + kKeys, n, kn);
+                load_tile<D>(pc, V, p.v_token, j0 + kKeys, n, vn);
             }
-            if (q0 >= n || j0 > wlast) continue;
-            const uint16_t* kl = kt[it & 1];
-            const uint16_t* vl = vt[it & 1];
-
-            // S^T: lane l holds query l % 32 at keys 32 b + 8 (i / 4) + 4 (l / 32) + i % 4.
-            f32x16_t st[2];
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) st[b][i] = 0.f;
-#pragma unroll
-                for (int s = 0; s < SL; ++s) {
-                    const int r = 32 * b + lq;
-                    const u32x4_t a = *reinterpret_cast<const u32x4_t*>(kl + r * D + 8 * ((2 * s + lh) ^ swizzle<D>(r)));
-                    st[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(qf[s]), st[b], 0, 0, 0);
-                }
-            }
-            const bool cut = j0 + kKeys - 1 > wfull;
-            if (cut) {
-#pragma unroll
-                for (int b = 0; b < 2; ++b)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (j0 + 32 * b + 8 * (i / 4) + 4 * lh + i % 4 > last) st[b][i] = -INFINITY;
-            }
-            float mx = st[0][0];
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) mx = fmaxf(mx, st[b][i]);
-            mx = pair_max32(mx);
-            if (__any(mx > m + p.slack)) {
-                const bool none = m == -INFINITY;                      // nothing summed yet: o and l are 0
-                m = fmaxf(m, mx);
-                const float nc = m == -INFINITY ? 0.f : m * p.c;
-                const float al = none ? 0.f : __builtin_amdgcn_exp2f(mc - nc);
-                mc = nc;
-                l *= al;
-#pragma unroll
-                for (int d = 0; d < DB; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[d][i] *= al;
-            }
-            u32x4_t pf[4];
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; i += 2) {
-                    const float x = __builtin_amdgcn_exp2f(fmaf(st[b][i], p.c, -mc));
-                    const float y = __builtin_amdgcn_exp2f(fmaf(st[b][i + 1], p.c, -mc));
-                    l += x + y;
-                    pf[2 * b + i / 8][i % 8 / 2] = pack_bf16x2(x, y);
-                }
-            // O^T += V^T P^T over 16 keys at a time: slot e of lane half lh holds
-            // key 16 u + 4 lh + e (e < 4) or 16 u + 8 + 4 lh + e - 4.
-            const int r0 = 4 * lh + ((lane & 15) >> 2), cq = 2 * (lane >> 4 & 1) + ((lane & 3) >> 1);
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int d = 0; d < DB; ++d) {
-                    const int ra = 16 * u + r0, rb = ra + 8, c = 4 * d + cq;
-                    const uint2 a = lds_read_tr16(vl + ra * D + 8 * (c ^ swizzle<D>(ra)) + 4 * (lane & 1));
-                    const uint2 b = lds_read_tr16(vl + rb * D + 8 * (c ^ swizzle<D>(rb)) + 4 * (lane & 1));
-                    u32x4_t v = {a.x, a.y, b.x, b.y};
-                    if (safe && cut)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) v[i] = finite_only(v[i]);
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v), as_bf16x8(pf[u]), o[d], 0, 0, 0);
-                }
-            if (safe && cut)
-                for (int r = 0; r < kKeys; ++r)
-#pragma unroll
-                    for (int d = 0; d < DB; ++d)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int dim = 32 * d + 8 * (i / 4) + 4 * lh + i % 4;
-                            const uint16_t v = vl[r * D + 8 * ((dim >> 3) ^ swizzle<D>(r)) + (dim & 7)];
-                            if (odd_half(v) && j0 + r <= last) o[d][i] += bf16_to_f32(v);
-                        }
+            if (q0 >= n || j0 > wlast) return;
+            if (j0 + kKeys - 1 > wfull) compute(std::true_type{}, safe, kl, vl, j0);
+            else compute(std::false_type{}, std::false_type{}, kl, vl, j0);
+        };
+        for (int it = 0; it < tiles; it += 2) {
+            step(it, k0, v0, k1, v1);
+            if (it + 1 < tiles) step(it + 1, k1, v1, k0, v0);
         }
-        float odd = 0.f;
+    };
+    pass(std::false_type{});
+    float odd = 0.f;
 #pragma unroll
-        for (int d = 0; d < DB; ++d)
+    for (int d = 0; d < DB; ++d)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) odd = fmaf(o[d][i], 0.f, odd);       // NaN if any is not finite
-        // also the barrier before the first tile's place is written again
-        if (!__syncthreads_or(odd != odd && row < n && !safe)) break;
+        for (int i = 0; i < 16; ++i) odd = fmaf(o[d][i], 0.f, odd);       // NaN if any is not finite
+    if (__syncthreads_or(odd != odd && row < n)) {
+        m = -INFINITY;
+        mc = l = 0.f;
+        pass(std::true_type{});
     }
     l = pair_sum32(l);
     if (row >= n) return;

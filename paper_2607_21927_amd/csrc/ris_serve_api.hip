@@ -22,6 +22,10 @@ bool vector_rows(const void* p, int64_t head, int64_t token, int32_t dtype) {
 // Token offsets fit 32 bits (ris_serve.h's packed sequences).
 constexpr int64_t kMaxTokens = 0x7FFFFFFFll;
 
+// Elements between the rows of K or V whose byte offsets within a tile of 64 keys
+// fit 32 bits, float32 rows too.
+constexpr int64_t kMaxKeyStride = (1ll << 32) / (64 * 4) - 1024;
+
 // Work-items of a launch, which a dispatch counts in 32 bits.
 bool fits_dispatch(int64_t blocks, int64_t threads) { return blocks <= 0xFFFFFFFFll / threads; }
 
@@ -151,6 +155,7 @@ int ris_prompt_attn(const void* Q, const void* K, const void* V, const int64_t* 
     if (!vector_rows(Q, d.q_head, d.q_token, d.dtype_in) || !vector_rows(K, d.k_head, d.k_token, d.dtype_in) ||
         !vector_rows(V, d.v_head, d.v_token, d.dtype_in) || !vector_rows(out, d.o_head, d.o_token, d.dtype_out))
         return RIS_E_ARG;
+    if (d.k_token > kMaxKeyStride || d.v_token > kMaxKeyStride) return RIS_E_UNSUPPORTED;
     ris::PromptParams p;
     p.Q = Q; p.K = K; p.V = V; p.cu = cu_seqlens; p.out = out;
     p.T = d.T;
