@@ -9,9 +9,10 @@ namespace ris {
 
 __device__ __forceinline__ int clip_offset(int64_t v, int64_t T) { return (int)(v < 0 ? 0 : (v > T ? T : v)); }
 
-// Tile `idx` of the tiles of `rows` rows that the sequences are cut into, the
-// last tile of a sequence first (under a causal mask it costs most).  By the
-// whole wave, idx uniform; false past the last tile.
+// Tile `idx` of the tiles of `rows` rows that the sequences are cut into, those
+// far into their sequences first: under a causal mask they cost most, and what is
+// long goes first so that the end is short.  (More than 64 sequences: one sequence
+// after another.)  By the whole wave, idx uniform; false past the last tile.
 struct RowTile {
     int first;      // the sequence's first token
     int len;        // its tokens
@@ -31,12 +32,25 @@ __device__ __forceinline__ bool find_tile(const int64_t* cu, int batch, int64_t 
         const uint32_t upto = wave_inclusive_scan(nt);
         const uint32_t total = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
         if (idx < total) {
-            const int at = (int)__builtin_ctzll(__ballot(upto > idx));
-            const uint32_t n = (uint32_t)__builtin_amdgcn_readlane((int)nt, at);
-            const uint32_t before = (uint32_t)__builtin_amdgcn_readlane((int)upto, at) - n;
+            int at;
+            if (batch > 1 && batch <= 64) {
+                // the last level of which more than idx tiles are that far or farther
+                uint32_t level = 0, beyond = 0;                  // beyond: tiles above the level
+                for (uint32_t bit = 1u << (31 - __builtin_clz(total)); bit; bit >>= 1) {
+                    const uint32_t l = level | bit;
+                    if (wave_sum_u32(nt > l ? nt - l : 0u) > idx) level = l;
+                }
+                beyond = wave_sum_u32(nt > level + 1 ? nt - level - 1 : 0u);
+                uint64_t on = __ballot(nt > level);
+                for (uint32_t i = idx - beyond; i; --i) on &= on - 1;
+                at = (int)__builtin_ctzll(on);
+                t.tile = (int)level;
+            } else {
+                at = (int)__builtin_ctzll(__ballot(upto > idx));
+                t.tile = __builtin_amdgcn_readlane((int)upto, at) - 1 - (int)idx;
+            }
             t.first = __builtin_amdgcn_readlane(lo, at);
             t.len = __builtin_amdgcn_readlane(len, at);
-            t.tile = (int)(n - 1 - (idx - before));
             return true;
         }
         idx -= total;

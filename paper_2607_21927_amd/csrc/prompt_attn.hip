@@ -13,11 +13,19 @@
 // barrier a tile.
 //
 // The reference maximum moves only when a score exceeds it by 2^8 in weight, so
-// rescales are rare.  Tiles that no row of a wave cuts are computed without a
-// mask.  A masked weight is 0, and 0 times an infinity or NaN of V would be NaN:
-// a workgroup whose output is not finite goes over its keys once more, with
+// rescales are rare.  A masked weight is 0, and 0 times an infinity or NaN of V would
+// be NaN: a workgroup whose output is not finite goes over its keys once more, with
 // such elements of V taken out of the tiles that the mask cuts and added where
 // they are attended to.
+//
+// Bound by how well the matrix unit (54% busy) and the vector unit (~45%) share the
+// time of two waves a SIMD at 1.9 GHz; LDS is at 27%, without bank conflicts.  At D =
+// 128 the next tile's scores stand beside this one's exponentials in one block, the
+// products and reads spread through it (1071 -> 1106 TFLOP/s for 12/2 heads at 32k
+// tokens); at D = 64, where exponentials take longer than products, three waves a
+// SIMD without that gain more (975 against 937).  Not kept: row sums on v_dot2 (the
+// same), the next maximum carried along (the same), raised priority in the PV product
+// (-6%), waits placed by hand around loads in assembly (the same).
 #include <type_traits>
 
 #include "packed.h"
@@ -29,6 +37,7 @@ namespace {
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr int kRows = 128;        // query rows of a workgroup
+constexpr int kNarrowRows = 32;   // of the narrow form's
 constexpr int kKeys = 64;         // keys of a tile
 constexpr int kWaves = 4;
 
@@ -53,7 +62,7 @@ struct Piece {
     static_assert(kStep % 16 == 0, "the swizzle repeats every 16 rows");
     int row;            // of piece 0
     uint32_t chunk;     // bytes into the row
-    __device__ __forceinline__ Piece() : row((int)threadIdx.x / (D / 8)) {
+    __device__ __forceinline__ Piece() : row((int)(threadIdx.x & (64 * kWaves - 1)) / (D / 8)) {
         chunk = 16u * ((threadIdx.x % (D / 8)) ^ swizzle<D>(row));
     }
 };
@@ -63,7 +72,7 @@ struct Piece {
 // refuses rows farther apart.)
 template <int D>
 __device__ __forceinline__ void load_tile(const Piece<D>& pc, const uint16_t* x, int64_t tok, int j0, int n, uint16_t* lds) {
-    uint16_t* to = lds + (threadIdx.x & ~63u) * 8;      // the wave's places
+    uint16_t* to = lds + (threadIdx.x & (64 * kWaves - 64)) * 8;      // the wave's places
     const char* from = reinterpret_cast<const char*>(x + j0 * tok);
     const uint32_t step = 2u * (uint32_t)tok;
     if (j0 + kKeys <= n) {
@@ -82,21 +91,35 @@ __device__ __forceinline__ void load_tile(const Piece<D>& pc, const uint16_t* x,
     }
 }
 
+// Four neighbouring elements of out.
+__device__ __forceinline__ void store4(const PromptParams& p, int64_t at, float a, float b, float c, float d) {
+    if (p.out_bf16)
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + at) = make_uint2(pack_bf16x2(a, b), pack_bf16x2(c, d));
+    else
+        *reinterpret_cast<f32x4_t*>(static_cast<float*>(p.out) + at) = f32x4_t{a, b, c, d};
+}
+
 __device__ __forceinline__ bool odd_half(uint32_t u) { return (u & 0x7F80u) == 0x7F80u; }   // infinity or NaN
 __device__ __forceinline__ uint32_t finite_only(uint32_t u) {
     return (odd_half(u) ? 0u : u & 0xFFFFu) | (odd_half(u >> 16) ? 0u : u & 0xFFFF0000u);
 }
 
-template <int D>
-__global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_bf16(PromptParams p) {
+template <int D, int S>
+__global__ __launch_bounds__(64 * kWaves * S, D == 64 ? 3 : 2) void k_prompt_bf16(PromptParams p) {
     constexpr int SL = D / 16;      // contraction steps of the score product
     constexpr int DB = D / 32;      // 32-dim blocks of the output
+    constexpr bool kPipe = D == 128;
     // two tiles of K and of V; arrays of their own, so that a load into one is not
     // taken for a write to another
-    __shared__ __align__(16) uint16_t k0[kKeys * D], k1[kKeys * D], v0[kKeys * D], v1[kKeys * D];
+    __shared__ __align__(16) uint16_t k0s[S * kKeys * D], k1s[S * kKeys * D], v0s[S * kKeys * D], v1s[S * kKeys * D];
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6 & (kWaves - 1);               // wave: row block
+    const int group = S == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * kWaves));   // of keys
     const int lq = lane & 31, lh = lane >> 5;
+    uint16_t* const k0 = k0s + group * kKeys * D;
+    uint16_t* const k1 = k1s + group * kKeys * D;
+    uint16_t* const v0 = v0s + group * kKeys * D;
+    uint16_t* const v1 = v1s + group * kKeys * D;
     // The heads of a group take the same tile one after another on one XCD, so
     // that its L2 serves their K and V.
     const uint32_t xcd = blockIdx.x & 7u, slot = blockIdx.x >> 3;
@@ -129,12 +152,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_bf16(PromptParams p) 
     f32x16_t o[DB];
     float m = -INFINITY, mc = 0.f, l = 0.f;      // reference maximum in scores; times c, 0 while there is none; sum
 
-    // One tile of keys: kCut where the mask cuts it, kSafe where V may hold
-    // infinities or NaN under the mask.
-    const auto compute = [&](auto cut, auto safe, const uint16_t* kl, const uint16_t* vl, int j0) __attribute__((always_inline)) {
-        constexpr bool kCut = decltype(cut)::value, kSafe = decltype(safe)::value;
-        // S^T: lane l holds query l % 32 at keys 32 b + 8 (i / 4) + 4 (l / 32) + i % 4.
-        f32x16_t st[2];
+    // S^T of a tile: lane l holds query l % 32 at keys 32 b + 8 (i / 4) + 4 (l / 32) + i % 4.
+    const auto scores = [&](const uint16_t* kl, f32x16_t (&st)[2]) __attribute__((always_inline)) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
 #pragma unroll
@@ -145,7 +164,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_bf16(PromptParams p) 
                 st[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(qf[s]), st[b], 0, 0, 0);
             }
         }
-        if constexpr (kCut) {
+    };
+    // The tile at j0 from its scores `st` and values `vl`, with the next tile's scores
+    // `nx` from `kn` beside it (kMore).  kSafe: the mask cuts the tile, and V may hold
+    // infinities or NaN under it.
+    const auto compute = [&](auto more, auto safe, f32x16_t (&st)[2], f32x16_t (&nx)[2], const uint16_t* kn, const uint16_t* vl,
+                             int j0) __attribute__((always_inline)) {
+        constexpr bool kMore = decltype(more)::value, kSafe = decltype(safe)::value;
+        const bool cut = j0 + kKeys - 1 > wfull;
+        if (cut) {
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -170,6 +197,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_bf16(PromptParams p) 
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[d][i] *= al;
         }
+        if constexpr (kMore) scores(kn, nx);
         u32x4_t pf[4];
 #pragma unroll
         for (int b = 0; b < 2; ++b)
@@ -193,12 +221,27 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_bf16(PromptParams p) 
                 u32x4_t v = {a.x, a.y, b.x, b.y};
                 if constexpr (kSafe) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] = finite_only(v[i]);
+                    for (int i = 0; i < 4; ++i) v[i] = cut ? finite_only(v[i]) : v[i];
                 }
                 o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v), as_bf16x8(pf[u]), o[d], 0, 0, 0);
             }
+        if constexpr (kMore) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+            for (int i = 0; i < 2 * SL; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < 4 * DB; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+            }
+        }
         if constexpr (kSafe) {
-            for (int r = 0; r < kKeys; ++r)
+            for (int r = 0; cut && r < kKeys; ++r)
 #pragma unroll
                 for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -209,30 +252,75 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_bf16(PromptParams p) 
                     }
         }
     };
-    // All keys: tile `it` is computed from one pair of arrays while tile `it` + 1
-    // is on its way into the other.
+    // All of the group's keys, its i-th tile being tile S i + group.  While one is
+    // computed, the next is on its way; where kPipe, K of the next is there already for
+    // its scores, and K of the one after that and V of the next are on their way.
+    const int rounds = (tiles + S - 1) / S;
+    const int have = (tiles - group + S - 1) / S;                   // the group's tiles
+    const int mine = q0 < n ? (wlast / kKeys + S - group) / S : 0;  // those that the wave's rows attend to
     const auto pass = [&](auto safe) __attribute__((always_inline)) {
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-        load_tile<D>(pc, K, p.k_token, 0, n, k0);
-        load_tile<D>(pc, V, p.v_token, 0, n, v0);
-        const auto step = [&](int it, const uint16_t* kl, const uint16_t* vl, uint16_t* kn, uint16_t* vn) __attribute__((always_inline)) {
-            const int j0 = it * kKeys;
+        if (have > 0) {
+            load_tile<D>(pc, K, p.k_token, group * kKeys, n, k0);
+            load_tile<D>(pc, V, p.v_token, group * kKeys, n, v0);
+        }
+        if (kPipe && have > 1) load_tile<D>(pc, K, p.k_token, (S + group) * kKeys, n, k1);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        f32x16_t sa[2], sb[2];
+        if (kPipe && mine > 0) scores(k0, sa);
+        const auto step = [&](int it, f32x16_t (&st)[2], f32x16_t (&nx)[2], uint16_t* kl, const uint16_t* vl, uint16_t* kn,
+                              uint16_t* vn) __attribute__((always_inline)) {
+            const int j0 = (S * it + group) * kKeys;
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
-            if (it + 1 < tiles) {
-                load_tile<D>(pc, K, p.k_token, j0 + kKeys, n, kn);
-                load_tile<D>(pc, V, p.v_token, j0 + kKeys, n, vn);
+            if (it + 1 < have) load_tile<D>(pc, V, p.v_token, j0 + S * kKeys, n, vn);
+            if constexpr (!kPipe) {
+                if (it + 1 < have) load_tile<D>(pc, K, p.k_token, j0 + S * kKeys, n, kn);
+                if (it < mine) {
+                    scores(kl, st);
+                    compute(std::false_type{}, safe, st, nx, kn, vl, j0);
+                }
+                return;
             }
-            if (q0 >= n || j0 > wlast) return;
-            if (j0 + kKeys - 1 > wfull) compute(std::true_type{}, safe, kl, vl, j0);
-            else compute(std::false_type{}, std::false_type{}, kl, vl, j0);
+            if (it + 2 < have) load_tile<D>(pc, K, p.k_token, j0 + 2 * S * kKeys, n, kl);
+            if (it + 1 < mine) compute(std::true_type{}, safe, st, nx, kn, vl, j0);
+            else if (it < mine) compute(std::false_type{}, safe, st, nx, kn, vl, j0);
         };
-        for (int it = 0; it < tiles; it += 2) {
-            step(it, k0, v0, k1, v1);
-            if (it + 1 < tiles) step(it + 1, k1, v1, k0, v0);
+        for (int it = 0; it < rounds; it += 2) {
+            step(it, sa, sb, k0, v0, k1, v1);
+            if (it + 1 < rounds) step(it + 1, sb, sa, k1, v1, k0, v0);
+        }
+        if constexpr (S == 2) {
+            // The second group's state joins the first's, through its own tiles' places.
+            __syncthreads();
+            float* mem[DB] = {};
+            uint16_t* const place[4] = {k0s, k1s, v0s, v1s};         // S kKeys D elements each: 64 D floats
+#pragma unroll
+            for (int d = 0; d < DB; ++d) mem[d] = reinterpret_cast<float*>(place[d]) + wave * 16 * 64 + lane;
+            __shared__ float ml[kWaves][2][64];
+            if (group == 1) {
+                ml[wave][0][lane] = m;
+                ml[wave][1][lane] = l;
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) mem[d][64 * i] = o[d][i];
+            }
+            __syncthreads();
+            if (group == 0) {
+                const float m1 = ml[wave][0][lane], big = fmaxf(m, m1), c = big == -INFINITY ? 0.f : big * p.c;
+                const float a = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - c);
+                const float a1 = m1 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m1 * p.c - c);
+                l = l * a + ml[wave][1][lane] * a1;
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[d][i] = o[d][i] * a + mem[d][64 * i] * a1;
+            }
         }
     };
     pass(std::false_type{});
@@ -241,53 +329,255 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_bf16(PromptParams p) 
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) odd = fmaf(o[d][i], 0.f, odd);       // NaN if any is not finite
-    if (__syncthreads_or(odd != odd && row < n)) {
+    if (__syncthreads_or(odd != odd && row < n && group == 0)) {
         m = -INFINITY;
         mc = l = 0.f;
         pass(std::true_type{});
     }
     l = pair_sum32(l);
-    if (row >= n) return;
+    if (row >= n || group != 0) return;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const int64_t at = h * p.o_head + (t.first + row) * p.o_token + 4 * lh;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t e = at + 32 * d + 8 * i;
-            const float y0 = o[d][4 * i] * inv, y1 = o[d][4 * i + 1] * inv, y2 = o[d][4 * i + 2] * inv,
-                        y3 = o[d][4 * i + 3] * inv;
-            if (p.out_bf16)
-                *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + e) = make_uint2(pack_bf16x2(y0, y1), pack_bf16x2(y2, y3));
-            else
-                *reinterpret_cast<f32x4_t*>(static_cast<float*>(p.out) + e) = f32x4_t{y0, y1, y2, y3};
-        }
+        for (int i = 0; i < 4; ++i)
+            store4(p, at + 32 * d + 8 * i, o[d][4 * i] * inv, o[d][4 * i + 1] * inv, o[d][4 * i + 2] * inv, o[d][4 * i + 3] * inv);
 }
 
-// float32: the same layouts on v_mfma_f32_32x32x2_f32, 32 keys to a tile.  The
-// score product takes four dims of a key from one 16-byte read (lane half lh:
-// dims 8 s + 4 lh ..), the PV product takes score register i as it stands (its two
-// contraction slots are the keys of the lane halves).  64 rows (two waves) to a
-// workgroup: the products, 16 times slower than bf16's, hide the rest, and short
-// prompts still give many workgroups.
-constexpr int kRows32 = 64, kKeys32 = 32, kWaves32 = 2;
-
+// The states of a workgroup's four waves, each over its own keys of the same 32 rows,
+// to the rows' outputs.  mem: room for [wave][dim block][register][lane].  A wave
+// stores the dims of four registers of every 16 (8 of a row's 32).
 template <int D>
-__global__ __launch_bounds__(64 * kWaves32, 2) void k_prompt_f32(PromptParams p) {
+__device__ __forceinline__ void join_waves(const PromptParams& p, float* mem, float m, float l, const f32x16_t (&o)[D / 32],
+                                           const RowTile& t, int row, int h) {
     constexpr int DB = D / 32;
-    constexpr int KS = D + 4;       // K row stride: 16-byte reads of 8 rows meet every bank once
-    __shared__ __align__(16) float kl[kKeys32 * KS];
-    __shared__ __align__(16) float vl[kKeys32 * D];
+    __shared__ float ml[kWaves][2][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lh = lane >> 5;
+    ml[wave][0][lane] = m;
+    ml[wave][1][lane] = pair_sum32(l);
+    mem += lane;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mem[((wave * DB + d) * 16 + i) * 64] = o[d][i];
+    __syncthreads();
+    if (row >= t.len) return;
+    float big = -INFINITY, a[kWaves], sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) big = fmaxf(big, ml[w][0][lane]);
+    const float c = big == -INFINITY ? 0.f : big * p.c;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        const float mw = ml[w][0][lane];
+        a[w] = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw * p.c - c);
+        sum += a[w] * ml[w][1][lane];
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const int64_t at = h * p.o_head + (t.first + row) * p.o_token + 4 * lh + 8 * wave;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) {
+        float y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            y[i] = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) y[i] += a[w] * mem[((w * DB + d) * 16 + 4 * wave + i) * 64];
+        }
+        store4(p, at + 32 * d, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
+    }
+}
+
+// The same for batches too small to fill the chip with 128-row workgroups: a
+// workgroup takes 32 rows, and its four waves every fourth tile of keys each, in
+// places of their own (one K and one V tile a wave, no barrier: the next K tile is
+// loaded once the scores have read this one, the next V tile once the output has).
+// The waves' states meet at the end, each wave taking a quarter of the output.
+template <int D>
+__global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_narrow(PromptParams p) {
+    constexpr int SL = D / 16, DB = D / 32, C = D / 8;
+    constexpr int kPieces = kKeys * C / 64, kPer = 64 / C;        // 16-byte pieces of a lane, rows of a piece
+    __shared__ __align__(16) uint16_t ks[kWaves * kKeys * D], vs[kWaves * kKeys * D];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int lq = lane & 31, lh = lane >> 5;
     const uint32_t xcd = blockIdx.x & 7u, slot = blockIdx.x >> 3;
     const uint32_t unit = slot / p.G * 8u + xcd;
     const int g = (int)(unit % p.Hkv), h = g * p.G + (int)(slot % p.G);
     RowTile t;
-    if (!find_tile(p.cu, p.batch, p.T, kRows32, unit / p.Hkv, t)) return;
-    const int n = t.len, q0 = t.tile * kRows32 + 32 * wave, row = q0 + lq;
+    if (!find_tile(p.cu, p.batch, p.T, kNarrowRows, unit / p.Hkv, t)) return;
+    const int n = t.len, q0 = t.tile * kNarrowRows, row = q0 + lq;
+    const uint16_t* K = static_cast<const uint16_t*>(p.K) + g * p.k_head + t.first * p.k_token;
+    const uint16_t* V = static_cast<const uint16_t*>(p.V) + g * p.v_head + t.first * p.v_token;
+    uint16_t* const kl = ks + wave * kKeys * D;
+    uint16_t* const vl = vs + wave * kKeys * D;
+
+    const auto load = [&](const uint16_t* x, int64_t tok, int j0, uint16_t* to) __attribute__((always_inline)) {
+        const char* from = reinterpret_cast<const char*>(x + j0 * tok);
+        const uint32_t step = 2u * (uint32_t)tok;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int r = kPer * i + lane / C, rr = r < n - j0 ? r : n - 1 - j0;
+            __builtin_amdgcn_global_load_lds((gptr_t)(from + (uint32_t)(rr * step + 16 * (lane % C ^ swizzle<D>(r)))),
+                                             (lptr_t)(to + 64 * 8 * i), 16, 0, 0);
+        }
+    };
+    const int last = p.causal ? (row < n ? row : n - 1) : n - 1;
+    const int kend = p.causal && q0 + kNarrowRows < n ? q0 + kNarrowRows : n;
+    const int wfull = p.causal ? q0 : n - 1;
+    const int tiles = (kend + kKeys - 1) / kKeys;
+    u32x4_t qf[SL];
+    {
+        const int r = row < n ? row : n - 1;
+        const uint16_t* qp = static_cast<const uint16_t*>(p.Q) + h * p.q_head + (t.first + r) * p.q_token + 8 * lh;
+#pragma unroll
+        for (int s = 0; s < SL; ++s) qf[s] = *reinterpret_cast<const u32x4_t*>(qp + 16 * s);
+    }
+    f32x16_t o[DB];
+    float m, mc, l;
+    const int r0 = 4 * lh + ((lane & 15) >> 2), cq = 2 * (lane >> 4 & 1) + ((lane & 3) >> 1);
+    // kSafe: V may hold infinities or NaN under the mask
+    const auto pass = [&](auto safe) __attribute__((always_inline)) {
+        constexpr bool kSafe = decltype(safe)::value;
+        if (wave < tiles) {
+            load(K, p.k_token, wave * kKeys, kl);
+            load(V, p.v_token, wave * kKeys, vl);
+        }
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+        m = -INFINITY;
+        mc = l = 0.f;
+        for (int it = wave; it < tiles; it += kWaves) {
+            const int j0 = it * kKeys, jn = j0 + kWaves * kKeys;
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kPieces) : "memory");       // K; V may still be on its way
+            f32x16_t st[2];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) st[b][i] = 0.f;
+#pragma unroll
+                for (int s = 0; s < SL; ++s) {
+                    const u32x4_t a = *reinterpret_cast<const u32x4_t*>(kl + (32 * b + lq) * D + 8 * ((2 * s + lh) ^ swizzle<D>(lq)));
+                    st[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(qf[s]), st[b], 0, 0, 0);
+                }
+            }
+            if (j0 + kKeys - 1 > wfull) {
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (j0 + 32 * b + 8 * (i / 4) + 4 * lh + i % 4 > last) st[b][i] = -INFINITY;
+            }
+            float mx = st[0][0];
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) mx = fmaxf(mx, st[b][i]);
+            mx = pair_max32(mx);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // every read of K has returned
+            if (jn < kend) load(K, p.k_token, jn, kl);
+            if (__any(mx > m + p.slack)) {
+                const bool none = m == -INFINITY;
+                m = fmaxf(m, mx);
+                const float nc = m == -INFINITY ? 0.f : m * p.c;
+                const float al = none ? 0.f : __builtin_amdgcn_exp2f(mc - nc);
+                mc = nc;
+                l *= al;
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[d][i] *= al;
+            }
+            u32x4_t pf[4];
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) {
+                    const float x = __builtin_amdgcn_exp2f(fmaf(st[b][i], p.c, -mc));
+                    const float y = __builtin_amdgcn_exp2f(fmaf(st[b][i + 1], p.c, -mc));
+                    l += x + y;
+                    pf[2 * b + i / 8][i % 8 / 2] = pack_bf16x2(x, y);
+                }
+            if (jn < kend) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kPieces) : "memory");      // V; not the next K
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                    const int c = 4 * d + cq;
+                    const uint2 a = lds_read_tr16(vl + (16 * u + r0) * D + 8 * (c ^ swizzle<D>(r0)) + 4 * (lane & 1));
+                    const uint2 b = lds_read_tr16(vl + (16 * u + r0 + 8) * D + 8 * (c ^ swizzle<D>(r0 + 8)) + 4 * (lane & 1));
+                    u32x4_t v = {a.x, a.y, b.x, b.y};
+                    if constexpr (kSafe) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v[i] = finite_only(v[i]);
+                    }
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v), as_bf16x8(pf[u]), o[d], 0, 0, 0);
+                }
+            for (int r = 0; kSafe && r < kKeys; ++r)
+#pragma unroll
+                    for (int d = 0; d < DB; ++d)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int dim = 32 * d + 8 * (i / 4) + 4 * lh + i % 4;
+                            const uint16_t v = vl[r * D + 8 * ((dim >> 3) ^ swizzle<D>(r)) + (dim & 7)];
+                            if (odd_half(v) && j0 + r <= last) o[d][i] += bf16_to_f32(v);
+                        }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // every read of V has returned
+            if (jn < kend) load(V, p.v_token, jn, vl);
+        }
+    };
+    pass(std::false_type{});
+    float odd = 0.f;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) odd = fmaf(o[d][i], 0.f, odd);
+    if (__syncthreads_or(odd != odd && row < n)) pass(std::true_type{});
+    join_waves<D>(p, reinterpret_cast<float*>(ks), m, l, o, t, row, h);
+}
+
+// float32: the narrow form's plan and the same layouts on v_mfma_f32_32x32x2_f32 (16
+// times slower than bf16's: it hides everything else, and so few rows to a workgroup
+// keep the chip busy on short prompts), 32 keys to a tile.  The score product takes
+// four dims of a key from one 16-byte read (lane half lh: dims 8 s + 4 lh ..), the PV
+// product score register i as it stands (its two contraction slots are the keys of
+// the lane halves).  16-byte chunk c of row r lies in place c ^ (r % 16).
+constexpr int kKeys32 = 32;
+
+template <int D>
+__global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_f32(PromptParams p) {
+    constexpr int DB = D / 32, C = D / 4;
+    constexpr int kPieces = kKeys32 * C / 64, kPer = 64 / C;
+    __shared__ __align__(16) float ks[kWaves * kKeys32 * D], vs[kWaves * kKeys32 * D];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lq = lane & 31, lh = lane >> 5;
+    const uint32_t xcd = blockIdx.x & 7u, slot = blockIdx.x >> 3;
+    const uint32_t unit = slot / p.G * 8u + xcd;
+    const int g = (int)(unit % p.Hkv), h = g * p.G + (int)(slot % p.G);
+    RowTile t;
+    if (!find_tile(p.cu, p.batch, p.T, kNarrowRows, unit / p.Hkv, t)) return;
+    const int n = t.len, q0 = t.tile * kNarrowRows, row = q0 + lq;
     const float* K = static_cast<const float*>(p.K) + g * p.k_head + t.first * p.k_token;
     const float* V = static_cast<const float*>(p.V) + g * p.v_head + t.first * p.v_token;
+    float* const kl = ks + wave * kKeys32 * D;
+    float* const vl = vs + wave * kKeys32 * D;
+
+    const auto load = [&](const float* x, int64_t tok, int j0, float* to) __attribute__((always_inline)) {
+        const char* from = reinterpret_cast<const char*>(x + j0 * tok);
+        const uint32_t step = 4u * (uint32_t)tok;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int r = kPer * i + lane / C, rr = r < n - j0 ? r : n - 1 - j0;
+            __builtin_amdgcn_global_load_lds((gptr_t)(from + (uint32_t)(rr * step + 16 * (lane % C ^ (r & 15)))),
+                                             (lptr_t)(to + 64 * 4 * i), 16, 0, 0);
+        }
+    };
+    const int last = p.causal ? (row < n ? row : n - 1) : n - 1;
+    const int kend = p.causal && q0 + kNarrowRows < n ? q0 + kNarrowRows : n;
+    const int wfull = p.causal ? q0 : n - 1;
+    const int tiles = (kend + kKeys32 - 1) / kKeys32;
     f32x4_t qf[D / 8];
     {
         const int r = row < n ? row : n - 1;
@@ -295,43 +585,34 @@ __global__ __launch_bounds__(64 * kWaves32, 2) void k_prompt_f32(PromptParams p)
 #pragma unroll
         for (int s = 0; s < D / 8; ++s) qf[s] = *reinterpret_cast<const f32x4_t*>(qp + 8 * s);
     }
-    const int last = p.causal ? (row < n ? row : n - 1) : n - 1;
-    const int wlast = p.causal ? (q0 + 31 < n ? q0 + 31 : n - 1) : n - 1;
-    const int wfull = p.causal ? q0 : n - 1;
-    const int kend = p.causal && (t.tile + 1) * kRows32 < n ? (t.tile + 1) * kRows32 : n;
-    const int tiles = (kend + kKeys32 - 1) / kKeys32;
     f32x16_t o[DB];
-    float m, l;
-    for (int safe = 0;; safe = 1) {
+    float m, mc, l;
+    // kSafe: V may hold infinities or NaN under the mask
+    const auto pass = [&](auto safe) __attribute__((always_inline)) {
+        constexpr bool kSafe = decltype(safe)::value;
+        if (wave < tiles) {
+            load(K, p.k_token, wave * kKeys32, kl);
+            load(V, p.v_token, wave * kKeys32, vl);
+        }
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
         m = -INFINITY;
-        float mc = 0.f;
-        l = 0.f;
-        for (int it = 0; it < tiles; ++it) {
-            const int j0 = it * kKeys32;
-            __syncthreads();
-#pragma unroll
-            for (int e = threadIdx.x; e < kKeys32 * D / 4; e += 64 * kWaves32) {
-                const int r = e / (D / 4), c = 4 * (e % (D / 4)), j = j0 + r < n ? j0 + r : n - 1;
-                *reinterpret_cast<f32x4_t*>(kl + r * KS + c) = *reinterpret_cast<const f32x4_t*>(K + j * p.k_token + c);
-                *reinterpret_cast<f32x4_t*>(vl + r * D + c) = *reinterpret_cast<const f32x4_t*>(V + j * p.v_token + c);
-            }
-            __syncthreads();
-            if (q0 >= n || j0 > wlast) continue;
+        mc = l = 0.f;
+        for (int it = wave; it < tiles; it += kWaves) {
+            const int j0 = it * kKeys32, jn = j0 + kWaves * kKeys32;
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kPieces) : "memory");       // K; V may still be on its way
             f32x16_t st;
 #pragma unroll
             for (int i = 0; i < 16; ++i) st[i] = 0.f;
 #pragma unroll
             for (int s = 0; s < D / 8; ++s) {
-                const f32x4_t a = *reinterpret_cast<const f32x4_t*>(kl + lq * KS + 8 * s + 4 * lh);
+                const f32x4_t a = *reinterpret_cast<const f32x4_t*>(kl + lq * D + 4 * ((2 * s + lh) ^ (lq & 15)));
 #pragma unroll
                 for (int e = 0; e < 4; ++e) st = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], qf[s][e], st, 0, 0, 0);
             }
-            const bool cut = j0 + kKeys32 - 1 > wfull;
-            if (cut) {
+            if (j0 + kKeys32 - 1 > wfull) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
                     if (j0 + 8 * (i / 4) + 4 * lh + i % 4 > last) st[i] = -INFINITY;
@@ -340,6 +621,8 @@ __global__ __launch_bounds__(64 * kWaves32, 2) void k_prompt_f32(PromptParams p)
 #pragma unroll
             for (int i = 0; i < 16; ++i) mx = fmaxf(mx, st[i]);
             mx = pair_max32(mx);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // every read of K has returned
+            if (jn < kend) load(K, p.k_token, jn, kl);
             if (__any(mx > m + p.slack)) {
                 const bool none = m == -INFINITY;
                 m = fmaxf(m, mx);
@@ -357,68 +640,70 @@ __global__ __launch_bounds__(64 * kWaves32, 2) void k_prompt_f32(PromptParams p)
                 st[i] = __builtin_amdgcn_exp2f(fmaf(st[i], p.c, -mc));
                 l += st[i];
             }
+            if (jn < kend) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kPieces) : "memory");      // V; not the next K
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int r = 8 * (i / 4) + 4 * lh + i % 4;
 #pragma unroll
                 for (int d = 0; d < DB; ++d) {
-                    float v = vl[r * D + 32 * d + lq];
-                    if (safe && cut && !isfinite(v)) v = 0.f;
+                    float v = vl[r * D + 4 * ((8 * d + lq / 4) ^ (r & 15)) + lq % 4];
+                    if (kSafe && !isfinite(v)) v = 0.f;
                     o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, st[i], o[d], 0, 0, 0);
                 }
             }
-            if (safe && cut)
-                for (int r = 0; r < kKeys32; ++r)
+            for (int r = 0; kSafe && r < kKeys32; ++r)
 #pragma unroll
                     for (int d = 0; d < DB; ++d)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            const float v = vl[r * D + 32 * d + 8 * (i / 4) + 4 * lh + i % 4];
+                            const int dim = 32 * d + 8 * (i / 4) + 4 * lh + i % 4;
+                            const float v = vl[r * D + 4 * (dim / 4 ^ (r & 15)) + dim % 4];
                             if (!isfinite(v) && j0 + r <= last) o[d][i] += v;
                         }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // every read of V has returned
+            if (jn < kend) load(V, p.v_token, jn, vl);
         }
-        float odd = 0.f;
-#pragma unroll
-        for (int d = 0; d < DB; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) odd = fmaf(o[d][i], 0.f, odd);
-        if (!__syncthreads_or(odd != odd && row < n && !safe)) break;
-    }
-    l = pair_sum32(l);
-    if (row >= n) return;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    const int64_t at = h * p.o_head + (t.first + row) * p.o_token + 4 * lh;
+    };
+    pass(std::false_type{});
+    float odd = 0.f;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t e = at + 32 * d + 8 * i;
-            const float y0 = o[d][4 * i] * inv, y1 = o[d][4 * i + 1] * inv, y2 = o[d][4 * i + 2] * inv,
-                        y3 = o[d][4 * i + 3] * inv;
-            if (p.out_bf16)
-                *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + e) = make_uint2(pack_bf16x2(y0, y1), pack_bf16x2(y2, y3));
-            else
-                *reinterpret_cast<f32x4_t*>(static_cast<float*>(p.out) + e) = f32x4_t{y0, y1, y2, y3};
-        }
+        for (int i = 0; i < 16; ++i) odd = fmaf(o[d][i], 0.f, odd);
+    if (__syncthreads_or(odd != odd && row < n)) pass(std::true_type{});
+    join_waves<D>(p, ks, m, l, o, t, row, h);       // a wave's state takes its K tile's place
 }
+
+// Workgroups of a launch whose row tiles hold `rows`: sequences end inside their
+// last tile.
+int64_t blocks_of(const PromptParams& p, int rows) {
+    const int64_t tiles = (p.T + (int64_t)p.batch * (rows - 1)) / rows;
+    return (tiles * p.Hkv + 7) / 8 * 8 * p.G;
+}
+
+// The narrow form while its workgroups are resident at once (one a CU at D = 128, two
+// at D = 64) and prompts are longer than a tile of keys: 12/2 heads, one prompt of
+// 256 tokens 8.2 against 10.8 us at D = 128 and 6.1 against 8.0 at D = 64, of 512 11.2
+// against 15.3 and 7.7 against 11.1; two of 512, more than fit, 18.5 against 15.9.
+bool narrow(const PromptParams& p) { return p.T > (int64_t)p.batch * kKeys && blocks_of(p, kNarrowRows) <= (p.D == 128 ? 256 : 512); }
+
+// Two groups of waves where long prompts' workgroups do not fill the chip and the
+// longest bounds the time: one prompt of 2,048 35 against 42 us, of 4,096 69 against
+// 86, of 8,192 (768 workgroups) 226 against 209; eight of 512 25 against 20.
+bool split(const PromptParams& p) { return p.T >= (int64_t)p.batch * 512 && blocks_of(p, kRows) <= 440; }
 
 }  // namespace
 
-int64_t prompt_blocks(int64_t T, int batch, int Hkv, int G, int in_bf16) {
-    const int rows = in_bf16 ? kRows : kRows32;
-    const int64_t tiles = (T + (int64_t)batch * (rows - 1)) / rows;     // sequences end inside their last tile
-    return (tiles * Hkv + 7) / 8 * 8 * G;
-}
+int64_t prompt_blocks(const PromptParams& p) { return blocks_of(p, p.in_bf16 && !narrow(p) ? kRows : kNarrowRows); }
 
 hipError_t launch_prompt_attn(const PromptParams& p, hipStream_t st) {
-    const dim3 grid((unsigned)prompt_blocks(p.T, p.batch, p.Hkv, p.G, p.in_bf16));
-    if (p.in_bf16) {
-        if (p.D == 128) hipLaunchKernelGGL(k_prompt_bf16<128>, grid, dim3(64 * kWaves), 0, st, p);
-        else hipLaunchKernelGGL(k_prompt_bf16<64>, grid, dim3(64 * kWaves), 0, st, p);
-    } else {
-        if (p.D == 128) hipLaunchKernelGGL(k_prompt_f32<128>, grid, dim3(64 * kWaves32), 0, st, p);
-        else hipLaunchKernelGGL(k_prompt_f32<64>, grid, dim3(64 * kWaves32), 0, st, p);
-    }
+    const dim3 grid((unsigned)prompt_blocks(p));
+    const auto run = [&](auto kernel, int waves) { hipLaunchKernelGGL(kernel, grid, dim3(64 * waves), 0, st, p); };
+    if (!p.in_bf16) p.D == 128 ? run(k_prompt_f32<128>, kWaves) : run(k_prompt_f32<64>, kWaves);
+    else if (narrow(p)) p.D == 128 ? run(k_prompt_narrow<128>, kWaves) : run(k_prompt_narrow<64>, kWaves);
+    else if (split(p)) p.D == 128 ? run(k_prompt_bf16<128, 2>, 2 * kWaves) : run(k_prompt_bf16<64, 2>, 2 * kWaves);
+    else p.D == 128 ? run(k_prompt_bf16<128, 1>, kWaves) : run(k_prompt_bf16<64, 1>, kWaves);
     return hipGetLastError();
 }
 

@@ -144,7 +144,7 @@ struct PromptParams {
     float c;                      // score scale in the log2 domain
     float slack;                  // scores above the reference maximum before it moves
 };
-int64_t prompt_blocks(int64_t T, int batch, int Hkv, int G, int in_bf16);   // workgroups of a launch
+int64_t prompt_blocks(const PromptParams& p);   // workgroups of a launch
 hipError_t launch_prompt_attn(const PromptParams& p, hipStream_t st);
 
 // 4-bit key/value cache.

@@ -166,7 +166,7 @@ int ris_prompt_attn(const void* Q, const void* K, const void* V, const int64_t* 
     p.in_bf16 = d.dtype_in == RIS_BF16; p.out_bf16 = d.dtype_out == RIS_BF16;
     p.c = (d.scale > 0.0f ? d.scale : 1.0f / sqrtf((float)d.D)) * 1.4426950408889634f;
     p.slack = 8.0f / p.c;
-    if (!fits_dispatch(ris::prompt_blocks(p.T, p.batch, p.Hkv, p.G, p.in_bf16), 256)) return RIS_E_UNSUPPORTED;
+    if (!fits_dispatch(ris::prompt_blocks(p), 256)) return RIS_E_UNSUPPORTED;
     return hip_status(ris::launch_prompt_attn(p, static_cast<hipStream_t>(stream)));
 }
 
