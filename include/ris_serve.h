@@ -65,7 +65,9 @@ typedef struct {
     int64_t q_head, q_token; /* element (h, t, d) of Q is at                    */
     int64_t k_head, k_token; /*   h * q_head + t * q_token + d; likewise K, V   */
     int64_t v_head, v_token; /*   and out.  Strides >= 0; every one of them and */
-    int64_t o_head, o_token; /*   every base a multiple of 16 bytes             */
+    int64_t o_head, o_token; /*   every base a multiple of 16 bytes; of out > 0 */
+                             /*   where there is more than one row; K and V     */
+                             /*   tokens less than 2^24 - 1024 apart            */
 } ris_prompt_desc;
 
 /*

@@ -252,9 +252,10 @@ __global__ __launch_bounds__(kThreads) void k_logprob(LogprobParams p) {
         }
 #pragma unroll
         for (int i = 0; i < kUnroll; ++i) {
+            if (v + i * kThreads + wave * 64 >= v1) break;          // nothing of the wave's is left
             float x[E];
             unpack<BF16>(r[i], x);
-            take(x, E, (uint32_t)(head + (v + i * kThreads + tid) * E));
+            take(x, E, (uint32_t)head + (uint32_t)(v + i * kThreads + tid) * E);
         }
     }
     {

@@ -9,53 +9,77 @@ namespace ris {
 
 __device__ __forceinline__ int clip_offset(int64_t v, int64_t T) { return (int)(v < 0 ? 0 : (v > T ? T : v)); }
 
-// Tile `idx` of the tiles of `rows` rows that the sequences are cut into, those
-// far into their sequences first: under a causal mask they cost most, and what is
-// long goes first so that the end is short.  (More than 64 sequences: one sequence
-// after another.)  By the whole wave, idx uniform; false past the last tile.
+// Tile `idx` of the tiles of `rows` rows that the sequences are cut into.  By the
+// whole wave, idx uniform; false where there is none.
+//
+// Up to 64 sequences, tiles far into their sequences come first: under a causal mask
+// they cost most, and what is long goes first so that the end is short.  Beyond, the
+// tiles of sequence b have the places from cu[b] / rows + b on, as many as it can need
+// (some stay empty), so that one search finds idx, the last tile of a sequence first.
 struct RowTile {
     int first;      // the sequence's first token
     int len;        // its tokens
     int tile;       // its tile: rows [tile * rows, ..)
 };
+constexpr int kSortedBatch = 64;
+
+// Places of the tiles of T tokens in `batch` sequences.
+inline int64_t tile_places(int64_t T, int64_t batch, int rows) {
+    return batch <= kSortedBatch ? (T + batch * (rows - 1)) / rows : T / rows + batch;
+}
+
 __device__ __forceinline__ bool find_tile(const int64_t* cu, int batch, int64_t T, int rows, uint32_t idx, RowTile& t) {
     const int lane = threadIdx.x & 63;
-    for (int b0 = 0; b0 < batch; b0 += 64) {
-        const int b = b0 + lane;
-        int lo = 0, len = 0;
-        if (b < batch) {
-            lo = clip_offset(cu[b], T);
-            len = clip_offset(cu[b + 1], T) - lo;
-            if (len < 0) len = 0;
-        }
-        const uint32_t nt = ((uint32_t)len + rows - 1) / rows;
-        const uint32_t upto = wave_inclusive_scan(nt);
-        const uint32_t total = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
-        if (idx < total) {
-            int at;
-            if (batch > 1 && batch <= 64) {
-                // the last level of which more than idx tiles are that far or farther
-                uint32_t level = 0, beyond = 0;                  // beyond: tiles above the level
-                for (uint32_t bit = 1u << (31 - __builtin_clz(total)); bit; bit >>= 1) {
-                    const uint32_t l = level | bit;
-                    if (wave_sum_u32(nt > l ? nt - l : 0u) > idx) level = l;
-                }
-                beyond = wave_sum_u32(nt > level + 1 ? nt - level - 1 : 0u);
-                uint64_t on = __ballot(nt > level);
-                for (uint32_t i = idx - beyond; i; --i) on &= on - 1;
-                at = (int)__builtin_ctzll(on);
-                t.tile = (int)level;
-            } else {
-                at = (int)__builtin_ctzll(__ballot(upto > idx));
-                t.tile = __builtin_amdgcn_readlane((int)upto, at) - 1 - (int)idx;
+    if (batch > kSortedBatch) {
+        const auto place = [&](int b) { return (uint32_t)clip_offset(cu[b], T) / (uint32_t)rows + (uint32_t)b; };
+        // sequences whose first place is at most idx, 64 looked at in a step
+        int lo = 0, n = batch;
+        while (n > 64) {
+            const int step = (n + 63) / 64, at = lane * step;
+            const int c = __popcll(__ballot(at < n && place(lo + at) <= idx));
+            if (c == 0) {
+                n = 0;
+                break;
             }
-            t.first = __builtin_amdgcn_readlane(lo, at);
-            t.len = __builtin_amdgcn_readlane(len, at);
-            return true;
+            const int skip = (c - 1) * step + 1;
+            n = n - skip < step - 1 ? n - skip : step - 1;
+            lo += skip;
         }
-        idx -= total;
+        const int b = lo + __popcll(__ballot(lane < n && place(lo + lane) <= idx)) - 1;
+        if (b < 0) return false;
+        t.first = clip_offset(cu[b], T);
+        t.len = clip_offset(cu[b + 1], T) - t.first;
+        const uint32_t j = idx - place(b), nt = t.len > 0 ? ((uint32_t)t.len + rows - 1) / rows : 0u;
+        t.tile = (int)(nt - 1 - j);
+        return j < nt;
     }
-    return false;
+    int lo = 0, len = 0;
+    if (lane < batch) {
+        lo = clip_offset(cu[lane], T);
+        len = clip_offset(cu[lane + 1], T) - lo;
+        if (len < 0) len = 0;
+    }
+    const uint32_t nt = ((uint32_t)len + rows - 1) / rows;
+    const uint32_t total = wave_sum_u32(nt);
+    if (idx >= total) return false;
+    int at = 0;
+    if (batch == 1) {
+        t.tile = (int)(total - 1 - idx);
+    } else {
+        // the last level of which more than idx tiles are that far or farther
+        uint32_t level = 0;
+        for (uint32_t bit = 1u << (31 - __builtin_clz(total)); bit; bit >>= 1) {
+            const uint32_t l = level | bit;
+            if (wave_sum_u32(nt > l ? nt - l : 0u) > idx) level = l;
+        }
+        uint64_t on = __ballot(nt > level);
+        for (uint32_t i = idx - wave_sum_u32(nt > level + 1 ? nt - level - 1 : 0u); i; --i) on &= on - 1;
+        at = (int)__builtin_ctzll(on);
+        t.tile = (int)level;
+    }
+    t.first = __builtin_amdgcn_readlane(lo, at);
+    t.len = __builtin_amdgcn_readlane(len, at);
+    return true;
 }
 
 // The sequence that owns token t (uniform), by the whole wave: the number of

@@ -675,11 +675,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_f32(PromptParams p) {
     join_waves<D>(p, ks, m, l, o, t, row, h);       // a wave's state takes its K tile's place
 }
 
-// Workgroups of a launch whose row tiles hold `rows`: sequences end inside their
-// last tile.
+// Workgroups of a launch whose row tiles hold `rows`.
 int64_t blocks_of(const PromptParams& p, int rows) {
-    const int64_t tiles = (p.T + (int64_t)p.batch * (rows - 1)) / rows;
-    return (tiles * p.Hkv + 7) / 8 * 8 * p.G;
+    return (tile_places(p.T, p.batch, rows) * p.Hkv + 7) / 8 * 8 * p.G;
 }
 
 // The narrow form while its workgroups are resident at once (one a CU at D = 128, two

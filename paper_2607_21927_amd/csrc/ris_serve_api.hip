@@ -19,6 +19,11 @@ bool vector_rows(const void* p, int64_t head, int64_t token, int32_t dtype) {
     return aligned(p, 16) && head >= 0 && token >= 0 && head % n == 0 && token % n == 0;
 }
 
+// The same for one that is written: rows that all lie in one place are refused.
+bool output_rows(const void* p, int64_t head, int64_t token, int32_t dtype, int64_t heads, int64_t tokens) {
+    return vector_rows(p, head, token, dtype) && (heads == 1 || head > 0) && (tokens == 1 || token > 0);
+}
+
 // Token offsets fit 32 bits (ris_serve.h's packed sequences).
 constexpr int64_t kMaxTokens = 0x7FFFFFFFll;
 
@@ -153,7 +158,8 @@ int ris_prompt_attn(const void* Q, const void* K, const void* V, const int64_t* 
     if (!Q || !K || !V || !cu_seqlens || !out) return RIS_E_ARG;
     const ris_prompt_desc& d = *desc;
     if (!vector_rows(Q, d.q_head, d.q_token, d.dtype_in) || !vector_rows(K, d.k_head, d.k_token, d.dtype_in) ||
-        !vector_rows(V, d.v_head, d.v_token, d.dtype_in) || !vector_rows(out, d.o_head, d.o_token, d.dtype_out))
+        !vector_rows(V, d.v_head, d.v_token, d.dtype_in) ||
+        !output_rows(out, d.o_head, d.o_token, d.dtype_out, d.Hq, d.T))
         return RIS_E_ARG;
     if (d.k_token > kMaxKeyStride || d.v_token > kMaxKeyStride) return RIS_E_UNSUPPORTED;
     ris::PromptParams p;
@@ -183,6 +189,8 @@ int ris_kv4_load(const uint8_t* K4, const uint8_t* V4, const uint8_t* S, const i
     ris::Kv4Params p;
     const int st = kv4_params(K, V, cu_seqlens, start, K4, V4, S, desc, &p);
     if (st != RIS_OK) return st;
+    if (!output_rows(K, p.k_head, p.k_token, desc->dtype, p.Hkv, p.T) || !output_rows(V, p.v_head, p.v_token, desc->dtype, p.Hkv, p.T))
+        return RIS_E_ARG;
     return hip_status(ris::launch_kv4_load(p, static_cast<hipStream_t>(stream)));
 }
 

@@ -83,8 +83,8 @@ def _need_dense(*ts):
 
 
 def _rows(t, shape):
-    """Head and token stride of a [heads, T, D] view whose rows 16-byte accesses can
-    walk; a dimension of one element counts with stride 0."""
+    """Address, head and token stride of a [heads, T, D] view whose rows 16-byte
+    accesses can walk; a dimension of one element counts with stride 0."""
     if t.shape != shape:
         raise ValueError(f"expected a {shape} view, got {tuple(t.shape)}")
     head, token, one = t.stride()
@@ -92,10 +92,10 @@ def _rows(t, shape):
         head = 0
     if shape[1] == 1:
         token = 0
-    per = 16 // t.element_size()
-    if one != 1 or t.data_ptr() % 16 or head % per or token % per:
+    at = t.data_ptr()
+    if one != 1 or (at | (head | token) * t.element_size()) & 15:
         raise ValueError("rows must be contiguous, bases and strides multiples of 16 bytes")
-    return head, token
+    return at, head, token
 
 
 def _bounds(cu_seqlens, start=None):
@@ -116,14 +116,24 @@ def _at(t):
     return 0 if t is None else t.data_ptr()
 
 
+# torch.cuda.current_stream without the Stream object around the handle (1 us of a 9 us call)
+_current_stream = torch._C._cuda_getCurrentRawStream if torch.version.hip else None
+_entry = {}
+
+
 def _call(index, stream, name, *args):
     """Launch on `stream` (torch's current one of GPU `index`) with that GPU current."""
     if index != torch.cuda.current_device():
         with torch.cuda.device(index):
             return _call(index, stream, name, *args)
     if stream is None:
-        stream = torch.cuda.current_stream(index)
-    status = getattr(lib(), name)(*args, stream if isinstance(stream, int) else stream.cuda_stream)
+        stream = _current_stream(index)
+    elif not isinstance(stream, int):
+        stream = stream.cuda_stream
+    entry = _entry.get(name)
+    if entry is None:
+        entry = _entry[name] = getattr(lib(), name)
+    status = entry(*args, stream)
     if status != ris.OK:
         raise ris.RisError(status, name)
 
@@ -148,7 +158,7 @@ def prompt_desc(Q, K, V, out, cu_seqlens, causal=1, scale=0.0):
     """Descriptor from views Q, out [Hq, T, D] and K, V [Hkv, T, D]."""
     Hq, T, D = Q.shape
     return PromptDesc(_dtype_code(Q), _dtype_code(out), Hq, K.shape[0], D, cu_seqlens.numel() - 1, T, causal, scale,
-                      *_rows(Q, Q.shape), *_rows(K, K.shape), *_rows(V, V.shape), *_rows(out, out.shape))
+                      *_rows(Q, Q.shape)[1:], *_rows(K, K.shape)[1:], *_rows(V, V.shape)[1:], *_rows(out, out.shape)[1:])
 
 
 def prompt_attn(Q, K, V, cu_seqlens, out, desc, stream=None):
@@ -161,13 +171,13 @@ def prompt_attn(Q, K, V, cu_seqlens, out, desc, stream=None):
     if _dtype_code(Q) != desc.dtype_in or _dtype_code(out) != desc.dtype_out:
         raise TypeError("Q and out dtypes must match the descriptor")
     q, kv = (desc.Hq, desc.T, desc.D), (desc.Hkv, desc.T, desc.D)
-    if (_rows(Q, q) != (desc.q_head, desc.q_token) or _rows(K, kv) != (desc.k_head, desc.k_token)
-            or _rows(V, kv) != (desc.v_head, desc.v_token) or _rows(out, q) != (desc.o_head, desc.o_token)):
+    (q_at, *sq), (k_at, *sk), (v_at, *sv), (o_at, *so) = _rows(Q, q), _rows(K, kv), _rows(V, kv), _rows(out, q)
+    if sq + sk + sv + so != [desc.q_head, desc.q_token, desc.k_head, desc.k_token, desc.v_head, desc.v_token, desc.o_head,
+                             desc.o_token]:
         raise ValueError("strides must match the descriptor")
     if _bounds(cu_seqlens) != desc.batch:
         raise ValueError("cu_seqlens must hold the descriptor's batch + 1 offsets")
-    _call(index, stream, "ris_prompt_attn", Q.data_ptr(), K.data_ptr(), V.data_ptr(), cu_seqlens.data_ptr(),
-          out.data_ptr(), desc)
+    _call(index, stream, "ris_prompt_attn", q_at, k_at, v_at, cu_seqlens.data_ptr(), o_at, desc)
     return out
 
 
@@ -196,22 +206,24 @@ def _kv4(K, V, cu_seqlens, K4, V4, S, start):
     Hkv, T, D = shape = tuple(K.shape)
     batch = _bounds(cu_seqlens, start)
     max_len = _need_cache(K4, V4, S, batch, Hkv, D)
-    return index, Kv4Desc(_dtype_code(K), Hkv, D, batch, T, max_len, *_rows(K, shape), *_rows(V, shape))
+    k_at, *k_strides = _rows(K, shape)
+    v_at, *v_strides = _rows(V, shape)
+    return index, k_at, v_at, Kv4Desc(_dtype_code(K), Hkv, D, batch, T, max_len, *k_strides, *v_strides)
 
 
 def kv4_store(K, V, cu_seqlens, K4, V4, S, start=None, stream=None):
     """ris_kv4_store: rows K, V [Hkv, T, D] (views as in ``prompt_attn``) quantised
     into the cache, token i of sequence b at position start[b] + i (start None: i)."""
-    index, desc = _kv4(K, V, cu_seqlens, K4, V4, S, start)
-    _call(index, stream, "ris_kv4_store", K.data_ptr(), V.data_ptr(), cu_seqlens.data_ptr(), _at(start), K4.data_ptr(),
+    index, k_at, v_at, desc = _kv4(K, V, cu_seqlens, K4, V4, S, start)
+    _call(index, stream, "ris_kv4_store", k_at, v_at, cu_seqlens.data_ptr(), _at(start), K4.data_ptr(),
           V4.data_ptr(), S.data_ptr(), desc)
 
 
 def kv4_load(K4, V4, S, cu_seqlens, K, V, start=None, stream=None):
     """ris_kv4_load: the cache's values at those positions into K, V [Hkv, T, D]."""
-    index, desc = _kv4(K, V, cu_seqlens, K4, V4, S, start)
+    index, k_at, v_at, desc = _kv4(K, V, cu_seqlens, K4, V4, S, start)
     _call(index, stream, "ris_kv4_load", K4.data_ptr(), V4.data_ptr(), S.data_ptr(), cu_seqlens.data_ptr(), _at(start),
-          K.data_ptr(), V.data_ptr(), desc)
+          k_at, v_at, desc)
 
 
 def kv4_decode_desc(Q, K4, out, anchor_stride=0, window=0, sink=0, scale=0.0):

@@ -52,7 +52,8 @@ def prompt(serve, **kw):
     (dict(D=96), -5), (dict(D=256), -5), (dict(batch=0), -1), (dict(T=0), -1), (dict(T=2**31), -5), (dict(causal=2), -1),
     (dict(scale=-1.0), -1), (dict(scale=float("nan")), -1), (dict(scale=float("inf")), -1), (dict(q_head=-128), -1),
     (dict(k_token=132), -1), (dict(v_head=4), -1), (dict(o_token=1537), -1),
-    (dict(dtype_out=0, o_token=1538), -1), (dict(T=2**31 - 1, Hq=12800, Hkv=100), -5),
+    (dict(dtype_out=0, o_token=1538), -1), (dict(T=2**31 - 1, Hq=12800, Hkv=100), -5), (dict(o_head=0), -1), (dict(o_token=0), -1),
+    (dict(k_token=2**24), -5), (dict(v_token=2**24), -5),
 ])
 def test_prompt_refusals(serve, bad, code):
     assert serve.lib().ris_prompt_attn(P, P, P, P, P, ctypes.byref(prompt(serve, **bad)), None) == code
@@ -102,6 +103,11 @@ def test_kv4_refusals(serve, bad, code):
     d = kv4(serve, **bad)
     assert serve.lib().ris_kv4_store(P, P, P, None, P, P, P, ctypes.byref(d), None) == code
     assert serve.lib().ris_kv4_load(P, P, P, P, None, P, P, ctypes.byref(d), None) == code
+
+
+def test_kv4_load_refuses_rows_in_one_place(serve):
+    for bad in (dict(k_token=0), dict(v_token=0), dict(k_head=0), dict(v_head=0)):
+        assert serve.lib().ris_kv4_load(P, P, P, P, None, P, P, ctypes.byref(kv4(serve, **bad)), None) == -1
 
 
 def test_kv4_null_and_unaligned(serve):
