@@ -159,6 +159,7 @@ __global__ __launch_bounds__(kThreads) void k_logprob(LogprobParams p) {
     constexpr uint32_t kNone = BF16 ? 0xFF80FF80u : 0xFF800000u;      // -inf
     __shared__ State states[kWaves];
     __shared__ uint32_t bound[kWaves][2];
+    __shared__ volatile uint32_t shares[kWaves];        // order of the (k / 4)-th logit of a wave's list, 0: none yet
     __shared__ __align__(16) uint64_t lists[kWaves][RIS_MAX_TOP];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, k = p.top_k;
     const int64_t row = blockIdx.x / p.parts;
@@ -174,6 +175,9 @@ __global__ __launch_bounds__(kThreads) void k_logprob(LogprobParams p) {
     const int v0 = part * per < nv ? part * per : nv, v1 = v0 + per < nv ? v0 + per : nv;
     const u32x4_t* vec = reinterpret_cast<const u32x4_t*>(addr + head * (BF16 ? 2 : 4));
 
+    const int share = k ? (k + kWaves - 1) / kWaves : 1;
+    if (tid < kWaves) shares[tid] = 0;
+    __syncthreads();
     float m = -INFINITY, b = 0.f;           // running maximum; times log2 e where that is a weight's reference, else 0
     float l = 0.f, u = 0.f;                 // sums of 2^d and of 2^d d, d = x log2 e - b
     uint64_t list = 0, least = kNothing;
@@ -201,8 +205,21 @@ __global__ __launch_bounds__(kThreads) void k_logprob(LogprobParams p) {
         // (fmaxf passes a NaN over, l does not.)
         if (k && __any(!(top <= above) || l != l)) {
 #pragma unroll
-            for (int i = 0; i < n; ++i) insert(list, least, key_of(x[i], id + i), k);
-            above = ordered((uint32_t)(least >> 32));
+            for (int i = 0; i < n; ++i)
+                if (__any(!(x[i] < above))) {
+                    insert(list, least, key_of(x[i], id + i), k);
+                    above = ordered((uint32_t)(least >> 32));
+                }
+            if (lane == 0) shares[wave] = (uint32_t)(lane_value(list, share - 1) >> 32);
+        }
+    };
+    // Start the list above the orders below t: at least k tokens of the part are known
+    // to lie at t or above, and t's own logits enter.
+    const auto start_at = [&](uint32_t t) {
+        const uint64_t start = ((uint64_t)t << 32) - 1;
+        if (t && start > least) {
+            least = start;
+            above = ordered(t == 0x80000000u ? t - 2 : t - 1);      // t - 1 under 0 is -0, which equals it
         }
     };
 
@@ -231,7 +248,7 @@ __global__ __launch_bounds__(kThreads) void k_logprob(LogprobParams p) {
                 for (int e = 0; e < E; ++e) top = fmaxf(top, x[e]);
             }
             const uint32_t o = order_of(top);
-            const uint32_t all = nth_largest(o, k), some = nth_largest(o, (k + kWaves - 1) / kWaves);
+            const uint32_t all = nth_largest(o, k), some = nth_largest(o, share);
             if (lane == 0) {
                 bound[wave][0] = all;
                 bound[wave][1] = some;
@@ -243,12 +260,17 @@ __global__ __launch_bounds__(kThreads) void k_logprob(LogprobParams p) {
                 t = bound[w][0] > t ? bound[w][0] : t;
                 f = bound[w][1] < f ? bound[w][1] : f;
             }
-            t = f > t ? f : t;
-            const uint64_t start = ((uint64_t)t << 32) - 1;         // t's own logits enter
-            if (t && start > least) {
-                least = start;
-                above = ordered(t == 0x80000000u ? t - 2 : t - 1);      // t - 1 under 0 is -0, which equals it
+            start_at(f > t ? f : t);
+        } else if (k) {
+            // The least of the waves' (k / 4)-th listed logits is such a bound too, an old
+            // one as well: no wave waits for another.
+            uint32_t t = 0xFFFFFFFFu;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const uint32_t o = shares[w];
+                t = o < t ? o : t;
             }
+            start_at(__builtin_amdgcn_readfirstlane(t));
         }
 #pragma unroll
         for (int i = 0; i < kUnroll; ++i) {
