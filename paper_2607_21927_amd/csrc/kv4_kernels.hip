@@ -75,7 +75,8 @@ __device__ __forceinline__ int64_t cache_row(const Kv4Params& p, int64_t first, 
     if (b < 0) b = 0;
     while (b < p.batch && p.cu[b + 1] <= t) ++b;
     if (t >= p.T || b >= p.batch || t < p.cu[b]) return -1;
-    const int64_t pos = (int64_t)((uint64_t)(t - p.cu[b]) + (uint64_t)(p.start ? p.start[b] : 0));
+    const int64_t from = p.cu[b] > 0 ? p.cu[b] : 0;            // clipped
+    const int64_t pos = (int64_t)((uint64_t)(t - from) + (uint64_t)(p.start ? p.start[b] : 0));
     return pos >= 0 && pos < p.max_len ? ((int64_t)b * p.Hkv + h) * p.max_len + pos : -1;
 }
 

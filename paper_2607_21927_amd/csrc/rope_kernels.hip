@@ -134,7 +134,8 @@ __global__ __launch_bounds__(kThreads) void k_rope_packed(const void* src, int64
     if (b < 0) b = 0;
     while (b < batch && cu[b + 1] <= t) ++b;
     if (t >= T || b >= batch || t < cu[b]) return;
-    const double pos = (double)(t - cu[b] + (start ? start[b] : 0));
+    const int64_t from = cu[b] > 0 ? cu[b] : 0;                   // clipped
+    const double pos = (double)(t - from + (start ? start[b] : 0));
     float c[P], s[P];
 #pragma unroll
     for (int k = 0; k < P; ++k) {

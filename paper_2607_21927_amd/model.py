@@ -248,7 +248,7 @@ class PrefillModel:
         T = ids.shape[0]
         at = torch.arange(1, T + 1, device=ids.device)
         ends = torch.zeros(T + 1, dtype=torch.bool, device=ids.device)
-        ends[cu_seqlens] = True
+        ends[cu_seqlens.clamp(0, T)] = True        # as the kernels read them
         none = ends[1:] | (at <= cu_seqlens[0]) | (at > cu_seqlens[-1])
         targets = torch.where(none, -1, ids.roll(-1))
         return self.score(self.prefill_packed(ids, cu_seqlens, rope_desc), targets[:, None], top_k)

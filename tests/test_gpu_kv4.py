@@ -113,6 +113,20 @@ def test_store_and_load(dtype, D, Hkv):
             assert torch.equal(got.double().cpu().nan_to_num(nan=-1e9), ref.nan_to_num(nan=-1e9))
 
 
+def test_cache_positions_count_from_the_clipped_offset():
+    serve = need_serve()
+    k, v = rows(2, 50, 64, BF16, seed=4)
+    far = torch.tensor([-9, 20, 1 << 40], device="cuda")
+    want, got = serve.kv4_cache(2, 2, 40, 64), serve.kv4_cache(2, 2, 40, 64)
+    serve.kv4_store(k, v, bounds([20, 30]), *want)
+    serve.kv4_store(k, v, far, *got)
+    back = [[torch.zeros_like(k), torch.zeros_like(v)] for _ in range(2)]
+    serve.kv4_load(*want, bounds([20, 30]), *back[0])
+    serve.kv4_load(*want, far, *back[1])
+    for a, b in zip(got + tuple(back[1]), want + tuple(back[0])):
+        assert torch.equal(a, b)
+
+
 def test_store_of_one_token_a_sequence_and_in_a_graph():
     """A decode step's rows: more sequences than a wave looks at in a step."""
     serve = need_serve()

@@ -256,6 +256,16 @@ def test_rope_packed_matches_the_oracle_and_rotates_in_place():
     np.testing.assert_allclose(x.cpu().numpy(), want, atol=2e-6)
 
 
+def test_rope_packed_positions_count_from_the_clipped_offset():
+    serve = need_serve()
+    from paper_2607_21927_amd import ris
+    desc = ris.rope_desc(ris.ROPE_PLAIN, 1e4)
+    x = torch.randn(2, 50, 64, generator=torch.Generator().manual_seed(4)).cuda()
+    far = torch.tensor([-9, 20, 1 << 40], device="cuda")
+    got = serve.rope_packed(x, torch.empty_like(x), far, desc)
+    assert torch.equal(got, serve.rope_packed(x, torch.empty_like(x), bounds([20, 30]), desc))
+
+
 def test_rope_packed_many_sequences_and_graph():
     serve = need_serve()
     from paper_2607_21927_amd import ris

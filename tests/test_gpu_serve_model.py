@@ -91,6 +91,19 @@ def test_scores_of_packed_prompts():
         assert (a - b).abs().max() <= (0 if key == "top_ids" else 1e-5)
 
 
+def test_scores_with_offsets_outside_the_tokens():
+    """Offsets are clipped to the tokens, in scoring as in the kernels."""
+    need_serve()
+    lens = [40, 0, 37]
+    _, _, ids, rd, model = setup("tiny_qwen2", torch.float32, lens)
+    ids_d = torch.tensor(ids, device="cuda")
+    want = model.score_prompts(ids_d, bounds(lens), rd, top_k=2)
+    got = model.score_prompts(ids_d, torch.tensor([-3, 40, 40, 10**12], device="cuda"), rd, top_k=2)
+    for key in want:
+        assert torch.equal(got[key], want[key]), key
+    assert want["logprob"][39] == 0 and want["logprob"][76] == 0 and want["logprob"][38] < 0
+
+
 def oracle_step(tok, W, cfg, pos, caches):
     """One token's final hidden state in float64, over the caches [(K, V)] [Hkv, n, D] of the
     layers, whose last row is the token's own (as the GPU quantised it)."""
