@@ -61,7 +61,7 @@ typedef struct {
     int64_t T;               /* token rows of Q, K, V and out                   */
     int32_t causal;          /* 1 = token i attends to the tokens up to itself; */
                              /* 0 = to its whole sequence                       */
-    float   scale;           /* score scale; 0 = 1 / sqrt(D)                    */
+    float   scale;           /* score scale, up to 2^127; 0 = 1 / sqrt(D)       */
     int64_t q_head, q_token; /* element (h, t, d) of Q is at                    */
     int64_t k_head, k_token; /*   h * q_head + t * q_token + d; likewise K, V   */
     int64_t v_head, v_token; /*   and out.  Strides >= 0; every one of them and */
@@ -132,7 +132,8 @@ int ris_kv4_load(const uint8_t* K4, const uint8_t* V4, const uint8_t* S, const i
  * ris_decode_attn over the 4-bit cache: the same descriptor, sets, clipping and
  * empty-row rule, with K and V read as the values they stand for.  window >=
  * max_len attends to every key up to pos[b] (the dense step).  anchor_ptr and
- * anchor_idx may be NULL when anchor_stride is 0 (no anchor).  The workspace is
+ * anchor_idx may be NULL when anchor_stride is 0 (no anchor).  scale goes up to
+ * 2^127.  The workspace is
  * ris_kv4_decode_workspace_bytes(desc) bytes, 16-byte aligned, and may not be
  * shared by calls that overlap in time.  Q must be 16-byte aligned.
  */

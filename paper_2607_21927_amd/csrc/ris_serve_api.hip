@@ -1,4 +1,5 @@
 // C ABI of the serving operators (ris_serve.h): argument validation and dispatch.
+#include <float.h>
 #include <math.h>
 #include <stdint.h>
 
@@ -6,6 +7,8 @@
 #include "ris_serve.h"
 
 namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;      // scores are weighed in the log2 domain
 
 int hip_status(hipError_t e) { return e == hipSuccess ? RIS_OK : RIS_E_HIP; }
 
@@ -41,7 +44,7 @@ int validate_prompt(const ris_prompt_desc* d) {
     if (d->Hq % d->Hkv != 0) return RIS_E_SHAPE;
     if (d->D != 64 && d->D != 128) return RIS_E_UNSUPPORTED;
     if (d->causal != 0 && d->causal != 1) return RIS_E_ARG;
-    if (!(d->scale >= 0.0f) || !isfinite(d->scale)) return RIS_E_ARG;
+    if (!(d->scale >= 0.0f) || !isfinite(d->scale * kLog2e)) return RIS_E_ARG;
     if (d->T > kMaxTokens || d->batch > (1 << 24)) return RIS_E_UNSUPPORTED;
     return RIS_OK;
 }
@@ -86,7 +89,7 @@ int validate_kv4_decode(const ris_decode_desc* d) {
     if (d->max_len < 1 || d->max_len > (1ll << 31)) return RIS_E_ARG;
     if (d->anchor_stride < 0 || d->anchor_stride > (1ll << 40)) return RIS_E_ARG;
     if (d->window < 0 || d->sink < 0) return RIS_E_ARG;
-    if (!(d->scale >= 0.0f) || !isfinite(d->scale)) return RIS_E_ARG;
+    if (!(d->scale >= 0.0f) || !isfinite(d->scale * kLog2e)) return RIS_E_ARG;
     if ((int64_t)d->batch * d->Hkv > 65535) return RIS_E_UNSUPPORTED;
     if ((int64_t)d->batch * d->Hq > 0x7FFFFFFFll) return RIS_E_UNSUPPORTED;
     return RIS_OK;
@@ -170,8 +173,8 @@ int ris_prompt_attn(const void* Q, const void* K, const void* V, const int64_t* 
     p.Hq = d.Hq; p.Hkv = d.Hkv; p.G = d.Hq / d.Hkv; p.D = d.D;
     p.batch = d.batch; p.causal = d.causal;
     p.in_bf16 = d.dtype_in == RIS_BF16; p.out_bf16 = d.dtype_out == RIS_BF16;
-    p.c = (d.scale > 0.0f ? d.scale : 1.0f / sqrtf((float)d.D)) * 1.4426950408889634f;
-    p.slack = 8.0f / p.c;
+    p.c = (d.scale > 0.0f ? d.scale : 1.0f / sqrtf((float)d.D)) * kLog2e;
+    p.slack = fminf(8.0f / p.c, FLT_MAX);       // -inf + slack stays -inf
     if (!fits_dispatch(ris::prompt_blocks(p), 256)) return RIS_E_UNSUPPORTED;
     return hip_status(ris::launch_prompt_attn(p, static_cast<hipStream_t>(stream)));
 }

@@ -133,6 +133,17 @@ def test_prompt_scales(dtype, scale, std):
     check(run(serve, q, k, v, bounds([333]), F32, 1, scale), q, k, v, [333], 1, float(np.float32(scale)))
 
 
+@pytest.mark.parametrize("dtype,T", [(BF16, 40), (BF16, 900), (F32, 100)])
+def test_prompt_smallest_scale(dtype, T):
+    """A scale below the normal numbers: every weight is 1 / its row's keys."""
+    serve = need_serve()
+    q, k, v = inputs(2, 1, T, 128, dtype, seed=16)
+    out = run(serve, q, k, v, bounds([T]), F32, 1, 1e-44).double().cpu()
+    mean = v.double().cpu().cumsum(1) / torch.arange(1, T + 1)[:, None]
+    # sums of up to T values below 8 in float32, the quotient
+    assert (out - mean).abs().max() <= 8 * (T + 2) * 2.0**-24
+
+
 def test_prompt_running_maximum_rises_and_falls():
     """Keys whose scores rise over the sequence, fall, and jump far within a tile."""
     serve = need_serve()

@@ -59,6 +59,13 @@ def test_prompt_refusals(serve, bad, code):
     assert serve.lib().ris_prompt_attn(P, P, P, P, P, ctypes.byref(prompt(serve, **bad)), None) == code
 
 
+def test_scales_beyond_the_range_are_refused(serve):
+    """scale * log2 e has to be a float32 number."""
+    L = serve.lib()
+    assert L.ris_prompt_attn(P, P, P, P, P, ctypes.byref(prompt(serve, scale=3e38)), None) == -1
+    assert L.ris_kv4_decode_workspace_bytes(ctypes.byref(decode(scale=3e38))) == -1
+
+
 def test_prompt_null_and_unaligned(serve):
     L, d = serve.lib(), prompt(serve)
     assert L.ris_prompt_attn(P, P, P, P, P, None, None) == -1
