@@ -25,7 +25,9 @@
 // tokens); at D = 64, where exponentials take longer than products, three waves a
 // SIMD without that gain more (975 against 937).  Not kept: row sums on v_dot2 (the
 // same), the next maximum carried along (the same), raised priority in the PV product
-// (-6%), waits placed by hand around loads in assembly (the same).
+// (-6%), waits placed by hand (the same), 64 rows a wave with each LDS fragment in two
+// products (996 against 949 at D = 64 in a kernel of its own; 680 against 1101 at D =
+// 128: one wave a SIMD, scores copied out of accumulation registers).
 #include <type_traits>
 
 #include "packed.h"
@@ -543,7 +545,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_narrow(PromptParams p
 // keep the chip busy on short prompts), 32 keys to a tile.  The score product takes
 // four dims of a key from one 16-byte read (lane half lh: dims 8 s + 4 lh ..), the PV
 // product score register i as it stands (its two contraction slots are the keys of
-// the lane halves).  16-byte chunk c of row r lies in place c ^ (r % 16).
+// the lane halves).  16-byte chunk c of row r lies in place c ^ (r % 16).  Bound by the
+// matrix unit on many rows (111 of a large product's 154 TFLOP/s for 32 heads of 5,000
+// tokens), by the unequal lengths of few workgroups on less (71 for 4 heads).
 constexpr int kKeys32 = 32;
 
 template <int D>

@@ -174,8 +174,9 @@ class PrefillModel:
 
         cu_seqlens: device int64 offsets [batch + 1].  rope_desc: as in ``prefill``,
         with the factor given for linear and YaRN.  cache: a ``kv4_cache`` of as
-        many sequences, which receives the prompts' keys and values.  Rows of
-        tokens outside every prompt hold nothing of use.
+        many sequences, which receives the prompts' keys and values (those of tokens
+        from its max_len on are left out).  Rows of tokens outside every prompt hold
+        nothing of use.
         """
         cfg = self.cfg
         T, D, Hq = ids.shape[0], cfg.head_dim, cfg.heads
@@ -198,7 +199,8 @@ class PrefillModel:
     def decode_step(self, ids, pos, cache, rope_desc=None, anchors=None, window=None, sink=0):
         """Final hidden states [batch, hidden] of one new token a sequence: ids
         [batch] at positions pos [batch] (device int64), whose keys and values join
-        the cache before the step attends to it.
+        the cache before the step attends to it; a sequence at max_len or beyond has no
+        place there, and its state is of no use.
 
         window None attends to every token of the cache.  anchors: per layer the
         (anchor_ptr, anchor_idx) that ``ris.mask_build_rows`` wrote for the sequences
