@@ -348,17 +348,18 @@ __global__ __launch_bounds__(64 * kWaves * S, D == 64 ? 3 : 2) void k_prompt_bf1
 }
 
 // The states of a workgroup's four waves, each over its own keys of the same 32 rows,
-// to the rows' outputs.  mem: room for [wave][dim block][register][lane].  A wave
+// to the rows' outputs.  mem: room for [wave][dim block][register][lane], a wave's in its
+// K tile's place; ml: 128 floats a wave, kTile apart, in its V tile's place.  A wave
 // stores the dims of four registers of every 16 (8 of a row's 32).
-template <int D>
-__device__ __forceinline__ void join_waves(const PromptParams& p, float* mem, float m, float l, const f32x16_t (&o)[D / 32],
+template <int D, int kTile>
+__device__ __forceinline__ void join_waves(const PromptParams& p, float* mem, float* ml, float m, float l, const f32x16_t (&o)[D / 32],
                                            const RowTile& t, int row, int h) {
     constexpr int DB = D / 32;
-    __shared__ float ml[kWaves][2][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lh = lane >> 5;
-    ml[wave][0][lane] = m;
-    ml[wave][1][lane] = pair_sum32(l);
     mem += lane;
+    ml += lane;
+    ml[wave * kTile] = m;
+    ml[wave * kTile + 64] = pair_sum32(l);
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -367,13 +368,13 @@ __device__ __forceinline__ void join_waves(const PromptParams& p, float* mem, fl
     if (row >= t.len) return;
     float big = -INFINITY, a[kWaves], sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) big = fmaxf(big, ml[w][0][lane]);
+    for (int w = 0; w < kWaves; ++w) big = fmaxf(big, ml[w * kTile]);
     const float c = big == -INFINITY ? 0.f : big * p.c;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-        const float mw = ml[w][0][lane];
+        const float mw = ml[w * kTile];
         a[w] = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw * p.c - c);
-        sum += a[w] * ml[w][1][lane];
+        sum += a[w] * ml[w * kTile + 64];
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     const int64_t at = h * p.o_head + (t.first + row) * p.o_token + 4 * lh + 8 * wave;
@@ -390,16 +391,35 @@ __device__ __forceinline__ void join_waves(const PromptParams& p, float* mem, fl
     }
 }
 
+// Whether any lane of the workgroup's waves says so; mem as join_waves' ml.  (The
+// library's vote has a shared array of its own, beside which the compiler cannot tell
+// K and V tiles apart.)
+template <int kTile>
+__device__ __forceinline__ bool any_wave(bool x, float* mem) {
+    const bool any = __any(x);
+    if ((threadIdx.x & 63) == 0) mem[(threadIdx.x >> 6) * kTile + 128] = any ? 1.f : 0.f;
+    __syncthreads();
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) sum += mem[w * kTile + 128];
+    return sum > 0.f;
+}
+
 // The same for batches too small to fill the chip with 128-row workgroups: a
 // workgroup takes 32 rows, and its four waves every fourth tile of keys each, in
 // places of their own (one K and one V tile a wave, no barrier: the next K tile is
 // loaded once the scores have read this one, the next V tile once the output has).
 // The waves' states meet at the end, each wave taking a quarter of the output.
+//
+// The compiler waits for every load before a read of LDS that one of them may write,
+// unless it can tell them apart: hence no load under a condition in the loop, tiles that
+// are restrict parameters, and one shared array in the kernel (two have marks of their
+// own, which these replace).  4 to 10% for one prompt of 1,500 to 3,000 tokens.
 template <int D>
 __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_narrow(PromptParams p) {
     constexpr int SL = D / 16, DB = D / 32, C = D / 8;
     constexpr int kPieces = kKeys * C / 64, kPer = 64 / C;        // 16-byte pieces of a lane, rows of a piece
-    __shared__ __align__(16) uint16_t ks[kWaves * kKeys * D], vs[kWaves * kKeys * D];
+    __shared__ __align__(16) uint16_t lds[2 * kWaves * kKeys * D];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int lq = lane & 31, lh = lane >> 5;
     const uint32_t xcd = blockIdx.x & 7u, slot = blockIdx.x >> 3;
@@ -410,8 +430,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_narrow(PromptParams p
     const int n = t.len, q0 = t.tile * kNarrowRows, row = q0 + lq;
     const uint16_t* K = static_cast<const uint16_t*>(p.K) + g * p.k_head + t.first * p.k_token;
     const uint16_t* V = static_cast<const uint16_t*>(p.V) + g * p.v_head + t.first * p.v_token;
-    uint16_t* const kl = ks + wave * kKeys * D;
-    uint16_t* const vl = vs + wave * kKeys * D;
+    uint16_t* const kl = lds + wave * kKeys * D;
+    uint16_t* const vl = kl + kWaves * kKeys * D;
 
     const auto load = [&](const uint16_t* x, int64_t tok, int j0, uint16_t* to) __attribute__((always_inline)) {
         const char* from = reinterpret_cast<const char*>(x + j0 * tok);
@@ -438,19 +458,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_narrow(PromptParams p
     float m, mc, l;
     const int r0 = 4 * lh + ((lane & 15) >> 2), cq = 2 * (lane >> 4 & 1) + ((lane & 3) >> 1);
     // kSafe: V may hold infinities or NaN under the mask
-    const auto pass = [&](auto safe) __attribute__((always_inline)) {
+    const auto pass = [&](auto safe, uint16_t* __restrict__ kt, uint16_t* __restrict__ vt) __attribute__((always_inline)) {
         constexpr bool kSafe = decltype(safe)::value;
-        if (wave < tiles) {
-            load(K, p.k_token, wave * kKeys, kl);
-            load(V, p.v_token, wave * kKeys, vl);
-        }
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
         m = -INFINITY;
         mc = l = 0.f;
-        for (int it = wave; it < tiles; it += kWaves) {
+        // kMore: the wave has a tile after this one
+        const auto step = [&](auto more, int it) __attribute__((always_inline)) {
+            constexpr bool kMore = decltype(more)::value;
             const int j0 = it * kKeys, jn = j0 + kWaves * kKeys;
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kPieces) : "memory");       // K; V may still be on its way
             f32x16_t st[2];
@@ -460,7 +478,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_narrow(PromptParams p
                 for (int i = 0; i < 16; ++i) st[b][i] = 0.f;
 #pragma unroll
                 for (int s = 0; s < SL; ++s) {
-                    const u32x4_t a = *reinterpret_cast<const u32x4_t*>(kl + (32 * b + lq) * D + 8 * ((2 * s + lh) ^ swizzle<D>(lq)));
+                    const u32x4_t a = *reinterpret_cast<const u32x4_t*>(kt + (32 * b + lq) * D + 8 * ((2 * s + lh) ^ swizzle<D>(lq)));
                     st[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(qf[s]), st[b], 0, 0, 0);
                 }
             }
@@ -478,7 +496,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_narrow(PromptParams p
                 for (int i = 0; i < 16; ++i) mx = fmaxf(mx, st[b][i]);
             mx = pair_max32(mx);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // every read of K has returned
-            if (jn < kend) load(K, p.k_token, jn, kl);
+            if constexpr (kMore) load(K, p.k_token, jn, kt);
             if (__any(mx > m + p.slack)) {
                 const bool none = m == -INFINITY;
                 m = fmaxf(m, mx);
@@ -501,15 +519,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_narrow(PromptParams p
                     l += x + y;
                     pf[2 * b + i / 8][i % 8 / 2] = pack_bf16x2(x, y);
                 }
-            if (jn < kend) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kPieces) : "memory");      // V; not the next K
-            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kMore ? kPieces : 0) : "memory");      // V; not the next K
 #pragma unroll
             for (int u = 0; u < 4; ++u)
 #pragma unroll
                 for (int d = 0; d < DB; ++d) {
                     const int c = 4 * d + cq;
-                    const uint2 a = lds_read_tr16(vl + (16 * u + r0) * D + 8 * (c ^ swizzle<D>(r0)) + 4 * (lane & 1));
-                    const uint2 b = lds_read_tr16(vl + (16 * u + r0 + 8) * D + 8 * (c ^ swizzle<D>(r0 + 8)) + 4 * (lane & 1));
+                    const uint2 a = lds_read_tr16(vt + (16 * u + r0) * D + 8 * (c ^ swizzle<D>(r0)) + 4 * (lane & 1));
+                    const uint2 b = lds_read_tr16(vt + (16 * u + r0 + 8) * D + 8 * (c ^ swizzle<D>(r0 + 8)) + 4 * (lane & 1));
                     u32x4_t v = {a.x, a.y, b.x, b.y};
                     if constexpr (kSafe) {
 #pragma unroll
@@ -523,21 +540,30 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_narrow(PromptParams p
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             const int dim = 32 * d + 8 * (i / 4) + 4 * lh + i % 4;
-                            const uint16_t v = vl[r * D + 8 * ((dim >> 3) ^ swizzle<D>(r)) + (dim & 7)];
+                            const uint16_t v = vt[r * D + 8 * ((dim >> 3) ^ swizzle<D>(r)) + (dim & 7)];
                             if (odd_half(v) && j0 + r <= last) o[d][i] += bf16_to_f32(v);
                         }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // every read of V has returned
-            if (jn < kend) load(V, p.v_token, jn, vl);
-        }
+            if constexpr (kMore) load(V, p.v_token, jn, vt);
+        };
+        if (wave >= tiles) return;
+        load(K, p.k_token, wave * kKeys, kt);
+        load(V, p.v_token, wave * kKeys, vt);
+        int it = wave;
+        for (; it + kWaves < tiles; it += kWaves) step(std::true_type{}, it);
+        step(std::false_type{}, it);
     };
-    pass(std::false_type{});
+    pass(std::false_type{}, kl, vl);
     float odd = 0.f;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) odd = fmaf(o[d][i], 0.f, odd);
-    if (__syncthreads_or(odd != odd && row < n)) pass(std::true_type{});
-    join_waves<D>(p, reinterpret_cast<float*>(ks), m, l, o, t, row, h);
+    if (any_wave<kKeys * D / 2>(odd != odd && row < n, reinterpret_cast<float*>(lds + kWaves * kKeys * D))) {
+        __syncthreads();
+        pass(std::true_type{}, kl, vl);
+    }
+    join_waves<D, kKeys * D / 2>(p, reinterpret_cast<float*>(lds), reinterpret_cast<float*>(lds + kWaves * kKeys * D), m, l, o, t, row, h);
 }
 
 // float32: the narrow form's plan and the same layouts on v_mfma_f32_32x32x2_f32 (16
@@ -554,7 +580,7 @@ template <int D>
 __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_f32(PromptParams p) {
     constexpr int DB = D / 32, C = D / 4;
     constexpr int kPieces = kKeys32 * C / 64, kPer = 64 / C;
-    __shared__ __align__(16) float ks[kWaves * kKeys32 * D], vs[kWaves * kKeys32 * D];
+    __shared__ __align__(16) float lds[2 * kWaves * kKeys32 * D];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int lq = lane & 31, lh = lane >> 5;
     const uint32_t xcd = blockIdx.x & 7u, slot = blockIdx.x >> 3;
@@ -565,8 +591,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_f32(PromptParams p) {
     const int n = t.len, q0 = t.tile * kNarrowRows, row = q0 + lq;
     const float* K = static_cast<const float*>(p.K) + g * p.k_head + t.first * p.k_token;
     const float* V = static_cast<const float*>(p.V) + g * p.v_head + t.first * p.v_token;
-    float* const kl = ks + wave * kKeys32 * D;
-    float* const vl = vs + wave * kKeys32 * D;
+    float* const kl = lds + wave * kKeys32 * D;
+    float* const vl = kl + kWaves * kKeys32 * D;
 
     const auto load = [&](const float* x, int64_t tok, int j0, float* to) __attribute__((always_inline)) {
         const char* from = reinterpret_cast<const char*>(x + j0 * tok);
@@ -592,19 +618,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_f32(PromptParams p) {
     f32x16_t o[DB];
     float m, mc, l;
     // kSafe: V may hold infinities or NaN under the mask
-    const auto pass = [&](auto safe) __attribute__((always_inline)) {
+    const auto pass = [&](auto safe, float* __restrict__ kt, float* __restrict__ vt) __attribute__((always_inline)) {
         constexpr bool kSafe = decltype(safe)::value;
-        if (wave < tiles) {
-            load(K, p.k_token, wave * kKeys32, kl);
-            load(V, p.v_token, wave * kKeys32, vl);
-        }
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
         m = -INFINITY;
         mc = l = 0.f;
-        for (int it = wave; it < tiles; it += kWaves) {
+        // kMore: the wave has a tile after this one
+        const auto step = [&](auto more, int it) __attribute__((always_inline)) {
+            constexpr bool kMore = decltype(more)::value;
             const int j0 = it * kKeys32, jn = j0 + kWaves * kKeys32;
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kPieces) : "memory");       // K; V may still be on its way
             f32x16_t st;
@@ -612,7 +636,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_f32(PromptParams p) {
             for (int i = 0; i < 16; ++i) st[i] = 0.f;
 #pragma unroll
             for (int s = 0; s < D / 8; ++s) {
-                const f32x4_t a = *reinterpret_cast<const f32x4_t*>(kl + lq * D + 4 * ((2 * s + lh) ^ (lq & 15)));
+                const f32x4_t a = *reinterpret_cast<const f32x4_t*>(kt + lq * D + 4 * ((2 * s + lh) ^ (lq & 15)));
 #pragma unroll
                 for (int e = 0; e < 4; ++e) st = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], qf[s][e], st, 0, 0, 0);
             }
@@ -626,7 +650,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_f32(PromptParams p) {
             for (int i = 0; i < 16; ++i) mx = fmaxf(mx, st[i]);
             mx = pair_max32(mx);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // every read of K has returned
-            if (jn < kend) load(K, p.k_token, jn, kl);
+            if constexpr (kMore) load(K, p.k_token, jn, kt);
             if (__any(mx > m + p.slack)) {
                 const bool none = m == -INFINITY;
                 m = fmaxf(m, mx);
@@ -644,14 +668,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_f32(PromptParams p) {
                 st[i] = __builtin_amdgcn_exp2f(fmaf(st[i], p.c, -mc));
                 l += st[i];
             }
-            if (jn < kend) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kPieces) : "memory");      // V; not the next K
-            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kMore ? kPieces : 0) : "memory");      // V; not the next K
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int r = 8 * (i / 4) + 4 * lh + i % 4;
 #pragma unroll
                 for (int d = 0; d < DB; ++d) {
-                    float v = vl[r * D + 4 * ((8 * d + lq / 4) ^ (r & 15)) + lq % 4];
+                    float v = vt[r * D + 4 * ((8 * d + lq / 4) ^ (r & 15)) + lq % 4];
                     if (kSafe && !isfinite(v)) v = 0.f;
                     o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, st[i], o[d], 0, 0, 0);
                 }
@@ -662,21 +685,30 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_f32(PromptParams p) {
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             const int dim = 32 * d + 8 * (i / 4) + 4 * lh + i % 4;
-                            const float v = vl[r * D + 4 * (dim / 4 ^ (r & 15)) + dim % 4];
+                            const float v = vt[r * D + 4 * (dim / 4 ^ (r & 15)) + dim % 4];
                             if (!isfinite(v) && j0 + r <= last) o[d][i] += v;
                         }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // every read of V has returned
-            if (jn < kend) load(V, p.v_token, jn, vl);
-        }
+            if constexpr (kMore) load(V, p.v_token, jn, vt);
+        };
+        if (wave >= tiles) return;
+        load(K, p.k_token, wave * kKeys32, kt);
+        load(V, p.v_token, wave * kKeys32, vt);
+        int it = wave;
+        for (; it + kWaves < tiles; it += kWaves) step(std::true_type{}, it);
+        step(std::false_type{}, it);
     };
-    pass(std::false_type{});
+    pass(std::false_type{}, kl, vl);
     float odd = 0.f;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) odd = fmaf(o[d][i], 0.f, odd);
-    if (__syncthreads_or(odd != odd && row < n)) pass(std::true_type{});
-    join_waves<D>(p, ks, m, l, o, t, row, h);       // a wave's state takes its K tile's place
+    if (any_wave<kKeys32 * D>(odd != odd && row < n, lds + kWaves * kKeys32 * D)) {
+        __syncthreads();
+        pass(std::true_type{}, kl, vl);
+    }
+    join_waves<D, kKeys32 * D>(p, lds, lds + kWaves * kKeys32 * D, m, l, o, t, row, h);
 }
 
 // Workgroups of a launch whose row tiles hold `rows`.
