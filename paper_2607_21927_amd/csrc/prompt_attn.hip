@@ -40,6 +40,7 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr int kRows = 128;        // query rows of a workgroup
 constexpr int kNarrowRows = 32;   // of the narrow form's
+constexpr int kShortRows = 32;    // of a wave of the short form
 constexpr int kKeys = 64;         // keys of a tile
 constexpr int kWaves = 4;
 
@@ -566,6 +567,167 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_narrow(PromptParams p
     join_waves<D, kKeys * D / 2>(p, reinterpret_cast<float*>(lds), reinterpret_cast<float*>(lds + kWaves * kKeys * D), m, l, o, t, row, h);
 }
 
+// The same for many prompts of a few tokens: a tile is 32 neighbouring tokens, of as
+// many prompts as they belong to, and a row's keys are the interval from its prompt's
+// first token on, so that tiles stay full however short prompts are.  A wave takes one
+// tile of one head by itself (heads of a tile side by side on one XCD), 32 keys at a
+// time from its rows' first to their last, K and V as in the narrow form.  10,000 prompts
+// of 8 tokens (12/2 heads of 128) take 199 us, 1.7 times a copy of their bytes.
+constexpr int kShortKeys = 32;
+
+template <int D>
+__global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_short(PromptParams p) {
+    constexpr int SL = D / 16, DB = D / 32, C = D / 8;
+    constexpr int kPieces = kShortKeys * C / 64, kPer = 64 / C;
+    __shared__ __align__(16) uint16_t lds[2 * kWaves * kShortKeys * D];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lq = lane & 31, lh = lane >> 5;
+    const uint32_t unit = (blockIdx.x >> 3) * kWaves + wave, tile = unit / p.Hq * 8u + (blockIdx.x & 7u);
+    const int h = (int)(unit % p.Hq), g = h / p.G;
+    const int64_t first = (int64_t)tile * kShortRows;
+    if (first >= p.T) return;
+    const int t = (int)first + lq;                     // the lane's row
+    int b = find_seq(p.cu, p.batch, first);
+    if (b < 0) b = 0;
+    while (b < p.batch && p.cu[b + 1] <= t) ++b;
+    const bool in = t < p.T && b < p.batch && p.cu[b] <= t;
+    const int lo = in ? clip_offset(p.cu[b], p.T) : (int)p.T;
+    const int hi = !in ? -1 : p.causal ? t : clip_offset(p.cu[b + 1], p.T) - 1;
+    int from = lo, to = hi;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        from = min(from, __shfl_xor(from, d));
+        to = max(to, __shfl_xor(to, d));
+    }
+    from = __builtin_amdgcn_readfirstlane(from);
+    to = __builtin_amdgcn_readfirstlane(to);
+    if (to < 0) return;                                // no row has a prompt
+    const uint16_t* K = static_cast<const uint16_t*>(p.K) + g * p.k_head;
+    const uint16_t* V = static_cast<const uint16_t*>(p.V) + g * p.v_head;
+    uint16_t* const kl = lds + wave * kShortKeys * D;
+    uint16_t* const vl = kl + kWaves * kShortKeys * D;
+
+    const auto load = [&](const uint16_t* x, int64_t tok, int j0, uint16_t* place) __attribute__((always_inline)) {
+        const char* at = reinterpret_cast<const char*>(x + j0 * tok);
+        const uint32_t step = 2u * (uint32_t)tok;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int r = kPer * i + lane / C, rr = r < to - j0 ? r : to - j0;
+            __builtin_amdgcn_global_load_lds((gptr_t)(at + (uint32_t)(rr * step + 16 * (lane % C ^ swizzle<D>(r)))),
+                                             (lptr_t)(place + 64 * 8 * i), 16, 0, 0);
+        }
+    };
+    u32x4_t qf[SL];
+    {
+        const uint16_t* qp = static_cast<const uint16_t*>(p.Q) + h * p.q_head + (in ? t : (int)first) * p.q_token + 8 * lh;
+#pragma unroll
+        for (int s = 0; s < SL; ++s) qf[s] = *reinterpret_cast<const u32x4_t*>(qp + 16 * s);
+    }
+    f32x16_t o[DB];
+    float m, mc, l;
+    const int r0 = 4 * lh + ((lane & 15) >> 2), cq = 2 * (lane >> 4 & 1) + ((lane & 3) >> 1);
+    // kSafe: V may hold infinities or NaN under the mask
+    const auto pass = [&](auto safe, uint16_t* __restrict__ kt, uint16_t* __restrict__ vt) __attribute__((always_inline)) {
+        constexpr bool kSafe = decltype(safe)::value;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+        m = -INFINITY;
+        mc = l = 0.f;
+        // kMore: there are keys after this tile's
+        const auto step = [&](auto more, int j0) __attribute__((always_inline)) {
+            constexpr bool kMore = decltype(more)::value;
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kPieces) : "memory");       // K; V may still be on its way
+            f32x16_t st;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) st[i] = 0.f;
+#pragma unroll
+            for (int s = 0; s < SL; ++s) {
+                const u32x4_t a = *reinterpret_cast<const u32x4_t*>(kt + lq * D + 8 * ((2 * s + lh) ^ swizzle<D>(lq)));
+                st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(qf[s]), st, 0, 0, 0);
+            }
+            float mx = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int j = j0 + 8 * (i / 4) + 4 * lh + i % 4;
+                if (j < lo || j > hi) st[i] = -INFINITY;
+                mx = fmaxf(mx, st[i]);
+            }
+            mx = pair_max32(mx);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // every read of K has returned
+            if constexpr (kMore) load(K, p.k_token, j0 + kShortKeys, kt);
+            if (__any(mx > m + p.slack)) {
+                const bool none = m == -INFINITY;
+                m = fmaxf(m, mx);
+                const float nc = m == -INFINITY ? 0.f : m * p.c;
+                const float al = none ? 0.f : __builtin_amdgcn_exp2f(mc - nc);
+                mc = nc;
+                l *= al;
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[d][i] *= al;
+            }
+            u32x4_t pf[2];
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                const float x = __builtin_amdgcn_exp2f(fmaf(st[i], p.c, -mc));
+                const float y = __builtin_amdgcn_exp2f(fmaf(st[i + 1], p.c, -mc));
+                l += x + y;
+                pf[i / 8][i % 8 / 2] = pack_bf16x2(x, y);
+            }
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kMore ? kPieces : 0) : "memory");      // V; not the next K
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                    const int c = 4 * d + cq;
+                    const uint2 a = lds_read_tr16(vt + (16 * u + r0) * D + 8 * (c ^ swizzle<D>(r0)) + 4 * (lane & 1));
+                    const uint2 e = lds_read_tr16(vt + (16 * u + r0 + 8) * D + 8 * (c ^ swizzle<D>(r0 + 8)) + 4 * (lane & 1));
+                    u32x4_t v = {a.x, a.y, e.x, e.y};
+                    if constexpr (kSafe) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v[i] = finite_only(v[i]);
+                    }
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v), as_bf16x8(pf[u]), o[d], 0, 0, 0);
+                }
+            for (int r = 0; kSafe && r < kShortKeys; ++r)
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int dim = 32 * d + 8 * (i / 4) + 4 * lh + i % 4;
+                        const uint16_t v = vt[r * D + 8 * ((dim >> 3) ^ swizzle<D>(r)) + (dim & 7)];
+                        if (odd_half(v) && j0 + r >= lo && j0 + r <= hi) o[d][i] += bf16_to_f32(v);
+                    }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // every read of V has returned
+            if constexpr (kMore) load(V, p.v_token, j0 + kShortKeys, vt);
+        };
+        load(K, p.k_token, from, kt);
+        load(V, p.v_token, from, vt);
+        int j0 = from;
+        for (; j0 <= to - kShortKeys; j0 += kShortKeys) step(std::true_type{}, j0);
+        step(std::false_type{}, j0);
+    };
+    pass(std::false_type{}, kl, vl);
+    float odd = 0.f;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) odd = fmaf(o[d][i], 0.f, odd);
+    if (__any(odd != odd && in)) pass(std::true_type{}, kl, vl);
+    l = pair_sum32(l);
+    if (!in) return;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int64_t at = h * p.o_head + t * p.o_token + 4 * lh;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            store4(p, at + 32 * d + 8 * i, o[d][4 * i] * inv, o[d][4 * i + 1] * inv, o[d][4 * i + 2] * inv, o[d][4 * i + 3] * inv);
+}
+
 // float32: the narrow form's plan and the same layouts on v_mfma_f32_32x32x2_f32 (16
 // times slower than bf16's: it hides everything else, and so few rows to a workgroup
 // keep the chip busy on short prompts), 32 keys to a tile.  The score product takes
@@ -727,14 +889,31 @@ bool narrow(const PromptParams& p) { return p.T > (int64_t)p.batch * kKeys && bl
 // 86, of 8,192 (768 workgroups) 226 against 209; eight of 512 25 against 20.
 bool split(const PromptParams& p) { return p.T >= (int64_t)p.batch * 512 && blocks_of(p, kRows) <= 440; }
 
+// The short form for prompts of a tile of keys or less in the mean that are more than the
+// 128-row form's workgroups resident at once.  12/2 heads of 128: 64 prompts of 30 tokens
+// 9.6 against 14.0 us, 500 of 20 27 against 65, of 64 73 against 100, 10,000 of 8 199
+// against 1225; 32/4 heads of 64: 32 of 20 6.5 against 10.5, 500 of 20 32 against 92.
+// Fewer: 32 of 20 (12/2 heads, 384 workgroups) 8.2 against 7.4; longer: 32 of 100 16.8
+// against 13.3.  A long prompt among them costs (one of 10,000 and 499 of 20: 520 against
+// 363), which the host does not see.
+bool brief(const PromptParams& p) { return p.batch > 1 && p.T <= (int64_t)p.batch * kKeys && blocks_of(p, kRows) > 512; }
+int64_t brief_blocks(const PromptParams& p) {
+    const int64_t tiles = ((p.T + kShortRows - 1) / kShortRows + 7) / 8;       // of an XCD
+    return (tiles * p.Hq + kWaves - 1) / kWaves * 8;
+}
+
 }  // namespace
 
-int64_t prompt_blocks(const PromptParams& p) { return blocks_of(p, p.in_bf16 && !narrow(p) ? kRows : kNarrowRows); }
+int64_t prompt_blocks(const PromptParams& p) {
+    if (!p.in_bf16) return blocks_of(p, kNarrowRows);
+    return brief(p) ? brief_blocks(p) : blocks_of(p, narrow(p) ? kNarrowRows : kRows);
+}
 
 hipError_t launch_prompt_attn(const PromptParams& p, hipStream_t st) {
     const dim3 grid((unsigned)prompt_blocks(p));
     const auto run = [&](auto kernel, int waves) { hipLaunchKernelGGL(kernel, grid, dim3(64 * waves), 0, st, p); };
     if (!p.in_bf16) p.D == 128 ? run(k_prompt_f32<128>, kWaves) : run(k_prompt_f32<64>, kWaves);
+    else if (brief(p)) p.D == 128 ? run(k_prompt_short<128>, kWaves) : run(k_prompt_short<64>, kWaves);
     else if (narrow(p)) p.D == 128 ? run(k_prompt_narrow<128>, kWaves) : run(k_prompt_narrow<64>, kWaves);
     else if (split(p)) p.D == 128 ? run(k_prompt_bf16<128, 2>, 2 * kWaves) : run(k_prompt_bf16<64, 2>, 2 * kWaves);
     else p.D == 128 ? run(k_prompt_bf16<128, 1>, kWaves) : run(k_prompt_bf16<64, 1>, kWaves);

@@ -190,6 +190,53 @@ def test_prompt_many_sequences(B, dtype):
     assert (np.abs(got.double().cpu().numpy() - want) <= attn_bar(q, k, v, 150, 0.125, want, dtype, F32)).all()
 
 
+@pytest.mark.parametrize("Hq,Hkv,D,causal,out_dtype", [(8, 2, 64, 1, BF16), (8, 1, 128, 1, F32), (6, 6, 128, 0, BF16),
+                                                       (24, 4, 64, 0, F32)])
+def test_prompt_many_short_prompts(Hq, Hkv, D, causal, out_dtype):
+    """Tiles that hold tokens of many prompts; views of a projection; tokens of no
+    prompt before and behind them."""
+    serve = need_serve()
+    rng = np.random.default_rng(D + Hq)
+    lens = [int(x) for x in rng.choice([0, 1, 2, 5, 17, 31, 32, 33, 40, 70, 130], 110)]
+    T = sum(lens) + 8
+    q, k, v = inputs(Hq, Hkv, T, D, BF16, seed=19)
+    qkv = torch.cat([x.transpose(0, 1).reshape(T, -1) for x in (q, k, v)], 1)
+    views = [head_view(qkv, a, n, D) for a, n in ((0, Hq), (Hq, Hkv), (Hq + Hkv, Hkv))]
+    out = head_view(torch.full((T, Hq * D), 7.0, dtype=out_dtype, device="cuda"), 0, Hq, D)
+    run(serve, *views, bounds(lens) + 3, causal=causal, out=out)
+    assert (out[:, :3] == 7).all() and (out[:, T - 5:] == 7).all()
+    check(out, q, k, v, lens, causal, D**-0.5, first=3)
+
+
+@pytest.mark.parametrize("long", [100, 3000])
+def test_prompt_a_long_one_among_short_ones(long):
+    serve = need_serve()
+    lens = [20] * 40 + [long] + [20] * 60
+    q, k, v = inputs(8, 2, sum(lens), 64, BF16, seed=20)
+    check(run(serve, q, k, v, bounds(lens), F32), q, k, v, lens, 1, 0.125)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_short_prompts_do_not_reach_each_other(D):
+    """Infinities and NaN in the neighbours of a tile; replays of a captured call."""
+    serve = need_serve()
+    lens, Hq, Hkv = [20] * 100, 8, 2
+    cu = bounds(lens)
+    q, k, v = inputs(Hq, Hkv, 2000, D, BF16, seed=21)
+    clean = run(serve, q, k, v, cu)
+    kb, vb = k.clone(), v.clone()
+    kb[:, 1015:1020], vb[:, 1015:1020] = float("nan"), float("inf")       # the end of prompt 50
+    vb[:, 1203, 3], vb[:, 1206, 3] = float("inf"), float("nan")           # an element in prompt 60
+    got = run(serve, q, kb, vb, cu)
+    bad = torch.zeros(2000, dtype=torch.bool)
+    bad[1015:1020] = True
+    assert got[:, 1015:1020].isnan().all()
+    assert (got[:, 1203:1206, 3] == float("inf")).all() and got[:, 1206:1220, 3].isnan().all()
+    got[:, 1203:1220, 3] = clean[:, 1203:1220, 3]
+    assert torch.equal(got[:, ~bad], clean[:, ~bad])
+    replay_checked(lambda: run(serve, q, k, v, cu, out=got), [got], lambda i: q.mul_(-1.25))
+
+
 def test_prompt_offsets_beyond_32_bits():
     """Rows whose byte and element offsets pass 2^32 and 2^31."""
     serve = need_serve()
