@@ -72,8 +72,7 @@ __device__ __forceinline__ void load8(const void* p, int64_t at, float* x) {
 __device__ __forceinline__ int64_t cache_row(const Kv4Params& p, int64_t first, int64_t t, int h) {
     if (first >= p.T) return -1;
     int b = find_seq(p.cu, p.batch, first);
-    if (b < 0) b = 0;
-    while (b < p.batch && p.cu[b + 1] <= t) ++b;
+    b = seq_from(p.cu, p.batch, b < 0 ? 0 : b, t);
     if (t >= p.T || b >= p.batch || t < p.cu[b]) return -1;
     const int64_t from = p.cu[b] > 0 ? p.cu[b] : 0;            // clipped
     const int64_t pos = (int64_t)((uint64_t)(t - from) + (uint64_t)(p.start ? p.start[b] : 0));

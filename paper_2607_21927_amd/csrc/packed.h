@@ -99,4 +99,17 @@ __device__ __forceinline__ int find_seq(const int64_t* cu, int batch, int64_t t)
     return lo + __popcll(__ballot(lane < n && cu[lo + lane] <= t)) - 1;
 }
 
+// The same for a lane's token t from a sequence b at or before its own: one step where
+// that is b, some 2 log2 of the distance otherwise (thousands of empty sequences).
+__device__ __forceinline__ int seq_from(const int64_t* cu, int batch, int b, int64_t t) {
+    int step = 1;
+    while (b + step <= batch && cu[b + step] <= t) {
+        b += step;
+        step *= 2;
+    }
+    for (step >>= 1; step > 0; step >>= 1)
+        if (b + step <= batch && cu[b + step] <= t) b += step;
+    return b;
+}
+
 }  // namespace ris

@@ -588,8 +588,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_short(PromptParams p)
     if (first >= p.T) return;
     const int t = (int)first + lq;                     // the lane's row
     int b = find_seq(p.cu, p.batch, first);
-    if (b < 0) b = 0;
-    while (b < p.batch && p.cu[b + 1] <= t) ++b;
+    b = seq_from(p.cu, p.batch, b < 0 ? 0 : b, t);
     const bool in = t < p.T && b < p.batch && p.cu[b] <= t;
     const int lo = in ? clip_offset(p.cu[b], p.T) : (int)p.T;
     const int hi = !in ? -1 : p.causal ? t : clip_offset(p.cu[b + 1], p.T) - 1;
@@ -601,7 +600,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_short(PromptParams p)
     }
     from = __builtin_amdgcn_readfirstlane(from);
     to = __builtin_amdgcn_readfirstlane(to);
-    if (to < 0) return;                                // no row has a prompt
+    if (to < from) return;                             // no row has a prompt
     const uint16_t* K = static_cast<const uint16_t*>(p.K) + g * p.k_head;
     const uint16_t* V = static_cast<const uint16_t*>(p.V) + g * p.v_head;
     uint16_t* const kl = lds + wave * kShortKeys * D;

@@ -131,8 +131,7 @@ __global__ __launch_bounds__(kThreads) void k_rope_packed(const void* src, int64
     const int64_t first = (gid - (threadIdx.x & 63)) / lanes;     // of the wave's tokens
     if (first >= T) return;
     int b = find_seq(cu, batch, first);
-    if (b < 0) b = 0;
-    while (b < batch && cu[b + 1] <= t) ++b;
+    b = seq_from(cu, batch, b < 0 ? 0 : b, t);
     if (t >= T || b >= batch || t < cu[b]) return;
     const int64_t from = cu[b] > 0 ? cu[b] : 0;                   // clipped
     const double pos = (double)(t - from + (start ? start[b] : 0));

@@ -324,6 +324,24 @@ def test_rope_packed_positions_count_from_the_clipped_offset():
     assert torch.equal(got, serve.rope_packed(x, torch.empty_like(x), bounds([20, 30]), desc))
 
 
+def test_thousands_of_empty_sequences_between_others():
+    """Rotation, attention and the cache pass them over, inside a wave's tokens too."""
+    serve = need_serve()
+    from paper_2607_21927_amd import ris
+    lens, few = [20] + [0] * 5000 + [7] + [0] * 777 + [3, 30], [20, 7, 3, 30]
+    q, k, v = inputs(4, 2, 60, 64, BF16, seed=22)
+    desc = ris.rope_desc(ris.ROPE_PLAIN, 1e4)
+    start = torch.zeros(len(lens), dtype=torch.int64, device="cuda")
+    got = serve.rope_packed(q, torch.empty_like(q), bounds(lens), desc, start=start)
+    assert torch.equal(got, serve.rope_packed(q, torch.empty_like(q), bounds(few), desc))
+    check(run(serve, q, k, v, bounds(lens), F32), q, k, v, few, 1, 0.125)
+    cache, small = serve.kv4_cache(len(lens), 2, 30, 64), serve.kv4_cache(4, 2, 30, 64)
+    serve.kv4_store(k, v, bounds(lens), *cache)
+    serve.kv4_store(k, v, bounds(few), *small)
+    for a, b in zip(cache, small):
+        assert torch.equal(a[[0, 5001, 5779, 5780]], b) and a.count_nonzero() == b.count_nonzero()
+
+
 def test_rope_packed_many_sequences_and_graph():
     serve = need_serve()
     from paper_2607_21927_amd import ris
