@@ -9,7 +9,6 @@ import ctypes
 import torch
 
 from . import ris
-from .ris import _dtype_code
 
 MAX_TOP = 64
 KV4_BLOCK = 32          # dimensions that share a scale in the 4-bit cache
@@ -65,6 +64,14 @@ def lib():
     return _lib
 
 
+_CODES = {torch.float32: ris.F32, torch.bfloat16: ris.BF16}
+
+
+def _code(t):
+    code = _CODES.get(t.dtype)
+    return ris._dtype_code(t) if code is None else code         # raises
+
+
 def _one_gpu(t, *others):
     """Index of the GPU that holds all of the tensors."""
     index = t.get_device()
@@ -96,6 +103,16 @@ def _rows(t, shape):
     if one != 1 or (at | (head | token) * t.element_size()) & 15:
         raise ValueError("rows must be contiguous, bases and strides multiples of 16 bytes")
     return at, head, token
+
+
+def _placed(t, shape, strides):
+    """Address of a view that a descriptor has the shape and (head, token, 1) strides of."""
+    if t.shape != shape or t.stride() != strides and _rows(t, shape)[1:] != strides[:2]:
+        raise ValueError(f"shape and strides must match the descriptor, got {tuple(t.shape)}, {t.stride()}")
+    at = t.data_ptr()
+    if at & 15:
+        raise ValueError("bases must be multiples of 16 bytes")
+    return at
 
 
 def _bounds(cu_seqlens, start=None):
@@ -149,7 +166,7 @@ def rope_packed(src, out, cu_seqlens, desc, start=None, stream=None):
     if src.shape != out.shape or one != 1 or src.dtype != out.dtype:
         raise ValueError("src must be a [heads, T, D] view of out's dtype with unit stride along D")
     batch = _bounds(cu_seqlens, start)
-    _call(index, stream, "ris_rope_packed", src.data_ptr(), head, token, out.data_ptr(), _dtype_code(out), H, T, D,
+    _call(index, stream, "ris_rope_packed", src.data_ptr(), head, token, out.data_ptr(), _code(out), H, T, D,
           cu_seqlens.data_ptr(), _at(start), batch, desc)
     return out
 
@@ -157,7 +174,7 @@ def rope_packed(src, out, cu_seqlens, desc, start=None, stream=None):
 def prompt_desc(Q, K, V, out, cu_seqlens, causal=1, scale=0.0):
     """Descriptor from views Q, out [Hq, T, D] and K, V [Hkv, T, D]."""
     Hq, T, D = Q.shape
-    return PromptDesc(_dtype_code(Q), _dtype_code(out), Hq, K.shape[0], D, cu_seqlens.numel() - 1, T, causal, scale,
+    return PromptDesc(_code(Q), _code(out), Hq, K.shape[0], D, cu_seqlens.numel() - 1, T, causal, scale,
                       *_rows(Q, Q.shape)[1:], *_rows(K, K.shape)[1:], *_rows(V, V.shape)[1:], *_rows(out, out.shape)[1:])
 
 
@@ -168,13 +185,11 @@ def prompt_attn(Q, K, V, cu_seqlens, out, desc, stream=None):
     index = _one_gpu(out, Q, K, V, cu_seqlens)
     if not (Q.dtype == K.dtype == V.dtype):
         raise TypeError("Q, K, V must share a dtype")
-    if _dtype_code(Q) != desc.dtype_in or _dtype_code(out) != desc.dtype_out:
+    if _code(Q) != desc.dtype_in or _code(out) != desc.dtype_out:
         raise TypeError("Q and out dtypes must match the descriptor")
     q, kv = (desc.Hq, desc.T, desc.D), (desc.Hkv, desc.T, desc.D)
-    (q_at, *sq), (k_at, *sk), (v_at, *sv), (o_at, *so) = _rows(Q, q), _rows(K, kv), _rows(V, kv), _rows(out, q)
-    if sq + sk + sv + so != [desc.q_head, desc.q_token, desc.k_head, desc.k_token, desc.v_head, desc.v_token, desc.o_head,
-                             desc.o_token]:
-        raise ValueError("strides must match the descriptor")
+    q_at, k_at = _placed(Q, q, (desc.q_head, desc.q_token, 1)), _placed(K, kv, (desc.k_head, desc.k_token, 1))
+    v_at, o_at = _placed(V, kv, (desc.v_head, desc.v_token, 1)), _placed(out, q, (desc.o_head, desc.o_token, 1))
     if _bounds(cu_seqlens) != desc.batch:
         raise ValueError("cu_seqlens must hold the descriptor's batch + 1 offsets")
     _call(index, stream, "ris_prompt_attn", q_at, k_at, v_at, cu_seqlens.data_ptr(), o_at, desc)
@@ -208,7 +223,7 @@ def _kv4(K, V, cu_seqlens, K4, V4, S, start):
     max_len = _need_cache(K4, V4, S, batch, Hkv, D)
     k_at, *k_strides = _rows(K, shape)
     v_at, *v_strides = _rows(V, shape)
-    return index, k_at, v_at, Kv4Desc(_dtype_code(K), Hkv, D, batch, T, max_len, *k_strides, *v_strides)
+    return index, k_at, v_at, Kv4Desc(_code(K), Hkv, D, batch, T, max_len, *k_strides, *v_strides)
 
 
 def kv4_store(K, V, cu_seqlens, K4, V4, S, start=None, stream=None):
@@ -229,7 +244,7 @@ def kv4_load(K4, V4, S, cu_seqlens, K, V, start=None, stream=None):
 def kv4_decode_desc(Q, K4, out, anchor_stride=0, window=0, sink=0, scale=0.0):
     """Descriptor from Q [B, Hq, D], the codes K4 [B, Hkv, max_len, D / 2] and out."""
     B, Hq, D = Q.shape
-    return ris.DecodeDesc(_dtype_code(Q), _dtype_code(out), B, Hq, K4.shape[1], D, K4.shape[2], anchor_stride, window,
+    return ris.DecodeDesc(_code(Q), _code(out), B, Hq, K4.shape[1], D, K4.shape[2], anchor_stride, window,
                           sink, scale)
 
 
@@ -255,7 +270,7 @@ def kv4_decode_attn(Q, K4, V4, S, pos, anchor_ptr, anchor_idx, out, workspace, d
             raise TypeError("anchor_ptr must be int64, anchor_idx int32")
         if anchor_ptr.numel() != desc.batch * (desc.Hkv + 1) or anchor_idx.numel() < desc.batch * desc.anchor_stride:
             raise ValueError("anchor_ptr must hold B * (Hkv + 1) entries and anchor_idx B * anchor_stride")
-    if _dtype_code(Q) != desc.dtype_in or _dtype_code(out) != desc.dtype_out:
+    if _code(Q) != desc.dtype_in or _code(out) != desc.dtype_out:
         raise TypeError("Q and out dtypes must match the descriptor")
     if Q.shape != (desc.batch, desc.Hq, desc.D) or out.shape != Q.shape:
         raise ValueError("Q and out must be [B, Hq, D] as in the descriptor")
@@ -270,7 +285,7 @@ def kv4_decode_attn(Q, K4, V4, S, pos, anchor_ptr, anchor_idx, out, workspace, d
 def logprob_desc(logits, n_targets=1, top_k=0):
     """Descriptor from logits [rows, vocab] (unit stride along vocab)."""
     rows, vocab = logits.shape
-    return LogprobDesc(_dtype_code(logits), n_targets, top_k, rows, vocab, max(logits.stride(0), vocab) if rows > 1 else vocab)
+    return LogprobDesc(_code(logits), n_targets, top_k, rows, vocab, max(logits.stride(0), vocab) if rows > 1 else vocab)
 
 
 def logprobs_workspace_bytes(desc):
@@ -289,7 +304,7 @@ def logprobs(logits, targets, logprob, entropy, top_ids, top_logprob, workspace,
     rows, n, k = desc.rows, desc.n_targets, desc.top_k
     if logits.shape != (rows, desc.vocab) or logits.stride(1) != 1 and desc.vocab > 1:
         raise ValueError("logits must be [rows, vocab] as in the descriptor, unit stride along vocab")
-    if rows > 1 and logits.stride(0) != desc.row_stride or _dtype_code(logits) != desc.dtype:
+    if rows > 1 and logits.stride(0) != desc.row_stride or _code(logits) != desc.dtype:
         raise ValueError("the logits' row stride and dtype must match the descriptor")
     _need_dense(targets, logprob, entropy, top_ids, top_logprob, workspace)
     for t, count, dtype in ((targets, n, torch.int64), (logprob, n, torch.float32), (top_ids, k, torch.int64),

@@ -234,3 +234,14 @@ def test_binding_refuses_before_any_call(serve):
         serve.logprobs_workspace_bytes(serve.logprob_desc(torch.zeros(2, 8), top_k=65))
     with pytest.raises(ris.RisError):
         serve.kv4_decode_workspace_bytes(decode(D=96))
+
+
+def test_binding_holds_views_against_the_descriptor(serve):
+    x = torch.zeros(2, 4, 64, dtype=torch.bfloat16)
+    one = torch.zeros(1, 1, 64)                 # any stride of a dimension of one
+    assert serve._placed(x, (2, 4, 64), (256, 64, 1)) == x.data_ptr() and serve._placed(one, (1, 1, 64), (0, 0, 1))
+    for bad, shape, strides in ((x, (2, 5, 64), (256, 64, 1)), (x, (2, 4, 64), (256, 128, 1)), (one, (1, 1, 64), (64, 64, 0))):
+        with pytest.raises(ValueError, match="match the descriptor"):
+            serve._placed(bad, shape, strides)
+    with pytest.raises(ValueError, match="16 bytes"):
+        serve._placed(torch.zeros(2, 4, 65)[..., 1:], (2, 4, 64), (260, 65, 1))
