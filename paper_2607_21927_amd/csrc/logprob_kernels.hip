@@ -20,7 +20,10 @@ constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kUnroll = 4;          // vectors a thread loads at a time
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kFar = -1e30f;      // stands for -inf in products with a weight of 0
-constexpr float kHuge = 1e38f;      // magnitudes whose product with log2 e may overflow
+// Magnitudes of a maximum up to which its product with log2 e, rounded, may be the
+// weights' reference: it is off by half a unit there, and weights by 2^0.5 alike (at 1e30
+// by 2^(2^75): infinite or 0).
+constexpr float kNear = 8388608.f;
 
 // Keys order logits as they compare, equal ones by descending id: the float's bits
 // made monotone, then the id's complement.  NaN ranks first, 0 is no token.
@@ -198,9 +201,9 @@ __global__ __launch_bounds__(kThreads) void k_logprob(LogprobParams p) {
         if (__any(top > m)) {
             const float old = b, was = m;
             m = fmaxf(m, top);
-            b = fabsf(m) < kHuge ? m * kLog2e : 0.f;
-            // references below -kHuge had weights of 0
-            const float d = was > -kHuge ? old - b : kFar, a = __builtin_amdgcn_exp2f(d);
+            b = fabsf(m) < kNear ? m * kLog2e : 0.f;
+            // under maxima of -kNear and below every weight was 0
+            const float d = was > -kNear ? old - b : kFar, a = __builtin_amdgcn_exp2f(d);
             u = a * fmaf(l, d, u);
             l *= a;
         }
@@ -299,7 +302,7 @@ __global__ __launch_bounds__(kThreads) void k_logprob(LogprobParams p) {
     // To natural units at the maximum itself, b being m log2 e rounded.
     State s{m, l, 0.f};
     {
-        const float c = fabsf(m) < kHuge ? fmaf(m, -kLog2e, b) : 0.f;
+        const float c = fabsf(m) < kNear ? fmaf(m, -kLog2e, b) : 0.f;
         const float f = __builtin_amdgcn_exp2f(c);
         s.u = kLn2 * f * fmaf(l, c, u);
         s.l = l * f;
@@ -320,9 +323,9 @@ __global__ __launch_bounds__(kThreads) void k_logprob(LogprobParams p) {
             s.u += t.u;
         }
     }
-    if (!(fabsf(s.m) < kHuge) && s.m != -INFINITY) {
-        // A maximum near the end of the range (a row masked as a whole with the type's
-        // lowest value): the sums once more from the differences.
+    if (!(fabsf(s.m) < kNear) && s.m != -INFINITY) {
+        // A maximum far from 0 (a row or part masked as a whole with a large negative
+        // number): the sums once more from the differences.
         State t{-INFINITY, 0.f, 0.f};
         const int64_t x0 = part == 0 ? 0 : head + (int64_t)v0 * E;
         const int64_t x1 = part == p.parts - 1 ? p.vocab : head + (int64_t)v1 * E;
