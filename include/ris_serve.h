@@ -175,7 +175,7 @@ int64_t ris_logprobs_workspace_bytes(const ris_logprob_desc* desc);
  * distribution: its log probabilities are -inf, its entropy is 0.  A NaN or
  * +inf makes its row's log probabilities and entropy NaN; such logits rank
  * first among the alternatives, NaN before +inf.  float32 arithmetic (the sums
- * of a row in at most 2^17 terms each before they meet).  The workspace may not
+ * of a row in some 2^17 terms each at most before they meet).  The workspace may not
  * be shared by calls that overlap in time; 16-byte aligned.
  */
 int ris_logprobs(const void* logits, const int64_t* targets, float* logprob, float* entropy, int64_t* top_ids,

@@ -396,12 +396,13 @@ __global__ __launch_bounds__(64) void k_logprob_merge(LogprobParams p) {
 
 }  // namespace
 
-// Workgroups of a row: ~1024 in all, at least 2048 logits each, at most one per
-// lane of the merging wave.
+// Workgroups of a row: ~1024 in all, at least 2048 logits each and 2^25 at most (2^17 terms
+// to a thread's sum), at most one per lane of the merging wave.
 int32_t logprob_parts(int64_t rows, int64_t vocab) {
     int64_t parts = (1024 + rows - 1) / rows;
-    const int64_t most = (vocab + 2047) / 2048;
+    const int64_t most = (vocab + 2047) / 2048, least = (vocab + (1 << 25) - 1) >> 25;
     if (parts > most) parts = most;
+    if (parts < least) parts = least;
     return (int32_t)(parts > 64 ? 64 : parts);
 }
 

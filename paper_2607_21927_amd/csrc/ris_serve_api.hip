@@ -129,7 +129,7 @@ int validate_logprob(const ris_logprob_desc* d) {
     if (d->rows < 1 || d->vocab < 1 || d->vocab > 0x7FFFFFFFll) return RIS_E_ARG;
     if (d->n_targets < 0 || d->n_targets > 65536 || d->top_k < 0 || d->top_k > RIS_MAX_TOP) return RIS_E_ARG;
     if (d->row_stride < d->vocab || d->row_stride > (1ll << 40)) return RIS_E_ARG;
-    if (!fits_dispatch(d->rows, 256)) return RIS_E_UNSUPPORTED;
+    if (d->rows > 0xFFFFFFFFll || !fits_dispatch(d->rows * ris::logprob_parts(d->rows, d->vocab), 256)) return RIS_E_UNSUPPORTED;
     return RIS_OK;
 }
 

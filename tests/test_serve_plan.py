@@ -1,0 +1,31 @@
+"""What the serving path plans on the host: workspaces (no GPU needed)."""
+import os
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def serve():
+    from paper_2607_21927_amd import _build, ris, serve as s
+    if not os.path.exists(ris.LIB_PATH):
+        _build.build()
+    s.lib()
+    return s
+
+
+@pytest.mark.parametrize("rows", [1, 1000, 1024, 4096, 100_000])
+@pytest.mark.parametrize("bits", [24, 25, 26, 28, 31])
+def test_wide_rows_are_cut_into_parts(serve, rows, bits):
+    """A float32 sum of a row has some 2^17 terms at most: 2^25 logits to a workgroup's
+    256 threads.  A part's state is 16 bytes of the workspace, 0 where there is one part."""
+    vocab = 2**bits - 1
+    d = serve.LogprobDesc(1, 1, 0, rows, vocab, vocab)
+    parts = max(1, serve.logprobs_workspace_bytes(d) // (16 * rows))
+    assert parts <= 64 and -(-vocab // parts) <= 2**25
+
+
+def test_parts_count_in_the_launch(serve):
+    """64 parts a row of 2^31 - 1 logits: what their work-items exceed is refused."""
+    for rows, ok in ((2**18 - 1, True), (2**18, False), (2**40, False)):
+        v = serve.lib().ris_logprobs_workspace_bytes(serve.LogprobDesc(1, 1, 0, rows, 2**31 - 1, 2**31 - 1))
+        assert v > 0 if ok else v == -5
