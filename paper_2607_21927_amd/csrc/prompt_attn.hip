@@ -16,7 +16,7 @@
 // rescales are rare.  A masked weight is 0, and 0 times an infinity or NaN of V would
 // be NaN: a workgroup whose output is not finite goes over its keys once more, with
 // such elements of V taken out of the tiles that the mask cuts and added where
-// they are attended to.
+// they are attended to.  So does one with a reference far from 0 (see Ref).
 //
 // Bound by how well the matrix unit (54% busy) and the vector unit (~45%) share the
 // time of two waves a SIMD at 1.9 GHz; LDS is at 27%, without bank conflicts.  At D =
@@ -107,6 +107,45 @@ __device__ __forceinline__ uint32_t finite_only(uint32_t u) {
     return (odd_half(u) ? 0u : u & 0xFFFFu) | (odd_half(u >> 16) ? 0u : u & 0xFFFF0000u);
 }
 
+// A row's reference: the maximum m that its weights 2^((s - m) c) are taken at.  As a
+// rule their exponent is one fma, s c - mc, with mc = m c rounded: the row's weights are
+// off by one factor then, within 2^0.5 while |mc| < kNearRef.  Beyond, where that factor
+// or mc itself may leave float32, a second pass (kSafe) takes the exponents of such rows
+// from s - m; other rows keep their bits.
+constexpr float kNearRef = 16777216.f;
+__device__ __forceinline__ bool far_ref(float mc) { return !(fabsf(mc) < kNearRef); }
+struct Ref {
+    float m, mc;        // mc: 0 while there is no maximum
+    bool apart;         // the row's exponents are taken from differences
+    __device__ __forceinline__ void reset() {
+        m = -INFINITY;
+        mc = 0.f;
+    }
+    // To the larger of m and mx; the factor for what was summed under the old one.
+    template <bool kSafe>
+    __device__ __forceinline__ float raise(float mx, float c) {
+        const float was = m, wasc = mc;
+        m = fmaxf(m, mx);
+        mc = m == -INFINITY ? 0.f : m * c;
+        return was == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(kSafe && apart ? (was - m) * c : wasc - mc);
+    }
+    template <bool kSafe>
+    __device__ __forceinline__ float weight(float s, float c) const {
+        return __builtin_amdgcn_exp2f(kSafe && apart ? (m == -INFINITY ? s : s - m) * c : fmaf(s, c, -mc));
+    }
+    // After a pass, with the row's sum of weights: references that were far for a while
+    // and rose have left a sum that is infinite or NaN.
+    __device__ __forceinline__ bool needs_apart(float l) {
+        const float sum = pair_sum32(l);
+        return apart = far_ref(mc) || !isfinite(sum);
+    }
+};
+// The factor of a partial sum under the reference m (mc) where partial sums of one row
+// meet under the largest, top (topc); far: one of theirs is.
+__device__ __forceinline__ float join_factor(float m, float mc, float top, float topc, bool far, float c) {
+    return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(far ? (m - top) * c : mc - topc);
+}
+
 template <int D, int S>
 __global__ __launch_bounds__(64 * kWaves * S, D == 64 ? 3 : 2) void k_prompt_bf16(PromptParams p) {
     constexpr int SL = D / 16;      // contraction steps of the score product
@@ -153,7 +192,8 @@ __global__ __launch_bounds__(64 * kWaves * S, D == 64 ? 3 : 2) void k_prompt_bf1
     const int tiles = (kend + kKeys - 1) / kKeys;
 
     f32x16_t o[DB];
-    float m = -INFINITY, mc = 0.f, l = 0.f;      // reference maximum in scores; times c, 0 while there is none; sum
+    Ref ref;
+    float l;
 
     // S^T of a tile: lane l holds query l % 32 at keys 32 b + 8 (i / 4) + 4 (l / 32) + i % 4.
     const auto scores = [&](const uint16_t* kl, f32x16_t (&st)[2]) __attribute__((always_inline)) {
@@ -188,12 +228,8 @@ __global__ __launch_bounds__(64 * kWaves * S, D == 64 ? 3 : 2) void k_prompt_bf1
 #pragma unroll
             for (int i = 0; i < 16; ++i) mx = fmaxf(mx, st[b][i]);
         mx = pair_max32(mx);
-        if (__any(mx > m + p.slack)) {
-            const bool none = m == -INFINITY;                      // nothing summed yet: o and l are 0
-            m = fmaxf(m, mx);
-            const float nc = m == -INFINITY ? 0.f : m * p.c;
-            const float al = none ? 0.f : __builtin_amdgcn_exp2f(mc - nc);
-            mc = nc;
+        if (__any(mx > ref.m + p.slack)) {
+            const float al = ref.template raise<kSafe>(mx, p.c);
             l *= al;
 #pragma unroll
             for (int d = 0; d < DB; ++d)
@@ -206,8 +242,8 @@ __global__ __launch_bounds__(64 * kWaves * S, D == 64 ? 3 : 2) void k_prompt_bf1
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
-                const float x = __builtin_amdgcn_exp2f(fmaf(st[b][i], p.c, -mc));
-                const float y = __builtin_amdgcn_exp2f(fmaf(st[b][i + 1], p.c, -mc));
+                const float x = ref.template weight<kSafe>(st[b][i], p.c);
+                const float y = ref.template weight<kSafe>(st[b][i + 1], p.c);
                 l += x + y;
                 pf[2 * b + i / 8][i % 8 / 2] = pack_bf16x2(x, y);
             }
@@ -262,10 +298,13 @@ __global__ __launch_bounds__(64 * kWaves * S, D == 64 ? 3 : 2) void k_prompt_bf1
     const int have = (tiles - group + S - 1) / S;                   // the group's tiles
     const int mine = q0 < n ? (wlast / kKeys + S - group) / S : 0;  // those that the wave's rows attend to
     const auto pass = [&](auto safe) __attribute__((always_inline)) {
+        constexpr bool kSafe = decltype(safe)::value;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+        ref.reset();
+        l = 0.f;
         if (have > 0) {
             load_tile<D>(pc, K, p.k_token, group * kKeys, n, k0);
             load_tile<D>(pc, V, p.v_token, group * kKeys, n, v0);
@@ -304,10 +343,11 @@ __global__ __launch_bounds__(64 * kWaves * S, D == 64 ? 3 : 2) void k_prompt_bf1
             uint16_t* const place[4] = {k0s, k1s, v0s, v1s};         // S kKeys D elements each: 64 D floats
 #pragma unroll
             for (int d = 0; d < DB; ++d) mem[d] = reinterpret_cast<float*>(place[d]) + wave * 16 * 64 + lane;
-            __shared__ float ml[kWaves][2][64];
+            __shared__ float ml[kWaves][3][64];
             if (group == 1) {
-                ml[wave][0][lane] = m;
-                ml[wave][1][lane] = l;
+                ml[wave][0][lane] = ref.m;
+                ml[wave][1][lane] = ref.mc;
+                ml[wave][2][lane] = l;
 #pragma unroll
                 for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -315,10 +355,10 @@ __global__ __launch_bounds__(64 * kWaves * S, D == 64 ? 3 : 2) void k_prompt_bf1
             }
             __syncthreads();
             if (group == 0) {
-                const float m1 = ml[wave][0][lane], big = fmaxf(m, m1), c = big == -INFINITY ? 0.f : big * p.c;
-                const float a = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - c);
-                const float a1 = m1 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m1 * p.c - c);
-                l = l * a + ml[wave][1][lane] * a1;
+                const float m1 = ml[wave][0][lane], mc1 = ml[wave][1][lane], top = fmaxf(ref.m, m1), topc = ref.m < m1 ? mc1 : ref.mc;
+                const bool far = far_ref(ref.mc) || far_ref(mc1);
+                const float a = join_factor(ref.m, ref.mc, top, topc, far, p.c), a1 = join_factor(m1, mc1, top, topc, far, p.c);
+                l = l * a + ml[wave][2][lane] * a1;
 #pragma unroll
                 for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -332,9 +372,7 @@ __global__ __launch_bounds__(64 * kWaves * S, D == 64 ? 3 : 2) void k_prompt_bf1
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) odd = fmaf(o[d][i], 0.f, odd);       // NaN if any is not finite
-    if (__syncthreads_or(odd != odd && row < n && group == 0)) {
-        m = -INFINITY;
-        mc = l = 0.f;
+    if (__syncthreads_or((ref.needs_apart(l) || odd != odd) && row < n)) {
         pass(std::true_type{});
     }
     l = pair_sum32(l);
@@ -350,31 +388,36 @@ __global__ __launch_bounds__(64 * kWaves * S, D == 64 ? 3 : 2) void k_prompt_bf1
 
 // The states of a workgroup's four waves, each over its own keys of the same 32 rows,
 // to the rows' outputs.  mem: room for [wave][dim block][register][lane], a wave's in its
-// K tile's place; ml: 128 floats a wave, kTile apart, in its V tile's place.  A wave
+// K tile's place; ml: 256 floats a wave, kTile apart, in its V tile's place.  A wave
 // stores the dims of four registers of every 16 (8 of a row's 32).
 template <int D, int kTile>
-__device__ __forceinline__ void join_waves(const PromptParams& p, float* mem, float* ml, float m, float l, const f32x16_t (&o)[D / 32],
+__device__ __forceinline__ void join_waves(const PromptParams& p, float* mem, float* ml, const Ref& ref, float l, const f32x16_t (&o)[D / 32],
                                            const RowTile& t, int row, int h) {
     constexpr int DB = D / 32;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lh = lane >> 5;
     mem += lane;
     ml += lane;
-    ml[wave * kTile] = m;
+    ml[wave * kTile] = ref.m;
     ml[wave * kTile + 64] = pair_sum32(l);
+    ml[wave * kTile + 192] = ref.mc;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) mem[((wave * DB + d) * 16 + i) * 64] = o[d][i];
     __syncthreads();
     if (row >= t.len) return;
-    float big = -INFINITY, a[kWaves], sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) big = fmaxf(big, ml[w * kTile]);
-    const float c = big == -INFINITY ? 0.f : big * p.c;
+    float top = -INFINITY, topc = 0.f, a[kWaves], sum = 0.f;
+    bool far = false;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-        const float mw = ml[w * kTile];
-        a[w] = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw * p.c - c);
+        const float m = ml[w * kTile], mc = ml[w * kTile + 192];
+        topc = top < m ? mc : topc;
+        top = fmaxf(top, m);
+        far |= far_ref(mc);
+    }
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        a[w] = join_factor(ml[w * kTile], ml[w * kTile + 192], top, topc, far, p.c);
         sum += a[w] * ml[w * kTile + 64];
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -456,7 +499,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_narrow(PromptParams p
         for (int s = 0; s < SL; ++s) qf[s] = *reinterpret_cast<const u32x4_t*>(qp + 16 * s);
     }
     f32x16_t o[DB];
-    float m, mc, l;
+    Ref ref;
+    float l;
     const int r0 = 4 * lh + ((lane & 15) >> 2), cq = 2 * (lane >> 4 & 1) + ((lane & 3) >> 1);
     // kSafe: V may hold infinities or NaN under the mask
     const auto pass = [&](auto safe, uint16_t* __restrict__ kt, uint16_t* __restrict__ vt) __attribute__((always_inline)) {
@@ -465,8 +509,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_narrow(PromptParams p
         for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-        m = -INFINITY;
-        mc = l = 0.f;
+        ref.reset();
+        l = 0.f;
         // kMore: the wave has a tile after this one
         const auto step = [&](auto more, int it) __attribute__((always_inline)) {
             constexpr bool kMore = decltype(more)::value;
@@ -498,12 +542,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_narrow(PromptParams p
             mx = pair_max32(mx);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // every read of K has returned
             if constexpr (kMore) load(K, p.k_token, jn, kt);
-            if (__any(mx > m + p.slack)) {
-                const bool none = m == -INFINITY;
-                m = fmaxf(m, mx);
-                const float nc = m == -INFINITY ? 0.f : m * p.c;
-                const float al = none ? 0.f : __builtin_amdgcn_exp2f(mc - nc);
-                mc = nc;
+            if (__any(mx > ref.m + p.slack)) {
+                const float al = ref.template raise<kSafe>(mx, p.c);
                 l *= al;
 #pragma unroll
                 for (int d = 0; d < DB; ++d)
@@ -515,8 +555,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_narrow(PromptParams p
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int i = 0; i < 16; i += 2) {
-                    const float x = __builtin_amdgcn_exp2f(fmaf(st[b][i], p.c, -mc));
-                    const float y = __builtin_amdgcn_exp2f(fmaf(st[b][i + 1], p.c, -mc));
+                    const float x = ref.template weight<kSafe>(st[b][i], p.c);
+                    const float y = ref.template weight<kSafe>(st[b][i + 1], p.c);
                     l += x + y;
                     pf[2 * b + i / 8][i % 8 / 2] = pack_bf16x2(x, y);
                 }
@@ -560,11 +600,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_narrow(PromptParams p
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) odd = fmaf(o[d][i], 0.f, odd);
-    if (any_wave<kKeys * D / 2>(odd != odd && row < n, reinterpret_cast<float*>(lds + kWaves * kKeys * D))) {
+    if (any_wave<kKeys * D / 2>((ref.needs_apart(l) || odd != odd) && row < n, reinterpret_cast<float*>(lds + kWaves * kKeys * D))) {
         __syncthreads();
         pass(std::true_type{}, kl, vl);
     }
-    join_waves<D, kKeys * D / 2>(p, reinterpret_cast<float*>(lds), reinterpret_cast<float*>(lds + kWaves * kKeys * D), m, l, o, t, row, h);
+    join_waves<D, kKeys * D / 2>(p, reinterpret_cast<float*>(lds), reinterpret_cast<float*>(lds + kWaves * kKeys * D), ref, l, o, t, row, h);
 }
 
 // The same for many prompts of a few tokens: a tile is 32 neighbouring tokens, of as
@@ -623,7 +663,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_short(PromptParams p)
         for (int s = 0; s < SL; ++s) qf[s] = *reinterpret_cast<const u32x4_t*>(qp + 16 * s);
     }
     f32x16_t o[DB];
-    float m, mc, l;
+    Ref ref;
+    float l;
     const int r0 = 4 * lh + ((lane & 15) >> 2), cq = 2 * (lane >> 4 & 1) + ((lane & 3) >> 1);
     // kSafe: V may hold infinities or NaN under the mask
     const auto pass = [&](auto safe, uint16_t* __restrict__ kt, uint16_t* __restrict__ vt) __attribute__((always_inline)) {
@@ -632,8 +673,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_short(PromptParams p)
         for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-        m = -INFINITY;
-        mc = l = 0.f;
+        ref.reset();
+        l = 0.f;
         // kMore: there are keys after this tile's
         const auto step = [&](auto more, int j0) __attribute__((always_inline)) {
             constexpr bool kMore = decltype(more)::value;
@@ -656,12 +697,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_short(PromptParams p)
             mx = pair_max32(mx);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // every read of K has returned
             if constexpr (kMore) load(K, p.k_token, j0 + kShortKeys, kt);
-            if (__any(mx > m + p.slack)) {
-                const bool none = m == -INFINITY;
-                m = fmaxf(m, mx);
-                const float nc = m == -INFINITY ? 0.f : m * p.c;
-                const float al = none ? 0.f : __builtin_amdgcn_exp2f(mc - nc);
-                mc = nc;
+            if (__any(mx > ref.m + p.slack)) {
+                const float al = ref.template raise<kSafe>(mx, p.c);
                 l *= al;
 #pragma unroll
                 for (int d = 0; d < DB; ++d)
@@ -671,8 +708,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_short(PromptParams p)
             u32x4_t pf[2];
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
-                const float x = __builtin_amdgcn_exp2f(fmaf(st[i], p.c, -mc));
-                const float y = __builtin_amdgcn_exp2f(fmaf(st[i + 1], p.c, -mc));
+                const float x = ref.template weight<kSafe>(st[i], p.c);
+                const float y = ref.template weight<kSafe>(st[i + 1], p.c);
                 l += x + y;
                 pf[i / 8][i % 8 / 2] = pack_bf16x2(x, y);
             }
@@ -715,7 +752,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_short(PromptParams p)
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) odd = fmaf(o[d][i], 0.f, odd);
-    if (__any(odd != odd && in)) pass(std::true_type{}, kl, vl);
+    if (__any((ref.needs_apart(l) || odd != odd) && in)) pass(std::true_type{}, kl, vl);
     l = pair_sum32(l);
     if (!in) return;
     const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -777,7 +814,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_f32(PromptParams p) {
         for (int s = 0; s < D / 8; ++s) qf[s] = *reinterpret_cast<const f32x4_t*>(qp + 8 * s);
     }
     f32x16_t o[DB];
-    float m, mc, l;
+    Ref ref;
+    float l;
     // kSafe: V may hold infinities or NaN under the mask
     const auto pass = [&](auto safe, float* __restrict__ kt, float* __restrict__ vt) __attribute__((always_inline)) {
         constexpr bool kSafe = decltype(safe)::value;
@@ -785,8 +823,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_f32(PromptParams p) {
         for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-        m = -INFINITY;
-        mc = l = 0.f;
+        ref.reset();
+        l = 0.f;
         // kMore: the wave has a tile after this one
         const auto step = [&](auto more, int it) __attribute__((always_inline)) {
             constexpr bool kMore = decltype(more)::value;
@@ -812,12 +850,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_f32(PromptParams p) {
             mx = pair_max32(mx);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // every read of K has returned
             if constexpr (kMore) load(K, p.k_token, jn, kt);
-            if (__any(mx > m + p.slack)) {
-                const bool none = m == -INFINITY;
-                m = fmaxf(m, mx);
-                const float nc = m == -INFINITY ? 0.f : m * p.c;
-                const float al = none ? 0.f : __builtin_amdgcn_exp2f(mc - nc);
-                mc = nc;
+            if (__any(mx > ref.m + p.slack)) {
+                const float al = ref.template raise<kSafe>(mx, p.c);
                 l *= al;
 #pragma unroll
                 for (int d = 0; d < DB; ++d)
@@ -826,7 +860,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_f32(PromptParams p) {
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                st[i] = __builtin_amdgcn_exp2f(fmaf(st[i], p.c, -mc));
+                st[i] = ref.template weight<kSafe>(st[i], p.c);
                 l += st[i];
             }
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kMore ? kPieces : 0) : "memory");      // V; not the next K
@@ -865,11 +899,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_f32(PromptParams p) {
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) odd = fmaf(o[d][i], 0.f, odd);
-    if (any_wave<kKeys32 * D>(odd != odd && row < n, lds + kWaves * kKeys32 * D)) {
+    if (any_wave<kKeys32 * D>((ref.needs_apart(l) || odd != odd) && row < n, lds + kWaves * kKeys32 * D)) {
         __syncthreads();
         pass(std::true_type{}, kl, vl);
     }
-    join_waves<D, kKeys32 * D>(p, lds, lds + kWaves * kKeys32 * D, m, l, o, t, row, h);
+    join_waves<D, kKeys32 * D>(p, lds, lds + kWaves * kKeys32 * D, ref, l, o, t, row, h);
 }
 
 // Workgroups of a launch whose row tiles hold `rows`.

@@ -1,0 +1,103 @@
+"""Packed prompt attention at the ends of what its arguments may hold: scores and
+scales whose products leave float32.  Every form that the batch's shape chooses is reached.
+"""
+import numpy as np
+import pytest
+
+from gpu_common import say, torch
+from serve_common import U, attn_bar, bounds, need_serve
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+# form: dtype, Hq, Hkv, lengths of the prompts
+FORMS = {
+    "narrow": (BF16, 4, 2, [300]),
+    "split": (BF16, 12, 2, [2048]),
+    "wide": (BF16, 12, 2, [3000, 1200, 1500]),
+    "short": (BF16, 12, 2, [5, 40, 64, 7, 1, 100] * 35),
+    "f32": (F32, 4, 2, [300, 77]),
+}
+
+
+def run(serve, q, k, v, cu, scale=0.0, causal=1):
+    out = torch.full(q.shape, 9.0, dtype=F32, device="cuda")
+    return serve.prompt_attn(q, k, v, cu, out, serve.prompt_desc(q, k, v, out, cu, causal=causal, scale=scale))
+
+
+def expect(q, k, v, lens, weigh, causal=1):
+    """float64: ``weigh`` makes the weights [n, n] of the masked scores of a prompt and head."""
+    G, at, out = q.shape[0] // k.shape[0], 0, []
+    for n in lens:
+        late = torch.ones(n, n, dtype=torch.bool, device="cuda").triu(1)
+        heads = []
+        for h in range(q.shape[0]):
+            s = q[h, at:at + n].double() @ k[h // G, at:at + n].double().t().contiguous()
+            if causal:
+                s.masked_fill_(late, -np.inf)
+            heads.append(weigh(s) @ v[h // G, at:at + n].double())
+        out.append(torch.stack(heads))
+        at += n
+    return torch.cat(out, 1)
+
+
+def best(s):
+    """Equal weights on the largest scores."""
+    top = (s == s.amax(1, keepdim=True)).double()
+    return top / top.sum(1, keepdim=True)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("scale,power", [(2.0**126, 0), (1e38, 0), (1e12, 0), (1.0, 40), (0.0, 60), (1.0, 118), (2.0**-20, 100)])
+def test_far_scores(form, D, scale, power):
+    """Q and K of small integers (times a power of two): scores are exact, and those below
+    a row's largest have no weight.  Outputs are then sums of at most n values V with
+    weights of 1, off by (n + 64) u max|V|."""
+    serve = need_serve()
+    dtype, Hq, Hkv, lens = FORMS[form]
+    say(f"prompt {form} D={D} scale={scale} 2^{power}")
+    g = torch.Generator().manual_seed(D + power)
+    T = sum(lens)
+    q = (torch.randint(-1, 2, (Hq, T, D), generator=g) * 2.0**power).to(dtype).cuda()
+    k = torch.randint(-1, 2, (Hkv, T, D), generator=g).to(dtype).cuda()
+    v = torch.randn(Hkv, T, D, generator=g).to(dtype).cuda()
+    for causal in (1, 0) if form in ("narrow", "short", "f32") else (1,):
+        got = run(serve, q, k, v, bounds(lens), scale, causal)
+        want = expect(q, k, v, lens, best, causal)
+        assert (got.double() - want).abs().max().item() <= (max(lens) + 64) * U * v.double().abs().max().item()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("form", FORMS)
+def test_far_rows_leave_the_others_as_they_are(form, D):
+    """Queries of every fifth token far from 0: the other rows stay within their bars (the
+    rows of a wave move their references together, so not to the bit).  Keys that are far
+    until a nearer one has come: its weight is all there is, so the output is its value,
+    off by 8 u: the product 3 log2 e is rounded in the reference (3 u in the weight, of which
+    bf16 products see a rounded one), the exponential, the quotient."""
+    serve = need_serve()
+    dtype, Hq, Hkv, lens = FORMS[form]
+    g = torch.Generator().manual_seed(D)
+    T = sum(lens)
+    q, k, v = (torch.randn(h, T, D, generator=g) for h in (Hq, Hkv, Hkv))
+    q, k, v = (x.to(dtype).cuda() for x in (q, k, v))
+    far = q.clone()
+    far[:, ::5] *= 2.0**30
+    got = run(serve, far, k, v, bounds(lens))
+    assert got.isfinite().all()
+    want = expect(q, k, v, lens, lambda s: (s * D**-0.5).softmax(1))
+    bar = attn_bar(q, k, v, max(lens), D**-0.5, want, dtype, F32)
+    near = torch.arange(T, device="cuda") % 5 > 0
+    assert ((got.double() - want).abs() <= bar)[:, near].all()
+    # all scores -2^40 but the last of each prompt's
+    q = torch.zeros_like(q)
+    q[..., 0] = 1.0
+    k = torch.zeros_like(k)
+    k[..., 0] = -(2.0**40)
+    last = bounds(lens)[1:] - 1
+    k[:, last, 0] = 3.0
+    got = run(serve, q, k, v, bounds(lens), 1.0)
+    want = v[:, last].double().repeat_interleave(Hq // Hkv, 0)
+    assert ((got[:, last].double() - want).abs() <= 8 * U * want.abs()).all() and got.isfinite().all()
