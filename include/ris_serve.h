@@ -75,8 +75,9 @@ typedef struct {
  *   out[h, t, :] = sum_j softmax_j(scale <Q[h, t], K[g, j]>) V[g, j],
  * g = floor(h / (Hq / Hkv)), j over the tokens of t's sequence up to t (or all
  * of them, causal = 0).  What lies in keys and values that a token does not
- * attend to, infinities and NaN included, does not reach its output.  float32
- * accumulation; with bf16 inputs the softmax weights enter the PV product
+ * attend to, infinities and NaN included, does not reach its output; an infinity
+ * of V that it attends to does, whatever its weight (with one of the other sign
+ * or a NaN: NaN).  float32 accumulation; with bf16 inputs the softmax weights enter the PV product
  * rounded to bf16.  out must not overlap the inputs, and its rows must not
  * overlap each other.
  */

@@ -13,10 +13,10 @@
 // barrier a tile.
 //
 // The reference maximum moves only when a score exceeds it by 2^8 in weight, so
-// rescales are rare.  A masked weight is 0, and 0 times an infinity or NaN of V would
-// be NaN: a workgroup whose output is not finite goes over its keys once more, with
-// such elements of V taken out of the tiles that the mask cuts and added where
-// they are attended to.  So does one with a reference far from 0 (see Ref).
+// rescales are rare.  A weight of 0, masked or too small for float32, times an infinity
+// or NaN of V would be NaN: a workgroup whose output is not finite goes over its keys
+// once more, with such elements of V taken out of the tiles and added, whatever their
+// weight, where they are attended to.  So does one with a reference far from 0 (see Ref).
 //
 // Bound by how well the matrix unit (54% busy) and the vector unit (~45%) share the
 // time of two waves a SIMD at 1.9 GHz; LDS is at 27%, without bank conflicts.  At D =
@@ -106,6 +106,32 @@ __device__ __forceinline__ bool odd_half(uint32_t u) { return (u & 0x7F80u) == 0
 __device__ __forceinline__ uint32_t finite_only(uint32_t u) {
     return (odd_half(u) ? 0u : u & 0xFFFFu) | (odd_half(u >> 16) ? 0u : u & 0xFFFF0000u);
 }
+// Whether a tile of N elements holds any such, by the whole wave.
+template <int N>
+__device__ __forceinline__ bool any_odd(const uint16_t* x) {
+    bool odd = false;
+#pragma unroll 1
+    for (int at = 8 * (threadIdx.x & 63); at < N; at += 8 * 64) {
+        const u32x4_t v = *reinterpret_cast<const u32x4_t*>(x + at);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) odd |= finite_only(v[i]) != v[i];
+    }
+    return __any(odd);
+}
+template <int N>
+__device__ __forceinline__ bool any_odd(const float* x) {
+    bool odd = false;
+#pragma unroll 1
+    for (int at = 4 * (threadIdx.x & 63); at < N; at += 4 * 64) {
+        const f32x4_t v = *reinterpret_cast<const f32x4_t*>(x + at);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) odd |= !isfinite(v[i]);
+    }
+    return __any(odd);
+}
+// A sum times a factor that may have fallen to 0; an infinity in it stays (kSafe).
+template <bool kSafe>
+__device__ __forceinline__ float scaled(float x, float a) { return kSafe && !isfinite(x) ? x : x * a; }
 
 // A row's reference: the maximum m that its weights 2^((s - m) c) are taken at.  As a
 // rule their exponent is one fma, s c - mc, with mc = m c rounded: the row's weights are
@@ -209,13 +235,11 @@ __global__ __launch_bounds__(64 * kWaves * S, D == 64 ? 3 : 2) void k_prompt_bf1
         }
     };
     // The tile at j0 from its scores `st` and values `vl`, with the next tile's scores
-    // `nx` from `kn` beside it (kMore).  kSafe: the mask cuts the tile, and V may hold
-    // infinities or NaN under it.
+    // `nx` from `kn` beside it (kMore).  kSafe: V may hold infinities or NaN.
     const auto compute = [&](auto more, auto safe, f32x16_t (&st)[2], f32x16_t (&nx)[2], const uint16_t* kn, const uint16_t* vl,
                              int j0) __attribute__((always_inline)) {
         constexpr bool kMore = decltype(more)::value, kSafe = decltype(safe)::value;
-        const bool cut = j0 + kKeys - 1 > wfull;
-        if (cut) {
+        if (j0 + kKeys - 1 > wfull) {
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -234,7 +258,7 @@ __global__ __launch_bounds__(64 * kWaves * S, D == 64 ? 3 : 2) void k_prompt_bf1
 #pragma unroll
             for (int d = 0; d < DB; ++d)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) o[d][i] *= al;
+                for (int i = 0; i < 16; ++i) o[d][i] = scaled<kSafe>(o[d][i], al);
         }
         if constexpr (kMore) scores(kn, nx);
         u32x4_t pf[4];
@@ -260,7 +284,7 @@ __global__ __launch_bounds__(64 * kWaves * S, D == 64 ? 3 : 2) void k_prompt_bf1
                 u32x4_t v = {a.x, a.y, b.x, b.y};
                 if constexpr (kSafe) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] = cut ? finite_only(v[i]) : v[i];
+                    for (int i = 0; i < 4; ++i) v[i] = finite_only(v[i]);
                 }
                 o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v), as_bf16x8(pf[u]), o[d], 0, 0, 0);
             }
@@ -280,15 +304,16 @@ __global__ __launch_bounds__(64 * kWaves * S, D == 64 ? 3 : 2) void k_prompt_bf1
             }
         }
         if constexpr (kSafe) {
-            for (int r = 0; cut && r < kKeys; ++r)
+            if (any_odd<kKeys * D>(vl))
+                for (int r = 0; r < kKeys; ++r)
 #pragma unroll
-                for (int d = 0; d < DB; ++d)
+                    for (int d = 0; d < DB; ++d)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int dim = 32 * d + 8 * (i / 4) + 4 * lh + i % 4;
-                        const uint16_t v = vl[r * D + 8 * ((dim >> 3) ^ swizzle<D>(r)) + (dim & 7)];
-                        if (odd_half(v) && j0 + r <= last) o[d][i] += bf16_to_f32(v);
-                    }
+                        for (int i = 0; i < 16; ++i) {
+                            const int dim = 32 * d + 8 * (i / 4) + 4 * lh + i % 4;
+                            const uint16_t v = vl[r * D + 8 * ((dim >> 3) ^ swizzle<D>(r)) + (dim & 7)];
+                            if (odd_half(v) && j0 + r <= last) o[d][i] += bf16_to_f32(v);
+                        }
         }
     };
     // All of the group's keys, its i-th tile being tile S i + group.  While one is
@@ -362,7 +387,7 @@ __global__ __launch_bounds__(64 * kWaves * S, D == 64 ? 3 : 2) void k_prompt_bf1
 #pragma unroll
                 for (int d = 0; d < DB; ++d)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) o[d][i] = o[d][i] * a + mem[d][64 * i] * a1;
+                    for (int i = 0; i < 16; ++i) o[d][i] = scaled<kSafe>(o[d][i], a) + scaled<kSafe>(mem[d][64 * i], a1);
             }
         }
     };
@@ -387,10 +412,10 @@ __global__ __launch_bounds__(64 * kWaves * S, D == 64 ? 3 : 2) void k_prompt_bf1
 }
 
 // The states of a workgroup's four waves, each over its own keys of the same 32 rows,
-// to the rows' outputs.  mem: room for [wave][dim block][register][lane], a wave's in its
+// to the rows' outputs (kSafe: after a second pass).  mem: room for [wave][dim block][register][lane], a wave's in its
 // K tile's place; ml: 256 floats a wave, kTile apart, in its V tile's place.  A wave
 // stores the dims of four registers of every 16 (8 of a row's 32).
-template <int D, int kTile>
+template <int D, int kTile, bool kSafe>
 __device__ __forceinline__ void join_waves(const PromptParams& p, float* mem, float* ml, const Ref& ref, float l, const f32x16_t (&o)[D / 32],
                                            const RowTile& t, int row, int h) {
     constexpr int DB = D / 32;
@@ -413,7 +438,7 @@ __device__ __forceinline__ void join_waves(const PromptParams& p, float* mem, fl
         const float m = ml[w * kTile], mc = ml[w * kTile + 192];
         topc = top < m ? mc : topc;
         top = fmaxf(top, m);
-        far |= far_ref(mc);
+        far |= kSafe && far_ref(mc);
     }
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
@@ -429,7 +454,7 @@ __device__ __forceinline__ void join_waves(const PromptParams& p, float* mem, fl
         for (int i = 0; i < 4; ++i) {
             y[i] = 0.f;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) y[i] += a[w] * mem[((w * DB + d) * 16 + 4 * wave + i) * 64];
+            for (int w = 0; w < kWaves; ++w) y[i] += scaled<kSafe>(mem[((w * DB + d) * 16 + 4 * wave + i) * 64], a[w]);
         }
         store4(p, at + 32 * d, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
     }
@@ -502,7 +527,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_narrow(PromptParams p
     Ref ref;
     float l;
     const int r0 = 4 * lh + ((lane & 15) >> 2), cq = 2 * (lane >> 4 & 1) + ((lane & 3) >> 1);
-    // kSafe: V may hold infinities or NaN under the mask
+    // kSafe: V may hold infinities or NaN
     const auto pass = [&](auto safe, uint16_t* __restrict__ kt, uint16_t* __restrict__ vt) __attribute__((always_inline)) {
         constexpr bool kSafe = decltype(safe)::value;
 #pragma unroll
@@ -548,7 +573,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_narrow(PromptParams p
 #pragma unroll
                 for (int d = 0; d < DB; ++d)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) o[d][i] *= al;
+                    for (int i = 0; i < 16; ++i) o[d][i] = scaled<kSafe>(o[d][i], al);
             }
             u32x4_t pf[4];
 #pragma unroll
@@ -575,7 +600,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_narrow(PromptParams p
                     }
                     o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v), as_bf16x8(pf[u]), o[d], 0, 0, 0);
                 }
-            for (int r = 0; kSafe && r < kKeys; ++r)
+            if (kSafe && any_odd<kKeys * D>(vt))
+                for (int r = 0; r < kKeys; ++r)
 #pragma unroll
                     for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -600,11 +626,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_narrow(PromptParams p
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) odd = fmaf(o[d][i], 0.f, odd);
-    if (any_wave<kKeys * D / 2>((ref.needs_apart(l) || odd != odd) && row < n, reinterpret_cast<float*>(lds + kWaves * kKeys * D))) {
+    float* const vf = reinterpret_cast<float*>(lds + kWaves * kKeys * D);
+    const bool again = any_wave<kKeys * D / 2>((ref.needs_apart(l) || odd != odd) && row < n, vf);
+    if (again) {
         __syncthreads();
         pass(std::true_type{}, kl, vl);
+        join_waves<D, kKeys * D / 2, true>(p, reinterpret_cast<float*>(lds), vf, ref, l, o, t, row, h);
+    } else {
+        join_waves<D, kKeys * D / 2, false>(p, reinterpret_cast<float*>(lds), vf, ref, l, o, t, row, h);
     }
-    join_waves<D, kKeys * D / 2>(p, reinterpret_cast<float*>(lds), reinterpret_cast<float*>(lds + kWaves * kKeys * D), ref, l, o, t, row, h);
 }
 
 // The same for many prompts of a few tokens: a tile is 32 neighbouring tokens, of as
@@ -666,7 +696,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_short(PromptParams p)
     Ref ref;
     float l;
     const int r0 = 4 * lh + ((lane & 15) >> 2), cq = 2 * (lane >> 4 & 1) + ((lane & 3) >> 1);
-    // kSafe: V may hold infinities or NaN under the mask
+    // kSafe: V may hold infinities or NaN
     const auto pass = [&](auto safe, uint16_t* __restrict__ kt, uint16_t* __restrict__ vt) __attribute__((always_inline)) {
         constexpr bool kSafe = decltype(safe)::value;
 #pragma unroll
@@ -703,7 +733,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_short(PromptParams p)
 #pragma unroll
                 for (int d = 0; d < DB; ++d)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) o[d][i] *= al;
+                    for (int i = 0; i < 16; ++i) o[d][i] = scaled<kSafe>(o[d][i], al);
             }
             u32x4_t pf[2];
 #pragma unroll
@@ -728,15 +758,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_short(PromptParams p)
                     }
                     o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v), as_bf16x8(pf[u]), o[d], 0, 0, 0);
                 }
-            for (int r = 0; kSafe && r < kShortKeys; ++r)
+            if (kSafe && any_odd<kShortKeys * D>(vt))
+                for (int r = 0; r < kShortKeys; ++r)
 #pragma unroll
-                for (int d = 0; d < DB; ++d)
+                    for (int d = 0; d < DB; ++d)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int dim = 32 * d + 8 * (i / 4) + 4 * lh + i % 4;
-                        const uint16_t v = vt[r * D + 8 * ((dim >> 3) ^ swizzle<D>(r)) + (dim & 7)];
-                        if (odd_half(v) && j0 + r >= lo && j0 + r <= hi) o[d][i] += bf16_to_f32(v);
-                    }
+                        for (int i = 0; i < 16; ++i) {
+                            const int dim = 32 * d + 8 * (i / 4) + 4 * lh + i % 4;
+                            const uint16_t v = vt[r * D + 8 * ((dim >> 3) ^ swizzle<D>(r)) + (dim & 7)];
+                            if (odd_half(v) && j0 + r >= lo && j0 + r <= hi) o[d][i] += bf16_to_f32(v);
+                        }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // every read of V has returned
             if constexpr (kMore) load(V, p.v_token, j0 + kShortKeys, vt);
         };
@@ -816,7 +847,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_f32(PromptParams p) {
     f32x16_t o[DB];
     Ref ref;
     float l;
-    // kSafe: V may hold infinities or NaN under the mask
+    // kSafe: V may hold infinities or NaN
     const auto pass = [&](auto safe, float* __restrict__ kt, float* __restrict__ vt) __attribute__((always_inline)) {
         constexpr bool kSafe = decltype(safe)::value;
 #pragma unroll
@@ -856,7 +887,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_f32(PromptParams p) {
 #pragma unroll
                 for (int d = 0; d < DB; ++d)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) o[d][i] *= al;
+                    for (int i = 0; i < 16; ++i) o[d][i] = scaled<kSafe>(o[d][i], al);
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -874,7 +905,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_f32(PromptParams p) {
                     o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, st[i], o[d], 0, 0, 0);
                 }
             }
-            for (int r = 0; kSafe && r < kKeys32; ++r)
+            if (kSafe && any_odd<kKeys32 * D>(vt))
+                for (int r = 0; r < kKeys32; ++r)
 #pragma unroll
                     for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -899,11 +931,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_f32(PromptParams p) {
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) odd = fmaf(o[d][i], 0.f, odd);
-    if (any_wave<kKeys32 * D>((ref.needs_apart(l) || odd != odd) && row < n, lds + kWaves * kKeys32 * D)) {
+    float* const vf = lds + kWaves * kKeys32 * D;
+    const bool again = any_wave<kKeys32 * D>((ref.needs_apart(l) || odd != odd) && row < n, vf);
+    if (again) {
         __syncthreads();
         pass(std::true_type{}, kl, vl);
+        join_waves<D, kKeys32 * D, true>(p, lds, vf, ref, l, o, t, row, h);
+    } else {
+        join_waves<D, kKeys32 * D, false>(p, lds, vf, ref, l, o, t, row, h);
     }
-    join_waves<D, kKeys32 * D>(p, lds, lds + kWaves * kKeys32 * D, ref, l, o, t, row, h);
 }
 
 // Workgroups of a launch whose row tiles hold `rows`.

@@ -1,5 +1,6 @@
 """Packed prompt attention at the ends of what its arguments may hold: scores and
-scales whose products leave float32.  Every form that the batch's shape chooses is reached.
+scales whose products leave float32, infinities and NaN of V under any weight.  Every
+form that the batch's shape chooses is reached.
 """
 import numpy as np
 import pytest
@@ -101,3 +102,48 @@ def test_far_rows_leave_the_others_as_they_are(form, D):
     got = run(serve, q, k, v, bounds(lens), 1.0)
     want = v[:, last].double().repeat_interleave(Hq // Hkv, 0)
     assert ((got[:, last].double() - want).abs() <= 8 * U * want.abs()).all() and got.isfinite().all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("form", FORMS)
+def test_attended_infinities_whatever_their_weight(form, D):
+    """An infinity of V reaches every token that attends to it, one whose weight is
+    exp(-362) too, before and after a key of weight exp(362) has come; infinities of
+    both signs, or a NaN, give NaN; every other output is that of finite values."""
+    serve = need_serve()
+    dtype, Hq, Hkv, lens = FORMS[form]
+    say(f"prompt infinities {form} D={D}")
+    g = torch.Generator().manual_seed(D)
+    T = sum(lens)
+    q = torch.zeros(Hq, T, D)
+    q[:, :, 0] = 64.0
+    k = torch.zeros(Hkv, T, D)
+    v = torch.randn(Hkv, T, D, generator=g)
+    at = 0
+    for n in lens:
+        for low, odd, high in ((3, 20, 35), (130, 160, 250), (1000, 1090, 1151)):
+            if n <= high:
+                break
+            k[:, at + low, 0] = -64.0 * D**0.5 / 11.3
+            v[:, at + low, low % 7] = np.inf
+            v[:, at + low, 9] = -np.inf
+            v[:, at + odd, 9] = np.inf
+            v[:, at + odd, 11 + low % 7] = np.nan
+            k[:, at + high, 0] = 64.0 * D**0.5 / 11.3
+        at += n
+    q, k, v = (x.to(dtype).cuda() for x in (q, k, v))
+    got = run(serve, q, k, v, bounds(lens))
+    fin = v.nan_to_num(0, 0, 0)
+    want = expect(q, k, fin, lens, lambda s: (s * D**-0.5).softmax(1))
+    odd = v - fin                                              # infinities and NaN among zeros
+    odd = torch.where(v.isfinite(), torch.zeros_like(v), v).double()
+    at = 0
+    for n in lens:
+        want[:, at:at + n] += odd[:, at:at + n].cumsum(1).repeat_interleave(Hq // Hkv, 0)
+        at += n
+    assert torch.equal(got.isnan(), want.isnan())
+    inf = want.isinf()
+    assert torch.equal(got[inf].double(), want[inf])
+    ok = want.isfinite()
+    bar = attn_bar(q, k, v, max(lens), D**-0.5, want.nan_to_num(0, 0, 0), dtype, F32)
+    assert ((got.double() - want).abs() <= bar)[ok].all()
