@@ -132,6 +132,9 @@ __device__ __forceinline__ bool any_odd(const float* x) {
 // A sum times a factor that may have fallen to 0; an infinity in it stays (kSafe).
 template <bool kSafe>
 __device__ __forceinline__ float scaled(float x, float a) { return kSafe && !isfinite(x) ? x : x * a; }
+// y + x a, the same way in both passes: finite rows have the same bits in either.
+template <bool kSafe>
+__device__ __forceinline__ float add_scaled(float y, float x, float a) { return kSafe && !isfinite(x) ? y + x : fmaf(x, a, y); }
 
 // A row's reference: the maximum m that its weights 2^((s - m) c) are taken at.  As a
 // rule their exponent is one fma, s c - mc, with mc = m c rounded: the row's weights are
@@ -383,11 +386,11 @@ __global__ __launch_bounds__(64 * kWaves * S, D == 64 ? 3 : 2) void k_prompt_bf1
                 const float m1 = ml[wave][0][lane], mc1 = ml[wave][1][lane], top = fmaxf(ref.m, m1), topc = ref.m < m1 ? mc1 : ref.mc;
                 const bool far = far_ref(ref.mc) || far_ref(mc1);
                 const float a = join_factor(ref.m, ref.mc, top, topc, far, p.c), a1 = join_factor(m1, mc1, top, topc, far, p.c);
-                l = l * a + ml[wave][2][lane] * a1;
+                l = fmaf(ml[wave][2][lane], a1, l * a);
 #pragma unroll
                 for (int d = 0; d < DB; ++d)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) o[d][i] = scaled<kSafe>(o[d][i], a) + scaled<kSafe>(mem[d][64 * i], a1);
+                    for (int i = 0; i < 16; ++i) o[d][i] = add_scaled<kSafe>(scaled<kSafe>(o[d][i], a), mem[d][64 * i], a1);
             }
         }
     };
@@ -412,12 +415,13 @@ __global__ __launch_bounds__(64 * kWaves * S, D == 64 ? 3 : 2) void k_prompt_bf1
 }
 
 // The states of a workgroup's four waves, each over its own keys of the same 32 rows,
-// to the rows' outputs (kSafe: after a second pass).  mem: room for [wave][dim block][register][lane], a wave's in its
-// K tile's place; ml: 256 floats a wave, kTile apart, in its V tile's place.  A wave
-// stores the dims of four registers of every 16 (8 of a row's 32).
+// to the rows' outputs (kSafe: after a second pass).  mem: room for [wave][dim
+// block][register][lane], a wave's in its K tile's place; ml: 256 floats a wave, kTile
+// apart, in its V tile's place.  A wave stores the dims of four registers of every 16 (8 of
+// a row's 32).
 template <int D, int kTile, bool kSafe>
-__device__ __forceinline__ void join_waves(const PromptParams& p, float* mem, float* ml, const Ref& ref, float l, const f32x16_t (&o)[D / 32],
-                                           const RowTile& t, int row, int h) {
+__device__ __forceinline__ void join_waves(const PromptParams& p, float* mem, float* ml, const Ref& ref, float l,
+                                           const f32x16_t (&o)[D / 32], const RowTile& t, int row, int h) {
     constexpr int DB = D / 32;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lh = lane >> 5;
     mem += lane;
@@ -443,7 +447,7 @@ __device__ __forceinline__ void join_waves(const PromptParams& p, float* mem, fl
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
         a[w] = join_factor(ml[w * kTile], ml[w * kTile + 192], top, topc, far, p.c);
-        sum += a[w] * ml[w * kTile + 64];
+        sum = fmaf(a[w], ml[w * kTile + 64], sum);
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     const int64_t at = h * p.o_head + (t.first + row) * p.o_token + 4 * lh + 8 * wave;
@@ -454,7 +458,7 @@ __device__ __forceinline__ void join_waves(const PromptParams& p, float* mem, fl
         for (int i = 0; i < 4; ++i) {
             y[i] = 0.f;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) y[i] += scaled<kSafe>(mem[((w * DB + d) * 16 + 4 * wave + i) * 64], a[w]);
+            for (int w = 0; w < kWaves; ++w) y[i] = add_scaled<kSafe>(y[i], mem[((w * DB + d) * 16 + 4 * wave + i) * 64], a[w]);
         }
         store4(p, at + 32 * d, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
     }

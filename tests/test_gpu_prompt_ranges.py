@@ -147,3 +147,22 @@ def test_attended_infinities_whatever_their_weight(form, D):
     ok = want.isfinite()
     bar = attn_bar(q, k, v, max(lens), D**-0.5, want.nan_to_num(0, 0, 0), dtype, F32)
     assert ((got.double() - want).abs() <= bar)[ok].all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("form", FORMS)
+def test_a_second_pass_leaves_the_bits_of_finite_outputs(form, D):
+    """An infinity in one dimension of a value: the other dimensions, and the tokens before
+    it, have the bits that they have without it."""
+    serve = need_serve()
+    dtype, Hq, Hkv, lens = FORMS[form]
+    g = torch.Generator().manual_seed(D + 1)
+    T = sum(lens)
+    q, k, v = (torch.randn(h, T, D, generator=g).to(dtype).cuda() for h in (Hq, Hkv, Hkv))
+    clean = run(serve, q, k, v, bounds(lens))
+    at = 0
+    for n in lens:
+        v[:, at + n // 2, 5] = np.inf
+        clean[:, at + n // 2:at + n, 5] = np.inf
+        at += n
+    assert torch.equal(run(serve, q, k, v, bounds(lens)), clean)
