@@ -143,6 +143,12 @@ __device__ __forceinline__ float add_scaled(float y, float x, float a) { return 
 // from s - m; other rows keep their bits.
 constexpr float kNearRef = 16777216.f;
 __device__ __forceinline__ bool far_ref(float mc) { return !(fabsf(mc) < kNearRef); }
+// kF32: float32 inputs, where a weight below 2^-126 times a large value counts; the bare
+// instruction gives 0 there.  Weights are the square of the half exponent's power, one
+// product more (with exp2f 5,000 tokens of 32 heads take 959 us instead of 903).
+template <bool kF32>
+__device__ __forceinline__ float pow2(float x) { return kF32 ? exp2f(x) : __builtin_amdgcn_exp2f(x); }
+template <bool kF32>
 struct Ref {
     float m, mc;        // mc: 0 while there is no maximum
     bool apart;         // the row's exponents are taken from differences
@@ -156,11 +162,14 @@ struct Ref {
         const float was = m, wasc = mc;
         m = fmaxf(m, mx);
         mc = m == -INFINITY ? 0.f : m * c;
-        return was == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(kSafe && apart ? (was - m) * c : wasc - mc);
+        return was == -INFINITY ? 0.f : pow2<kF32>(kSafe && apart ? (was - m) * c : wasc - mc);
     }
     template <bool kSafe>
     __device__ __forceinline__ float weight(float s, float c) const {
-        return __builtin_amdgcn_exp2f(kSafe && apart ? (m == -INFINITY ? s : s - m) * c : fmaf(s, c, -mc));
+#pragma clang fp contract(off)              // the square is a number of its own in both passes
+        const float f = kF32 ? 0.5f : 1.f;
+        const float w = __builtin_amdgcn_exp2f(kSafe && apart ? (m == -INFINITY ? s : s - m) * (f * c) : fmaf(s, f * c, -(f * mc)));
+        return kF32 ? w * w : w;
     }
     // After a pass, with the row's sum of weights: references that were far for a while
     // and rose have left a sum that is infinite or NaN.
@@ -171,8 +180,9 @@ struct Ref {
 };
 // The factor of a partial sum under the reference m (mc) where partial sums of one row
 // meet under the largest, top (topc); far: one of theirs is.
+template <bool kF32>
 __device__ __forceinline__ float join_factor(float m, float mc, float top, float topc, bool far, float c) {
-    return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(far ? (m - top) * c : mc - topc);
+    return m == -INFINITY ? 0.f : pow2<kF32>(far ? (m - top) * c : mc - topc);
 }
 
 template <int D, int S>
@@ -221,7 +231,7 @@ __global__ __launch_bounds__(64 * kWaves * S, D == 64 ? 3 : 2) void k_prompt_bf1
     const int tiles = (kend + kKeys - 1) / kKeys;
 
     f32x16_t o[DB];
-    Ref ref;
+    Ref<false> ref;
     float l;
 
     // S^T of a tile: lane l holds query l % 32 at keys 32 b + 8 (i / 4) + 4 (l / 32) + i % 4.
@@ -385,7 +395,7 @@ __global__ __launch_bounds__(64 * kWaves * S, D == 64 ? 3 : 2) void k_prompt_bf1
             if (group == 0) {
                 const float m1 = ml[wave][0][lane], mc1 = ml[wave][1][lane], top = fmaxf(ref.m, m1), topc = ref.m < m1 ? mc1 : ref.mc;
                 const bool far = far_ref(ref.mc) || far_ref(mc1);
-                const float a = join_factor(ref.m, ref.mc, top, topc, far, p.c), a1 = join_factor(m1, mc1, top, topc, far, p.c);
+                const float a = join_factor<false>(ref.m, ref.mc, top, topc, far, p.c), a1 = join_factor<false>(m1, mc1, top, topc, far, p.c);
                 l = fmaf(ml[wave][2][lane], a1, l * a);
 #pragma unroll
                 for (int d = 0; d < DB; ++d)
@@ -419,8 +429,8 @@ __global__ __launch_bounds__(64 * kWaves * S, D == 64 ? 3 : 2) void k_prompt_bf1
 // block][register][lane], a wave's in its K tile's place; ml: 256 floats a wave, kTile
 // apart, in its V tile's place.  A wave stores the dims of four registers of every 16 (8 of
 // a row's 32).
-template <int D, int kTile, bool kSafe>
-__device__ __forceinline__ void join_waves(const PromptParams& p, float* mem, float* ml, const Ref& ref, float l,
+template <int D, int kTile, bool kSafe, bool kF32>
+__device__ __forceinline__ void join_waves(const PromptParams& p, float* mem, float* ml, const Ref<kF32>& ref, float l,
                                            const f32x16_t (&o)[D / 32], const RowTile& t, int row, int h) {
     constexpr int DB = D / 32;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lh = lane >> 5;
@@ -446,7 +456,7 @@ __device__ __forceinline__ void join_waves(const PromptParams& p, float* mem, fl
     }
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-        a[w] = join_factor(ml[w * kTile], ml[w * kTile + 192], top, topc, far, p.c);
+        a[w] = join_factor<kF32>(ml[w * kTile], ml[w * kTile + 192], top, topc, far, p.c);
         sum = fmaf(a[w], ml[w * kTile + 64], sum);
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -528,7 +538,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_narrow(PromptParams p
         for (int s = 0; s < SL; ++s) qf[s] = *reinterpret_cast<const u32x4_t*>(qp + 16 * s);
     }
     f32x16_t o[DB];
-    Ref ref;
+    Ref<false> ref;
     float l;
     const int r0 = 4 * lh + ((lane & 15) >> 2), cq = 2 * (lane >> 4 & 1) + ((lane & 3) >> 1);
     // kSafe: V may hold infinities or NaN
@@ -697,7 +707,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_short(PromptParams p)
         for (int s = 0; s < SL; ++s) qf[s] = *reinterpret_cast<const u32x4_t*>(qp + 16 * s);
     }
     f32x16_t o[DB];
-    Ref ref;
+    Ref<false> ref;
     float l;
     const int r0 = 4 * lh + ((lane & 15) >> 2), cq = 2 * (lane >> 4 & 1) + ((lane & 3) >> 1);
     // kSafe: V may hold infinities or NaN
@@ -849,7 +859,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_f32(PromptParams p) {
         for (int s = 0; s < D / 8; ++s) qf[s] = *reinterpret_cast<const f32x4_t*>(qp + 8 * s);
     }
     f32x16_t o[DB];
-    Ref ref;
+    Ref<true> ref;
     float l;
     // kSafe: V may hold infinities or NaN
     const auto pass = [&](auto safe, float* __restrict__ kt, float* __restrict__ vt) __attribute__((always_inline)) {

@@ -1,6 +1,6 @@
 """Packed prompt attention at the ends of what its arguments may hold: scores and
-scales whose products leave float32, infinities and NaN of V under any weight.  Every
-form that the batch's shape chooses is reached.
+scales whose products leave float32, infinities and NaN of V under any weight, and
+float32 weights below 2^-126.  Every form that the batch's shape chooses is reached.
 """
 import numpy as np
 import pytest
@@ -166,3 +166,25 @@ def test_a_second_pass_leaves_the_bits_of_finite_outputs(form, D):
         clean[:, at + n // 2:at + n, 5] = np.inf
         at += n
     assert torch.equal(run(serve, q, k, v, bounds(lens)), clean)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n,low,high", [(20, 0, None), (20, 0, 7), (200, 1, 70), (200, 40, 130), (200, 150, 10)])
+def test_float32_weights_below_the_normal_range(D, n, low, high):
+    """A weight of exp(-90) on a value of 1e38 counts.  It is a multiple of 2^-149, off by
+    2^-20 of itself; beside that the score's error (as in attn_bar) and the sums'."""
+    serve = need_serve()
+    q = torch.zeros(2, n, D)
+    q[:, :, 0] = 1.0
+    k = torch.zeros(1, n, D)
+    if high is None:
+        k[0, low, 0] = -90.0
+    else:
+        k[0, high, 0] = 90.0                                   # the others fall to exp(-90)
+    v = torch.zeros(1, n, D)
+    v[0, low] = 1e38
+    q, k, v = (x.cuda() for x in (q, k, v))
+    got = run(serve, q, k, v, bounds([n]), 1.0)
+    want = expect(q, k, v, [n], lambda s: s.softmax(1))
+    rel = 2 * (D + 4) * U * 90 + (2 * n + 64) * U + 2.0**-19
+    assert ((got.double() - want).abs() <= rel * want).all()
