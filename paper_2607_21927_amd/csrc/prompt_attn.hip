@@ -499,7 +499,7 @@ __device__ __forceinline__ bool any_wave(bool x, float* mem) {
 // are restrict parameters, and one shared array in the kernel (two have marks of their
 // own, which these replace).  4 to 10% for one prompt of 1,500 to 3,000 tokens.
 template <int D>
-__global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_narrow(PromptParams p) {
+__global__ __launch_bounds__(64 * kWaves, D == 128 ? 1 : 2) void k_prompt_narrow(PromptParams p) {
     constexpr int SL = D / 16, DB = D / 32, C = D / 8;
     constexpr int kPieces = kKeys * C / 64, kPer = 64 / C;        // 16-byte pieces of a lane, rows of a piece
     __shared__ __align__(16) uint16_t lds[2 * kWaves * kKeys * D];
@@ -820,7 +820,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_short(PromptParams p)
 constexpr int kKeys32 = 32;
 
 template <int D>
-__global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_f32(PromptParams p) {
+__global__ __launch_bounds__(64 * kWaves, D == 128 ? 1 : 2) void k_prompt_f32(PromptParams p) {
     constexpr int DB = D / 32, C = D / 4;
     constexpr int kPieces = kKeys32 * C / 64, kPer = 64 / C;
     __shared__ __align__(16) float lds[2 * kWaves * kKeys32 * D];
