@@ -2,13 +2,15 @@
 // the merge of its partials.
 #pragma once
 
+#include <float.h>
+
 #include "ris_device.h"
 #include "ris_internal.h"
 
 namespace ris {
 namespace {
 
-constexpr float kNegBig = -1e30f;   // finite start of the running max
+constexpr float kNegBig = -1e30f;   // finite start of ris_decode_attn's running max
 
 struct RowSegs {
     int64_t na, nw, ns;   // anchor entries, window keys, initial keys below the window
@@ -64,6 +66,13 @@ __device__ __forceinline__ void store_out(const DecodeParams& p, int64_t at, flo
         static_cast<float*>(p.out)[at] = y;
 }
 
+// The factor of a sum under the running maximum m where it meets others under M >= m: 2^((m
+// - M) unit), the unit being log2 of the weight that 1 in the maxima stands for.  Maxima
+// start finite: where nothing is summed any factor will do.
+__device__ __forceinline__ float merge_factor(const DecodeParams& p, float m, float M) {
+    return __builtin_amdgcn_exp2f((m - M) * p.unit);
+}
+
 // A workgroup's partial: its waves' states merged in LDS (`ow`: kDecodeWaves * G *
 // D floats, which the waves may still be reading as something else, hence the
 // first barrier).  Lane l holds head l % 16's running maximum and its quarter of
@@ -99,7 +108,7 @@ __device__ __forceinline__ void merge_waves(const DecodeParams& p, int row, floa
         float O = 0.f, L = 0.f;
 #pragma unroll
         for (int w = 0; w < kDecodeWaves; ++w) {
-            const float c = __builtin_amdgcn_exp2f(ml[w][h].x - M);
+            const float c = merge_factor(p, ml[w][h].x, M);
             O += c * ow[w * G * D + e];
             L += c * ml[w][h].y;
         }
@@ -135,7 +144,7 @@ __global__ __launch_bounds__(kCombineThreads) void k_decode_combine(DecodeParams
     const int64_t step_ml = p.G, step_o = (int64_t)p.G * D;
     const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + row * parts * step_ml + hh;
     const float* po = p.part_o + row * parts * step_o + (int64_t)hh * D;
-    float M = kNegBig;
+    float M = -FLT_MAX;
     for (int i = tid; i < parts; i += kCombineThreads) M = fmaxf(M, ml[i * step_ml].x);
     M = wave_max(M);
     if (lane == 0) red[wv][0] = M;
@@ -145,7 +154,7 @@ __global__ __launch_bounds__(kCombineThreads) void k_decode_combine(DecodeParams
     float L = 0.f;
     for (int i = tid; i < parts; i += kCombineThreads) {
         const float2 x = ml[i * step_ml];
-        const float w = __builtin_amdgcn_exp2f(x.x - M);
+        const float w = merge_factor(p, x.x, M);
         wgt[i] = w;
         L += w * x.y;
     }

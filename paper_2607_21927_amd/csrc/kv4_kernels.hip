@@ -203,7 +203,7 @@ __device__ __forceinline__ void load_tile(const RowSegs& r, const uint8_t* Kr, c
 }
 
 template <int D>
-__global__ __launch_bounds__(64 * kDecodeWaves, 4) void k_kv4_decode(DecodeParams p, const uint8_t* S, float c) {
+__global__ __launch_bounds__(64 * kDecodeWaves, 4) void k_kv4_decode(DecodeParams p, const uint8_t* S, float slack) {
     constexpr int SL = D / 32;         // k-slices of the score product
     constexpr int DB = D / 16;         // 16-dim blocks of the output
     constexpr int VS = D + 16;         // V row stride in LDS (bf16 elements)
@@ -242,7 +242,8 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 4) void k_kv4_decode(DecodeParam
     f32x4_t o[DB];
 #pragma unroll
     for (int db = 0; db < DB; ++db) o[db] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    float m_run = kNegBig, l_run = 0.f;
+    const float c = p.unit;
+    float m_run = -FLT_MAX, l_run = 0.f;        // maximum in scores: times c it may leave float32
 
     const int64_t v_first = part * kTileKeys;
     if (v_first < total) {
@@ -275,7 +276,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 4) void k_kv4_decode(DecodeParam
             // the next tile's codes take the registers that these have left
             if (v0 + stride < total) load_tile<D>(r, Kr, Vr, Sr, v0 + stride, li, lg, cur);
 
-            // Online softmax over the tile (scores in the log2 domain).
+            // Online softmax over the tile.
             float sc[2][4];
             float mx = -INFINITY;
 #pragma unroll
@@ -283,15 +284,15 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 4) void k_kv4_decode(DecodeParam
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const bool ok = (valid >> (16 * kb + 4 * lg + i)) & 1u;
-                    sc[kb][i] = ok ? st[kb][i] * c : -INFINITY;
+                    sc[kb][i] = ok ? st[kb][i] : -INFINITY;
                     mx = fmaxf(mx, sc[kb][i]);
                 }
             mx = quad_max16(mx);
             // The reference moves, and what was summed is rescaled, only where a score
             // exceeds it by 2^8 in weight.
-            if (__any(mx > m_run + 8.f)) {
+            if (__any(mx > m_run + slack)) {
                 const float m_new = fmaxf(m_run, mx);
-                const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+                const float alpha = merge_factor(p, m_run, m_new);
                 m_run = m_new;
                 l_run *= alpha;
                 // lane l holds the output of heads 4 (l / 16) + i
@@ -307,7 +308,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 4) void k_kv4_decode(DecodeParam
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    pv[kb][i] = __builtin_amdgcn_exp2f(sc[kb][i] - m_run);
+                    pv[kb][i] = __builtin_amdgcn_exp2f((sc[kb][i] - m_run) * c);
                     l_run += pv[kb][i];
                 }
 
@@ -331,10 +332,11 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 4) void k_kv4_decode(DecodeParam
 }
 
 template <int D>
-hipError_t launch_d(const DecodeParams& p, const uint8_t* S, float c, hipStream_t st) {
+hipError_t launch_d(const DecodeParams& p, const uint8_t* S, hipStream_t st) {
     const dim3 grid((unsigned)(p.parts / kDecodeWaves), (unsigned)(p.B * p.Hkv));
     if (p.parts % kDecodeWaves != 0 || p.parts > kDecodeMaxParts) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(k_kv4_decode<D>, grid, dim3(64 * kDecodeWaves), 0, st, p, S, c);
+    hipLaunchKernelGGL(k_kv4_decode<D>, grid, dim3(64 * kDecodeWaves), 0, st, p, S,
+                       fminf(8.0f / p.unit, FLT_MAX));
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || grid.x == 1) return e;
     return launch_decode_combine<D>(p, st);
@@ -361,8 +363,7 @@ hipError_t launch_kv4_load(const Kv4Params& p, hipStream_t st) {
 }
 
 hipError_t launch_kv4_decode(const DecodeParams& p, const uint8_t* S, hipStream_t st) {
-    const float c = p.scale * 1.4426950408889634f;   // scores in the log2 domain
-    return p.D == 128 ? launch_d<128>(p, S, c, st) : launch_d<64>(p, S, c, st);
+    return p.D == 128 ? launch_d<128>(p, S, st) : launch_d<64>(p, S, st);
 }
 
 }  // namespace ris

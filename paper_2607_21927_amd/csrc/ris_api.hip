@@ -466,6 +466,7 @@ int ris_decode_attn(const void* Q, const void* K, const void* V, const int64_t* 
     p.out_bf16 = d.dtype_out == RIS_BF16;
     p.window = d.window; p.sink = d.sink;
     p.keep_nan = 0;
+    p.unit = 1.0f;
     p.parts = (int32_t)decode_waves(d);
     // a row holds max_len keys at most: no overflow for any descriptor
     const int64_t keys = decode_keys(d) < d.max_len ? decode_keys(d) : d.max_len;

@@ -116,6 +116,7 @@ struct DecodeParams {
     int64_t kv_bytes;             // K and V bytes of a step, estimated as for `parts`
     int32_t parts;                // waves per row (a multiple of kDecodeWaves)
     float scale;
+    float unit;                   // log2 of the weight that 1 in the running maxima stands for
 };
 hipError_t launch_decode(const DecodeParams& p, hipStream_t st);
 

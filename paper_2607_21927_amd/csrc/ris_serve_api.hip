@@ -225,6 +225,7 @@ int ris_kv4_decode_attn(const void* Q, const uint8_t* K4, const uint8_t* V4, con
     p.parts = (int32_t)kv4_decode_waves(d);
     p.kv_bytes = 0;
     p.scale = d.scale > 0.0f ? d.scale : 1.0f / sqrtf((float)d.D);
+    p.unit = p.scale * kLog2e;
     p.part_o = static_cast<float*>(workspace);
     p.part_ml = p.part_o + (int64_t)d.batch * d.Hq * (p.parts / ris::kDecodeWaves) * d.D;
     return hip_status(ris::launch_kv4_decode(p, S, static_cast<hipStream_t>(stream)));
