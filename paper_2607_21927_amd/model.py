@@ -264,13 +264,8 @@ class KV4Cache:
         self.max_len = max_len
         self.layers = [serve.kv4_cache(batch, cfg.kv_heads, max_len, cfg.head_dim, model.device) for _ in model.layers]
         self.cu = torch.arange(batch + 1, dtype=torch.int64, device=model.device)   # one token a sequence
-        self._ws = {}
 
     def workspace(self, desc):
-        """Device scratch of the decode step: steps of one cache follow each other and
-        share it, one buffer a size, none of which moves while a captured step may
-        hold its address."""
-        n = serve.kv4_decode_workspace_bytes(desc)
-        if n not in self._ws:
-            self._ws[n] = torch.empty(n, dtype=torch.uint8, device=self.cu.device)
-        return self._ws[n]
+        """Device scratch of one decode call, of its own: steps on two streams, or in two
+        captured graphs that are replayed side by side, do not meet in it."""
+        return torch.empty(serve.kv4_decode_workspace_bytes(desc), dtype=torch.uint8, device=self.cu.device)

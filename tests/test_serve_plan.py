@@ -1,7 +1,9 @@
 """What the serving path plans on the host: workspaces (no GPU needed)."""
 import os
+from types import SimpleNamespace
 
 import pytest
+import torch
 
 
 @pytest.fixture(scope="module")
@@ -11,6 +13,21 @@ def serve():
         _build.build()
     s.lib()
     return s
+
+
+def test_calls_that_overlap_have_scratch_of_their_own(serve):
+    """Two steps over one cache, on two streams or in two captured graphs, must not write
+    their partial results to one place."""
+    from paper_2607_21927_amd.model import PrefillModel
+    cfg = SimpleNamespace(kv_heads=2, head_dim=128)
+    cache = PrefillModel.kv4_cache(SimpleNamespace(cfg=cfg, device="cpu", layers=[0]), 2, 4096)
+    Q = torch.zeros(2, 12, 128, dtype=torch.bfloat16)
+    desc = serve.kv4_decode_desc(Q, cache.layers[0][0], Q, window=4096)
+    a, b = cache.workspace(desc), cache.workspace(desc)
+    need = serve.kv4_decode_workspace_bytes(desc)
+    assert need > 0 and a.numel() >= need and b.numel() >= need
+    assert a.data_ptr() + a.numel() <= b.data_ptr() or b.data_ptr() + b.numel() <= a.data_ptr()
+    assert a.data_ptr() % 16 == 0
 
 
 @pytest.mark.parametrize("rows", [1, 1000, 1024, 4096, 100_000])
