@@ -138,7 +138,7 @@ class PrefillModel:
 
     def kv4_cache(self, batch, max_len):
         """A 4-bit key/value cache for ``batch`` sequences of up to ``max_len``
-        tokens, one (K4, V4, S) per layer, with what the steps over it reuse."""
+        tokens, one (K4, V4, S) per layer."""
         return KV4Cache(self, batch, max_len)
 
     def _packed_qkv(self, h, layer, cu_seqlens, rope_desc, start):
@@ -209,16 +209,19 @@ class PrefillModel:
         """
         cfg = self.cfg
         B, D, Hq = ids.shape[0], cfg.head_dim, cfg.heads
+        if ids.shape != (cache.batch,) or pos.numel() != B:
+            raise ValueError(f"ids and pos must hold one entry for each of the cache's {cache.batch} sequences")
 
         def attention(l, layer, h):
             q, k, v = self._packed_qkv(h, layer, cache.cu, rope_desc, pos)
-            serve.kv4_store(k, v, cache.cu, *cache.layers[l], start=pos)
             ptr, idx = anchors[l] if anchors is not None else (None, None)
             q = q.transpose(0, 1).contiguous()
             out = torch.empty(B, Hq, D, dtype=h.dtype, device=h.device)
             desc = serve.kv4_decode_desc(q, cache.layers[l][0], out, idx.shape[1] if idx is not None else 0,
                                          window=cache.max_len if window is None else window, sink=sink)
-            serve.kv4_decode_attn(q, *cache.layers[l], pos, ptr, idx, out, cache.workspace(desc), desc)
+            workspace = cache.workspace(desc)              # refuses what the step cannot do before the cache changes
+            serve.kv4_store(k, v, cache.cu, *cache.layers[l], start=pos)
+            serve.kv4_decode_attn(q, *cache.layers[l], pos, ptr, idx, out, workspace, desc)
             return out.view(B, Hq * D)
 
         return self._stack(ids, attention)
@@ -261,7 +264,7 @@ class KV4Cache:
 
     def __init__(self, model, batch, max_len):
         cfg = model.cfg
-        self.max_len = max_len
+        self.batch, self.max_len = batch, max_len
         self.layers = [serve.kv4_cache(batch, cfg.kv_heads, max_len, cfg.head_dim, model.device) for _ in model.layers]
         self.cu = torch.arange(batch + 1, dtype=torch.int64, device=model.device)   # one token a sequence
 

@@ -30,6 +30,17 @@ def test_calls_that_overlap_have_scratch_of_their_own(serve):
     assert a.data_ptr() % 16 == 0
 
 
+def test_steps_of_another_batch_are_refused(serve):
+    """Before the cache takes anything."""
+    from paper_2607_21927_amd.model import PrefillModel
+    cfg = SimpleNamespace(kv_heads=2, head_dim=128, heads=12)
+    model = SimpleNamespace(cfg=cfg, device="cpu", layers=[0])
+    cache = PrefillModel.kv4_cache(model, 2, 64)
+    for ids, pos in (([1, 2, 3], [0, 0, 0]), ([1], [0]), ([1, 2], [0, 0, 0])):
+        with pytest.raises(ValueError, match="2 sequences"):
+            PrefillModel.decode_step(model, torch.tensor(ids), torch.tensor(pos), cache)
+
+
 @pytest.mark.parametrize("rows", [1, 1000, 1024, 4096, 100_000])
 @pytest.mark.parametrize("bits", [24, 25, 26, 28, 31])
 def test_wide_rows_are_cut_into_parts(serve, rows, bits):
