@@ -11,7 +11,8 @@
 // their dimensions in the order in which the codes lie: lane group l / 16 owns the
 // D / 4 dimensions from (l / 16) D / 4 on, 16 bytes of codes (D = 128) under one
 // scale, and Q is loaded in the same order.  V rows are read whole, become bf16 in
-// wave-private LDS and come back transposed.
+// wave-private LDS and come back transposed.  Weights enter the PV product as bf16, as in
+// that pass: off by 2^-8 of themselves at most, their sum taken in float32 before that.
 #include "decode_rows.h"
 #include "packed.h"
 

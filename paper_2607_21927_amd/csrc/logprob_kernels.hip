@@ -5,7 +5,7 @@
 // the entropy is log(sum) - sum(exp(x - m) (x - m)) / sum.
 //
 // HBM-bound, and close to it by VALU: 16-byte loads, the exponent's argument as one
-// fma in the log2 domain, and a list that few logits reach (see `threshold`).  A row
+// fma in the log2 domain, and a list that few logits reach (see `start_at`).  A row
 // is cut into parts where rows are few; each part's workgroup leaves its state and
 // list in the workspace, and one wave a row merges them.
 #include <float.h>

@@ -18,10 +18,16 @@
 // once more, with such elements of V taken out of the tiles and added, whatever their
 // weight, where they are attended to.  So does one with a reference far from 0 (see Ref).
 //
-// Bound by how well the matrix unit (54% busy) and the vector unit (~45%) share the
-// time of two waves a SIMD at 1.9 GHz; LDS is at 27%, without bank conflicts.  At D =
+// Weights enter the PV product as bf16, the type in which the matrix unit takes V (a
+// product in float32 would be 16 times slower): each is off by 2^-8 of itself at most, their
+// sum is taken in float32 before that.  Nine prompts of 32k tokens are off by 2.1e-3 of the
+// outputs' norm, of which rounding the outputs to bf16 alone makes 1.6e-3.
+//
+// Bound by how well the matrix unit and the vector unit share the waves' time: one prompt
+// of 32k tokens keeps them 61% and 39% busy at D = 128 (two waves a SIMD, 1.07 PFLOP/s), 49%
+// and 58% at D = 64 (three), LDS 30% and 24%, without bank conflicts, at 1.8 GHz.  At D =
 // 128 the next tile's scores stand beside this one's exponentials in one block, the
-// products and reads spread through it (1071 -> 1106 TFLOP/s for 12/2 heads at 32k
+// products and reads spread through it (1071 -> 1106 TFLOP/s on one machine, 12/2 heads, 32k
 // tokens); at D = 64, where exponentials take longer than products, three waves a
 // SIMD without that gain more (975 against 937).  Not kept: row sums on v_dot2 (the
 // same), the next maximum carried along (the same), raised priority in the PV product
@@ -656,7 +662,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 128 ? 1 : 2) void k_prompt_narrow
 // first token on, so that tiles stay full however short prompts are.  A wave takes one
 // tile of one head by itself (heads of a tile side by side on one XCD), 32 keys at a
 // time from its rows' first to their last, K and V as in the narrow form.  10,000 prompts
-// of 8 tokens (12/2 heads of 128) take 199 us, 1.7 times a copy of their bytes.
+// of 8 tokens (12/2 heads of 128) take 175 us, 1.5 times a copy of their bytes.
 constexpr int kShortKeys = 32;
 
 template <int D>
@@ -815,8 +821,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_short(PromptParams p)
 // four dims of a key from one 16-byte read (lane half lh: dims 8 s + 4 lh ..), the PV
 // product score register i as it stands (its two contraction slots are the keys of
 // the lane halves).  16-byte chunk c of row r lies in place c ^ (r % 16).  Bound by the
-// matrix unit on many rows (111 of a large product's 154 TFLOP/s for 32 heads of 5,000
-// tokens), by the unequal lengths of few workgroups on less (71 for 4 heads).
+// matrix unit on many rows (75% busy, 113 of a large product's 154 TFLOP/s for 32 heads
+// of 5,000 tokens), by the unequal lengths of few workgroups on less (71 for 4 heads).
 constexpr int kKeys32 = 32;
 
 template <int D>
@@ -962,23 +968,35 @@ int64_t blocks_of(const PromptParams& p, int rows) {
 }
 
 // The narrow form while its workgroups are resident at once (one a CU at D = 128, two
-// at D = 64) and prompts are longer than a tile of keys: 12/2 heads, one prompt of
-// 256 tokens 8.2 against 10.8 us at D = 128 and 6.1 against 8.0 at D = 64, of 512 11.2
-// against 15.3 and 7.7 against 11.1; two of 512, more than fit, 18.5 against 15.9.
+// at D = 64) and prompts are longer than a tile of keys.  Below the limit and above it,
+// against the 128-row form, us: D = 128, 12/2 heads, one prompt of 512 tokens (192
+// workgroups) 9.9 and 16.0; 32/8 heads, of 256 (256) 7.9 and 11.4, of 320 (320) 12.9 and
+// 11.6; 16/16 heads, of 512 (256) 10.0 and 16.0; D = 64, 32/4 heads, of 512 (512) 7.8 and
+// 11.1, of 800 (832) 14.0 and 13.9.  Few heads of longer prompts would gain beyond it too
+// (4/1 heads, one of 3,264: 31 and 49); several prompts lose there (two of 512, 12/2 heads:
+// 18.5 and 15.9).
 bool narrow(const PromptParams& p) { return p.T > (int64_t)p.batch * kKeys && blocks_of(p, kNarrowRows) <= (p.D == 128 ? 256 : 512); }
 
 // Two groups of waves where long prompts' workgroups do not fill the chip and the
-// longest bounds the time: one prompt of 2,048 35 against 42 us, of 4,096 69 against
-// 86, of 8,192 (768 workgroups) 226 against 209; eight of 512 25 against 20.
+// longest bounds the time.  With them and without, us: one prompt, 12/2 heads of 128, 4,096
+// tokens (384 workgroups) 71 and 88, 5,120 (480) 98 and 113, 6,144 (576) 143 and 144, 6,784
+// (636) 170 and 166; 32/4 heads of 64, 1,664 (416) 25.5 and 29.1, 2,048 (512) 32.7 and 34.6,
+// 2,304 (576) 43.7 and 39.7.  Several prompts turn earlier: 12/2 heads of 128, four of 1,024
+// (420) 32.9 and 31.5, three of 1,600 (480) 47.8 and 44.8, seven of 600 (480) 29.9 and 23.3;
+// 32/4 heads of 64, two of 900 (512) 22.9 and 19.6.  The limit lies between the two.
 bool split(const PromptParams& p) { return p.T >= (int64_t)p.batch * 512 && blocks_of(p, kRows) <= 440; }
 
 // The short form for prompts of a tile of keys or less in the mean that are more than the
-// 128-row form's workgroups resident at once.  12/2 heads of 128: 64 prompts of 30 tokens
-// 9.6 against 14.0 us, 500 of 20 27 against 65, of 64 73 against 100, 10,000 of 8 199
-// against 1225; 32/4 heads of 64: 32 of 20 6.5 against 10.5, 500 of 20 32 against 92.
-// Fewer: 32 of 20 (12/2 heads, 384 workgroups) 8.2 against 7.4; longer: 32 of 100 16.8
-// against 13.3.  A long prompt among them costs (one of 10,000 and 499 of 20: 520 against
-// 363), which the host does not see.
+// 128-row form's workgroups resident at once.  With it and without, us: 12/2 heads of 128,
+// 42 prompts of 20 tokens (576 workgroups) 9.1 and 12.4, 500 of 20 27 and 66, of 64 70 and
+// 83, 10,000 of 8 175 and 1,219; 32/4 heads of 64, 500 of 20 32 and 92.  Fewer: 21 of 20
+// (288) 8.9 and 7.5; longer: 64 of 100 23.9 and 24.2.  One head to a group, which shares
+// nothing there, turns later: 16/16 heads of 128, 32 of 20 (576) 8.9 and 8.1, of 60 (736)
+// 12.8 and 10.2, 93 of 20 (1,712) 11.0 and 18.6.
+// A long prompt among them, which the host does not see, costs the more the longer it is,
+// each wave reading its keys for 32 rows alone: 12/2 heads of 128, one of 10,000 and 499 of
+// 20 513 and 363, of 30,000 and 1,000 of 20 4,190 and 2,580, of 63,000 and 1,000 of one token,
+// the longest that this rule takes beside 1,000 others, 28,000 and 10,900.
 bool brief(const PromptParams& p) { return p.batch > 1 && p.T <= (int64_t)p.batch * kKeys && blocks_of(p, kRows) > 512; }
 int64_t brief_blocks(const PromptParams& p) {
     const int64_t tiles = ((p.T + kShortRows - 1) / kShortRows + 7) / 8;       // of an XCD

@@ -104,6 +104,9 @@ int validate_kv4_decode(const ris_decode_desc* d) {
 // are fastest with 2048 (64 rows of 65,536 keys 105 us with 2048, 110 with 4096, 111 with
 // 8192), rows of lengths between a quarter and all of that with 8192 (87, 81, 80).  A row
 // takes kMostWaves at most (2 rows of 33,000 keys: 11.9 us, 12.9 with twice as many).
+// Positions are on the device, so this counts what the cache may hold: sequences of 500
+// tokens (12/2 heads of 128) take 7.1 us for one and 8.6 for 32 in a cache of 516 rows, 8.1
+// and 11.1 in one of 65,536.
 constexpr int64_t kSoloTiles = 16, kWaves = 4096, kMostWaves = 512;
 int64_t kv4_decode_waves(const ris_decode_desc& d) {
     const int64_t win = d.window < d.max_len ? d.window : d.max_len;
