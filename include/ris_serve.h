@@ -77,9 +77,10 @@ typedef struct {
  * of them, causal = 0).  What lies in keys and values that a token does not
  * attend to, infinities and NaN included, does not reach its output; an infinity
  * of V that it attends to does, whatever its weight (with one of the other sign
- * or a NaN: NaN).  float32 accumulation; with bf16 inputs the softmax weights
- * enter the PV product rounded to bf16, those below 2^-126 as 0.  out must not
- * overlap the inputs, and its rows must not overlap each other.
+ * or a NaN: NaN).  A token whose scores are -inf alone gets NaN.  float32
+ * accumulation; with bf16 inputs the softmax weights enter the PV product
+ * rounded to bf16, those below 2^-126 as 0.  out must not overlap the inputs, and
+ * its rows must not overlap each other.
  */
 int ris_prompt_attn(const void* Q, const void* K, const void* V, const int64_t* cu_seqlens, void* out,
                     const ris_prompt_desc* desc, void* stream);

@@ -421,7 +421,7 @@ __global__ __launch_bounds__(64 * kWaves * S, D == 64 ? 3 : 2) void k_prompt_bf1
     }
     l = pair_sum32(l);
     if (row >= n || group != 0) return;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float inv = 1.f / l;              // every score -inf: 0 / 0, NaN
     const int64_t at = h * p.o_head + (t.first + row) * p.o_token + 4 * lh;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
@@ -465,7 +465,7 @@ __device__ __forceinline__ void join_waves(const PromptParams& p, float* mem, fl
         a[w] = join_factor<kF32>(ml[w * kTile], ml[w * kTile + 192], top, topc, far, p.c);
         sum = fmaf(a[w], ml[w * kTile + 64], sum);
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const float inv = 1.f / sum;            // every score -inf: 0 / 0, NaN
     const int64_t at = h * p.o_head + (t.first + row) * p.o_token + 4 * lh + 8 * wave;
 #pragma unroll
     for (int d = 0; d < DB; ++d) {
@@ -806,7 +806,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_prompt_short(PromptParams p)
     if (__any((ref.needs_apart(l) || odd != odd) && in)) pass(std::true_type{}, kl, vl);
     l = pair_sum32(l);
     if (!in) return;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float inv = 1.f / l;              // every score -inf: 0 / 0, NaN
     const int64_t at = h * p.o_head + t * p.o_token + 4 * lh;
 #pragma unroll
     for (int d = 0; d < DB; ++d)

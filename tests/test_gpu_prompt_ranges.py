@@ -188,3 +188,28 @@ def test_float32_weights_below_the_normal_range(D, n, low, high):
     want = expect(q, k, v, [n], lambda s: s.softmax(1))
     rel = 2 * (D + 4) * U * 90 + (2 * n + 64) * U + 2.0**-19
     assert ((got.double() - want).abs() <= rel * want).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("form", FORMS)
+def test_infinite_scores(form, D):
+    """Scores of -inf have no weight; tokens that attend to nothing else, or to a score of
+    +inf, have no softmax: NaN, as the formula gives."""
+    serve = need_serve()
+    dtype, Hq, Hkv, lens = FORMS[form]
+    g = torch.Generator().manual_seed(D + 2)
+    T = sum(lens)
+    q, k, v = (torch.randn(h, T, D, generator=g) for h in (Hq, Hkv, Hkv))
+    q[..., 0] = 1.0
+    at = 0
+    for n in lens:
+        k[:, at:at + min(3, n), 0] = -np.inf
+        if n > 30:
+            k[:, at + n - 2, 0] = np.inf
+        at += n
+    q, k, v = (x.to(dtype).cuda() for x in (q, k, v))
+    got = run(serve, q, k, v, bounds(lens)).double()
+    want = expect(q, k, v, lens, lambda s: (s * D**-0.5).softmax(1))
+    assert want.isnan().any() and torch.equal(got.isnan(), want.isnan())
+    bar = attn_bar(q, k, v, max(lens), D**-0.5, want.nan_to_num(0), dtype, F32)
+    assert ((got - want).abs() <= bar)[~want.isnan()].all()
