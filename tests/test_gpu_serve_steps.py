@@ -60,3 +60,33 @@ def test_anchored_steps_match_float64(name, window, sink):
         rel = np.linalg.norm(h[b] - want) / np.linalg.norm(want)
         say(f"  sequence {b}: relative {rel:.4f} (bar {bar:.4f})")
         assert rel <= bar
+
+
+def test_captured_steps():
+    """A step captured once and replayed as tokens and positions move on, with eager steps
+    over the same cache and a second captured step in between."""
+    need_serve()
+    lens, L = [30, 5, 17], 64
+    cfg, W, ids, rd, model = setup("tiny_qwen2", torch.bfloat16, lens)
+    cache = model.kv4_cache(3, L)
+    model.prefill_packed(torch.tensor(ids, device="cuda"), bounds(lens), rd, cache=cache)
+    tok, pos = torch.tensor([3, 4, 5], device="cuda"), torch.tensor(lens, device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        model.decode_step(tok, pos, cache, rd)
+    torch.cuda.current_stream().wait_stream(s)
+    torch.cuda.synchronize()
+    graphs, outs = [torch.cuda.CUDAGraph() for _ in range(2)], []
+    for g in graphs:
+        with torch.cuda.graph(g):
+            outs.append(model.decode_step(tok, pos, cache, rd))
+    for step in range(4):
+        graphs[step % 2].replay()
+        torch.cuda.synchronize()
+        got = outs[step % 2].clone()
+        want = model.decode_step(tok, pos, cache, rd)          # stores the same row again
+        torch.cuda.synchronize()
+        assert torch.equal(got, want), step
+        tok.add_(7).remainder_(cfg.vocab)
+        pos.add_(1)
