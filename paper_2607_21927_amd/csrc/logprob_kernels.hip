@@ -8,8 +8,6 @@
 // fma in the log2 domain, and a list that few logits reach (see `start_at`).  A row
 // is cut into parts where rows are few; each part's workgroup leaves its state and
 // list in the workspace, and one wave a row merges them.
-#include <float.h>
-
 #include "ris_device.h"
 #include "ris_internal.h"
 
@@ -35,13 +33,6 @@ __device__ __forceinline__ uint32_t order_of(float x) {
 __device__ __forceinline__ float ordered(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u); }
 __device__ __forceinline__ uint64_t key_of(float x, uint32_t id) { return (uint64_t)order_of(x) << 32 | (uint32_t)~id; }
 constexpr uint64_t kNothing = 0x007FFFFFull << 32 | 0xFFFFFFFFull;   // -inf: keys up to here are not listed
-
-// A logit below which none has a key above `least`.  (The order just below 0's would be
-// -0, which is not below 0: a lower logit stands for it.)
-__device__ __forceinline__ float floor_of(uint64_t least) {
-    const uint32_t u = (uint32_t)(least >> 32);
-    return u == 0x7FFFFFFFu ? -FLT_MIN : ordered(u);
-}
 
 struct State {
     float m, l, u;      // maximum, sum of exp(x - m), sum of exp(x - m) (x - m)
@@ -193,7 +184,7 @@ __global__ __launch_bounds__(kThreads) void k_logprob(LogprobParams p) {
     float m = -INFINITY, b = 0.f;           // running maximum; times log2 e where that is a weight's reference, else 0
     float l = 0.f, u = 0.f;                 // sums of 2^d and of 2^d d, d = x log2 e - b
     uint64_t list = 0, least = kNothing;
-    float above = -INFINITY;                // floor_of(least)
+    float above = -INFINITY;                // least's logit
     const auto take = [&](const float* x, int n, uint32_t id) {
         float top = x[0];
 #pragma unroll
@@ -220,18 +211,19 @@ __global__ __launch_bounds__(kThreads) void k_logprob(LogprobParams p) {
             for (int i = 0; i < n; ++i)
                 if (__any(!(x[i] < above))) {
                     insert(list, least, key_of(x[i], id + i), k);
-                    above = floor_of(least);
+                    above = ordered((uint32_t)(least >> 32));
                 }
             if (lane == 0) shares[wave] = (uint32_t)(lane_value(list, share - 1) >> 32);
         }
     };
     // Start the list above the orders below t: at least k tokens of the part are known
-    // to lie at t or above, and t's own logits enter.
+    // to lie at t or above, and t's own logits enter.  (The order just below 0's is -0's,
+    // which as a number is not below 0: that list starts above -2^-126.)
     const auto start_at = [&](uint32_t t) {
-        const uint64_t start = ((uint64_t)t << 32) - 1;
+        const uint64_t start = ((uint64_t)(t == 0x80000000u ? 0x7F800000u : t) << 32) - 1;
         if (t && start > least) {
             least = start;
-            above = floor_of(least);
+            above = ordered((uint32_t)(least >> 32));
         }
     };
 
