@@ -358,7 +358,7 @@ const char* ris_status_string(int status);
  * host-model layers (RMSNorm, SwiGLU); 2.3 the strided rotation
  * ris_rope_from; 2.4 changed the draws' round function (the same descriptor
  * now yields different, equally distributed sets); 2.5 the serving operators of
- * ris_serve.h. */
+ * ris_serve.h; 2.6 its cache in pages and weights in 4 bits. */
 int ris_version(void);
 
 #ifdef __cplusplus

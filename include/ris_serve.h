@@ -2,7 +2,8 @@
  * ris_serve.h -- serving operators around the RIS hot path (C ABI, same
  * library and conventions as ris.h): prompts of different lengths packed into
  * one batch, a key/value cache held in 4 bits with the Hybrid-Anchor decode
- * step over it, and log probabilities of given tokens.
+ * step over it, log probabilities of given tokens, a cache in pages with the
+ * attention of new tokens over it, and products with weights in 4 bits.
  *
  * As in ris.h every call is asynchronous on the given HIP stream, arguments
  * are validated on the host before anything is launched, the caller owns every
@@ -183,6 +184,143 @@ int64_t ris_logprobs_workspace_bytes(const ris_logprob_desc* desc);
 int ris_logprobs(const void* logits, const int64_t* targets, float* logprob, float* entropy, int64_t* top_ids,
                  float* top_logprob, void* workspace, int64_t workspace_bytes, const ris_logprob_desc* desc,
                  void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Cache in pages                                                           */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * Keys and values of many sequences in pages of `page` tokens that a block table
+ * names: position j of sequence b lies in page table[b, j / page], slot j % page,
+ *
+ *   Kp, Vp: [pages, Hkv, page, D], page_stride elements between pages;
+ *   table:  int32 [batch, max_pages], table_stride entries between rows.
+ *
+ * A sequence has places for max_pages * page positions.  An entry outside [0,
+ * pages) names no page: nothing is written for it and nothing attended to, so
+ * entries behind a sequence's end, or of pages that a sliding window has left, may
+ * hold -1.  Sequences may share pages (common beginnings); pages that are written in one call
+ * may not be shared.
+ */
+typedef struct {
+    int32_t page;            /* tokens of a page: a power of two, 1..65536      */
+    int32_t max_pages;       /* entries in a row of the table, >= 1; places     */
+                             /*   (max_pages * page) at most 2^30               */
+    int64_t pages;           /* pages of Kp and of Vp, 1..2^31 - 1              */
+    int64_t page_stride;     /* elements, >= Hkv * page * D, a multiple of D;   */
+                             /*   pages * page_stride / D at most 2^32 - 1      */
+    int64_t table_stride;    /* >= max_pages                                    */
+} ris_page_map;
+
+typedef struct {
+    int32_t dtype;           /* ris_dtype of rows and pages: RIS_BF16           */
+    int32_t Hq;              /* query heads rotated beside (0: none)            */
+    int32_t Hkv;             /* KV heads                                        */
+    int32_t D;               /* head dimension: 64 or 128                       */
+    int32_t batch;           /* sequences                                       */
+    int64_t T;               /* token rows of Q, K and V                        */
+    ris_page_map map;
+    int64_t q_head, q_token; /* strides of Q, Qout, K and V as in               */
+    int64_t qo_head, qo_token; /* ris_prompt_desc; all, and all bases, multiples */
+    int64_t k_head, k_token; /*   of 16 bytes, those of Qout > 0 where there is */
+    int64_t v_head, v_token; /*   more than one row                             */
+} ris_page_store_desc;
+
+/*
+ * The new tokens of a batch into their pages: token i of sequence b has position
+ * start[b] + i (start NULL: i; device int64[batch]; sums within [-2^52, 2^52]).  V
+ * is copied to its place, K rotated to its position there, and Q rotated into Qout,
+ * as ris_rope_packed rotates (the same bits); rope NULL: no rotation, linear and YaRN
+ * need the factor.  A token without a place in the cache keeps its Q alone.  Places that
+ * no token goes to stay as they were.  Qout may be Q itself with the same strides, and
+ * must not overlap the inputs otherwise.  Q and Qout may be NULL where Hq is 0.
+ */
+int ris_page_store(const void* Q, void* Qout, const void* K, const void* V, const int64_t* cu_seqlens,
+                   const int64_t* start, const int32_t* table, void* Kp, void* Vp, const ris_page_store_desc* desc,
+                   const ris_rope_desc* rope, void* stream);
+
+typedef struct {
+    int32_t dtype_in;        /* ris_dtype of Q and the pages: RIS_BF16          */
+    int32_t dtype_out;       /* ris_dtype of out                                */
+    int32_t Hq;              /* query heads                                     */
+    int32_t Hkv;             /* KV heads; Hq % Hkv == 0, Hq / Hkv <= 128        */
+    int32_t D;               /* head dimension: 64 or 128                       */
+    int32_t batch;           /* sequences (>= 1)                                */
+    int64_t T;               /* token rows of Q and out                         */
+    ris_page_map map;
+    int32_t window;          /* keys up to a token's own (>= 0; 0 = none)       */
+    int32_t sink;            /* first tokens that stay visible (>= 0)           */
+    float   scale;           /* score scale, up to 2^127; 0 = 1 / sqrt(D)       */
+    int64_t q_head, q_token; /* strides of Q and out as in ris_prompt_desc      */
+    int64_t o_head, o_token;
+} ris_page_attn_desc;
+
+/* Bytes of device workspace ris_page_attn needs (host only; 0 is possible, and
+ * then workspace may be NULL). */
+int64_t ris_page_attn_workspace_bytes(const ris_page_attn_desc* desc);
+
+/*
+ * Attention of new tokens over the cache that holds them already, one token a
+ * sequence (a decode step), a few, or long chunks, in one batch:
+ *   out[h, t, :] = sum_j softmax_j(scale <Q[h, t], k[g, j]>) v[g, j],
+ * g = floor(h / (Hq / Hkv)), for the token at position p = start[b] + i over the
+ * positions j <= p with j > p - window or j < sink and a page there.  window >=
+ * max_pages * page attends to every key up to the token.  A token that attends to
+ * nothing, or whose position has no place, gets zeros; one whose scores are -inf alone gets NaN.
+ * What lies in places that a token does not attend to, infinities and NaN included, does
+ * not reach its output; infinities of V that it attends to do, whatever their weight.
+ * float32 accumulation of values below 2^100 in magnitude; the softmax weights enter the PV
+ * product rounded to bf16, those below 2^-126 as 0.  out must not overlap the inputs.
+ * The workspace, 16-byte aligned, may not be shared by calls that overlap in time.
+ */
+int ris_page_attn(const void* Q, const void* Kp, const void* Vp, const int32_t* table, const int64_t* cu_seqlens,
+                  const int64_t* start, void* out, void* workspace, int64_t workspace_bytes,
+                  const ris_page_attn_desc* desc, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Weights in 4 bits                                                        */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * A weight matrix W [N, K] (outputs, inputs) in the 4-bit format of the cache:
+ * E2M1 codes in blocks of 32 consecutive inputs that share a power of two, laid out in
+ * tiles of 16 outputs and 128 inputs,
+ *
+ *   C: uint8 [ceil(N / 16), ceil(K / 128), 4, 16, 16]: tile n, tile k, block g, output
+ *      r, byte i hold the inputs 128 k + 32 g + 2 i (low half) and + 2 i + 1 of output
+ *      16 n + r;
+ *   S: uint8 [ceil(N / 16), ceil(K / 512), 4, 16, 4]: entry (n, q, g, r, i) is the scale
+ *      byte of block g of tile k = 4 q + i, 2^(byte - 127), 255 = NaN.
+ *
+ * Outputs from N on and inputs from K on are zeros.  C must be 16-byte aligned.
+ */
+
+/* Quantise rows of W (dtype; row_stride elements apart, any alignment of the type) as
+ * ris_kv4_store does: every block's values are those that it would store. */
+int ris_w4_pack(const void* W, int32_t dtype, int64_t N, int64_t K, int64_t row_stride, uint8_t* C, uint8_t* S, void* stream);
+
+/* The way back: W [N, K] receives the values that the weights stand for, exactly. */
+int ris_w4_load(const uint8_t* C, const uint8_t* S, void* W, int32_t dtype, int64_t N, int64_t K, int64_t row_stride, void* stream);
+
+typedef struct {
+    int32_t dtype;           /* ris_dtype of x, bias and out                    */
+    int32_t gated;           /* 1: SwiGLU of the two halves of the outputs      */
+    int64_t rows;            /* rows of x and out, 1..2^31 - 1                  */
+    int64_t N, K;            /* outputs and inputs of W, up to 2^28 and 2^24;   */
+                             /*   gated: N a multiple of 32                     */
+    int64_t x_stride;        /* elements between rows of x, >= K; it and x      */
+                             /*   multiples of 16 bytes                         */
+    int64_t out_stride;      /* of out, >= its columns; any alignment           */
+} ris_w4_desc;
+
+/*
+ * out = x W^T + bias, [rows, N]; gated: out = silu(a) * b, [rows, N / 2], with a and b the
+ * first and second half of x W^T + bias (gate above up, as ris_swiglu takes them).
+ * bias NULL: none.  Products are exact, sums float32, one rounding at the store: meant for
+ * few rows (a decode step), right for any.  out must not overlap the inputs.
+ */
+int ris_w4_linear(const void* x, const uint8_t* C, const uint8_t* S, const void* bias, void* out, const ris_w4_desc* desc,
+                  void* stream);
 
 #ifdef __cplusplus
 }

@@ -88,3 +88,58 @@ def logprobs(x, targets, top_k):
     top[:len(order)] = y[order]
     lp = np.array([0.0 if t < 0 else np.nan if t >= len(x) else y[t] for t in targets])
     return lp, ent, ids, top
+
+
+def page_places(table, page, pages):
+    """Row (page, slot) of every position that a row of the block table names, -1 where
+    its entry names no page: [len(table) * page, 2]."""
+    j = np.arange(len(table) * page)
+    p = np.asarray(table, np.int64)[j // page]
+    return np.where(((p >= 0) & (p < pages))[:, None], np.stack([p, j % page], 1), -1)
+
+
+def paged_attention(Q, Kp, Vp, table, cu, start, window, sink, scale):
+    """Q [Hq, T, D], Kp, Vp [pages, Hkv, page, D] -> [Hq, T, D]: the token at position p
+    over the positions j <= p with j > p - window or j < sink that have a page; zeros where
+    there are none and for tokens whose position has no place."""
+    Q, Kp, Vp = (np.asarray(x, np.float64) for x in (Q, Kp, Vp))
+    Hq, T, D = Q.shape
+    pages, Hkv, page, _ = Kp.shape
+    out = np.zeros((Hq, T, D))
+    for b, (a, z) in enumerate(zip(cu[:-1], cu[1:])):
+        at = page_places(table[b], page, pages)
+        for t in range(max(a, 0), min(z, T)):
+            p = int(start[b]) + t - max(a, 0)
+            if not 0 <= p < len(at):
+                continue
+            j = np.arange(p + 1)
+            j = j[((j > p - window) | (j < sink)) & (at[:p + 1, 0] >= 0)]
+            if len(j) == 0:
+                continue
+            for h in range(Hq):
+                g = h // (Hq // Hkv)
+                k, v = (x[at[j, 0], g, at[j, 1]] for x in (Kp, Vp))
+                with np.errstate(invalid="ignore", over="ignore"):
+                    s = k @ Q[h, t] * scale
+                    w = np.exp(s - s.max())
+                    w /= w.sum()
+                    # a weight may be 0 here where it is not in truth
+                    fin = np.isfinite(v)
+                    out[h, t] = w @ np.where(fin, v, 0.0) + np.where(fin, 0.0, v).sum(0)
+    return out
+
+
+def w4_tiles(codes, scales):
+    """Codes [N, K] and scale bytes [N, ceil(K / 32)] in the layout of the 4-bit weights: tiles of
+    16 outputs and 128 inputs, element by element."""
+    N, K = codes.shape
+    n, k = -(-N // 16), -(-K // 128)
+    C = np.zeros((n, k, 4, 16, 16), np.uint8)
+    S = np.zeros((n, -(-K // 512), 4, 16, 4), np.uint8)
+    for r in range(16 * n):
+        for i in range(128 * k):
+            if r < N and i < K:
+                C[r // 16, i // 128, i % 128 // 32, r % 16, i % 32 // 2] |= int(codes[r, i]) << (4 * (i % 2))
+            if i % 32 == 0:
+                S[r // 16, i // 512, i % 128 // 32, r % 16, i // 128 % 4] = scales[r, i // 32] if r < N and i < K else 3
+    return C, S

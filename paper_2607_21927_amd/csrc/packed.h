@@ -4,6 +4,7 @@
 #pragma once
 
 #include "ris_device.h"
+#include "ris_internal.h"
 
 namespace ris {
 
@@ -17,7 +18,8 @@ __device__ __forceinline__ int clip_offset(int64_t v, int64_t T) { return (int)(
 // tiles of sequence b have the places from cu[b] / rows + b on, as many as it can need
 // (some stay empty), so that one search finds idx, the last tile of a sequence first.
 struct RowTile {
-    int first;      // the sequence's first token
+    int seq;        // the sequence
+    int first;      // its first token
     int len;        // its tokens
     int tile;       // its tile: rows [tile * rows, ..)
 };
@@ -47,6 +49,7 @@ __device__ __forceinline__ bool find_tile(const int64_t* cu, int batch, int64_t 
         }
         const int b = lo + __popcll(__ballot(lane < n && place(lo + lane) <= idx)) - 1;
         if (b < 0) return false;
+        t.seq = b;
         t.first = clip_offset(cu[b], T);
         t.len = clip_offset(cu[b + 1], T) - t.first;
         const uint32_t j = idx - place(b), nt = t.len > 0 ? ((uint32_t)t.len + rows - 1) / rows : 0u;
@@ -77,6 +80,7 @@ __device__ __forceinline__ bool find_tile(const int64_t* cu, int batch, int64_t 
         at = (int)__builtin_ctzll(on);
         t.tile = (int)level;
     }
+    t.seq = at;
     t.first = __builtin_amdgcn_readlane(lo, at);
     t.len = __builtin_amdgcn_readlane(len, at);
     return true;
@@ -110,6 +114,14 @@ __device__ __forceinline__ int seq_from(const int64_t* cu, int batch, int b, int
     for (step >>= 1; step > 0; step >>= 1)
         if (b + step <= batch && cu[b + step] <= t) b += step;
     return b;
+}
+
+// Row (of D elements) of head 0 of the place that the block table names for position pos
+// of sequence b; -1 where there is none.  Head g's is g << shift rows on.
+__device__ __forceinline__ int64_t page_row(const PageMap& m, int b, int64_t pos) {
+    if (pos < 0 || pos >= m.places) return -1;
+    const int32_t page = m.table[b * m.table_stride + (pos >> m.shift)];
+    return page >= 0 && page < m.pages ? (int64_t)page * m.page_rows + (pos & ((1 << m.shift) - 1)) : -1;
 }
 
 }  // namespace ris

@@ -185,7 +185,7 @@ int make_rope_table(const ris_rope_desc* desc, int32_t D, int64_t window, RopeTa
 
 extern "C" {
 
-int ris_version(void) { return (2 << 16) | 5; }
+int ris_version(void) { return (2 << 16) | 6; }
 
 const char* ris_status_string(int status) {
     switch (status) {

@@ -183,4 +183,69 @@ int32_t logprob_parts(int64_t rows, int64_t vocab);
 int64_t logprob_workspace(int64_t rows, int32_t parts, int32_t top_k);
 hipError_t launch_logprobs(const LogprobParams& p, hipStream_t st);
 
+// Paged cache: pages of `1 << shift` tokens, rows of D elements, named by a block table.
+struct PageMap {
+    const int32_t* table;         // [batch, table_stride]
+    int64_t table_stride;
+    uint32_t page_rows;           // rows of D elements between pages (all rows fit 32 bits)
+    int32_t pages;                // pages there are
+    int32_t places;               // tokens that a row of the table can name
+    int32_t shift;
+};
+struct PageStoreParams {
+    const void* Q;
+    void* Qout;
+    const void* K;
+    const void* V;
+    void* Kp;
+    void* Vp;
+    const int64_t* cu;            // [batch + 1]
+    const int64_t* start;         // [batch] or null
+    PageMap map;
+    int64_t T;
+    int64_t q_head, q_token, qo_head, qo_token, k_head, k_token, v_head, v_token;
+    int32_t Hq, Hkv, D, batch;
+    int32_t rotate;
+};
+hipError_t launch_page_store(const PageStoreParams& p, const RopeTable& tab, hipStream_t st);
+
+struct PageAttnParams {
+    const void* Q;
+    const void* K;                // pages
+    const void* V;
+    const int64_t* cu;            // [batch + 1]
+    const int64_t* start;         // [batch] or null
+    void* out;
+    PageMap map;
+    int64_t T;
+    int64_t q_head, q_token, o_head, o_token;
+    int32_t Hq, Hkv, G, D, batch;
+    int32_t tokens;               // of a row tile: `tokens` tokens of the G heads of a group
+    int32_t window, sink;
+    int32_t out_bf16;
+    float c;                      // score scale in the log2 domain
+    float slack;                  // scores above the reference maximum before it moves
+};
+constexpr int kPageRows = 128;    // rows of a row tile at most
+int64_t page_attn_blocks(const PageAttnParams& p);
+hipError_t launch_page_attn(const PageAttnParams& p, hipStream_t st);
+
+// Products with 4-bit weights, in tiles of 16 outputs x 128 inputs.
+struct W4Params {
+    const void* x;                // [rows, K]
+    const uint8_t* C;             // [tiles of 16 outputs, chunks of 128 inputs, 4, 16, 16]
+    const uint8_t* S;             // [tiles, quads of chunks, 4, 16, 4]
+    const void* bias;             // [N] or null
+    void* out;                    // [rows, N] or, gated, [rows, N / 2]
+    int64_t x_stride, out_stride;
+    int32_t rows, N, K;
+    int32_t f32, gated;
+    int32_t vector_out;           // rows of out take four neighbouring outputs in one store
+};
+int64_t w4_blocks(const W4Params& p);
+hipError_t launch_w4_linear(const W4Params& p, hipStream_t st);
+hipError_t launch_w4_pack(const void* W, int64_t stride, int bf16, int32_t N, int32_t K, uint8_t* C, uint8_t* S, hipStream_t st);
+hipError_t launch_w4_load(const uint8_t* C, const uint8_t* S, int32_t N, int32_t K, void* W, int64_t stride, int bf16,
+                          hipStream_t st);
+
 }  // namespace ris

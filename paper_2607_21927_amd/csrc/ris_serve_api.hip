@@ -136,6 +136,78 @@ int validate_logprob(const ris_logprob_desc* d) {
     return RIS_OK;
 }
 
+constexpr int64_t kMostPlaces = 1ll << 30;      // of a sequence in a paged cache: positions fit 32 bits
+
+int page_map(const ris_page_map& m, int32_t Hkv, int32_t D, ris::PageMap* out) {
+    if (m.page < 1 || m.page > 65536 || (m.page & (m.page - 1)) || m.max_pages < 1) return RIS_E_ARG;
+    if (m.pages < 1 || m.pages > 0x7FFFFFFFll || m.table_stride < m.max_pages) return RIS_E_ARG;
+    if (m.page_stride < (int64_t)Hkv * m.page * D || m.page_stride % D != 0) return RIS_E_ARG;
+    if ((int64_t)m.max_pages * m.page > kMostPlaces || m.page_stride / D > 0xFFFFFFFFll / m.pages ||
+        m.table_stride > (1ll << 32))
+        return RIS_E_UNSUPPORTED;
+    out->table = nullptr;
+    out->table_stride = m.table_stride;
+    out->page_rows = (uint32_t)(m.page_stride / D);
+    out->pages = (int32_t)m.pages;
+    out->places = m.max_pages * m.page;
+    out->shift = 31 - __builtin_clz((unsigned)m.page);
+    return RIS_OK;
+}
+
+int validate_page_store(const ris_page_store_desc* d, ris::PageMap* map) {
+    if (!d) return RIS_E_ARG;
+    if (!known_dtype(d->dtype)) return RIS_E_DTYPE;
+    if (d->dtype != RIS_BF16) return RIS_E_UNSUPPORTED;
+    if (d->Hq < 0 || d->Hkv < 1 || d->batch < 1 || d->T < 1) return RIS_E_ARG;
+    if (d->D != 64 && d->D != 128) return RIS_E_UNSUPPORTED;
+    if (d->T > kMaxTokens || d->batch > (1 << 24) || d->Hq > 65535 || d->Hkv > 65535) return RIS_E_UNSUPPORTED;
+    if (!fits_dispatch((d->T * (d->D / 2) + 255) / 256, 256)) return RIS_E_UNSUPPORTED;
+    return page_map(d->map, d->Hkv, d->D, map);
+}
+
+// The descriptor resolved, all but the pointers.
+int page_attn_params(const ris_page_attn_desc* d, ris::PageAttnParams* p) {
+    if (!d) return RIS_E_ARG;
+    if (!known_dtype(d->dtype_in) || !known_dtype(d->dtype_out)) return RIS_E_DTYPE;
+    if (d->dtype_in != RIS_BF16) return RIS_E_UNSUPPORTED;
+    if (d->Hq < 1 || d->Hkv < 1 || d->batch < 1 || d->T < 1) return RIS_E_ARG;
+    if (d->Hq % d->Hkv != 0) return RIS_E_SHAPE;
+    if (d->Hq / d->Hkv > ris::kPageRows) return RIS_E_UNSUPPORTED;
+    if (d->D != 64 && d->D != 128) return RIS_E_UNSUPPORTED;
+    if (d->window < 0 || d->sink < 0) return RIS_E_ARG;
+    if (!(d->scale >= 0.0f) || !isfinite(d->scale * kLog2e)) return RIS_E_ARG;
+    if (d->T > kMaxTokens || d->batch > (1 << 24) || d->Hkv > 65535) return RIS_E_UNSUPPORTED;
+    const int st = page_map(d->map, d->Hkv, d->D, &p->map);
+    if (st != RIS_OK) return st;
+    p->T = d->T;
+    p->q_head = d->q_head; p->q_token = d->q_token; p->o_head = d->o_head; p->o_token = d->o_token;
+    p->Hq = d->Hq; p->Hkv = d->Hkv; p->G = d->Hq / d->Hkv; p->D = d->D;
+    p->batch = d->batch;
+    p->tokens = ris::kPageRows / p->G;
+    p->window = d->window; p->sink = d->sink;
+    p->out_bf16 = d->dtype_out == RIS_BF16;
+    p->c = (d->scale > 0.0f ? d->scale : 1.0f / sqrtf((float)d->D)) * kLog2e;
+    p->slack = fminf(8.0f / p->c, FLT_MAX);       // -inf + slack stays -inf
+    if (!fits_dispatch(ris::page_attn_blocks(*p), 256)) return RIS_E_UNSUPPORTED;
+    return RIS_OK;
+}
+
+// Sizes of 4-bit weights whose tiles a launch can count.
+int w4_sizes(int32_t dtype, int64_t N, int64_t K) {
+    if (!known_dtype(dtype)) return RIS_E_DTYPE;
+    if (N < 1 || K < 1) return RIS_E_ARG;
+    if (N > (1ll << 28) || K > (1ll << 24)) return RIS_E_UNSUPPORTED;
+    return RIS_OK;
+}
+
+int w4_rows(const void* W, int32_t dtype, int64_t N, int64_t K, int64_t row_stride, const uint8_t* C, const uint8_t* S) {
+    const int st = w4_sizes(dtype, N, K);
+    if (st != RIS_OK) return st;
+    if (!W || !C || !S || !aligned(W, (uintptr_t)elt_bytes(dtype)) || !aligned(C, 16)) return RIS_E_ARG;
+    if (row_stride < K || row_stride > (1ll << 40)) return RIS_E_ARG;
+    return RIS_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -259,6 +331,97 @@ int ris_logprobs(const void* logits, const int64_t* targets, float* logprob, flo
     p.rows = d.rows; p.vocab = d.vocab; p.row_stride = d.row_stride;
     p.n_targets = d.n_targets; p.top_k = d.top_k; p.bf16 = d.dtype == RIS_BF16;
     return hip_status(ris::launch_logprobs(p, static_cast<hipStream_t>(stream)));
+}
+
+int ris_page_store(const void* Q, void* Qout, const void* K, const void* V, const int64_t* cu_seqlens, const int64_t* start,
+                   const int32_t* table, void* Kp, void* Vp, const ris_page_store_desc* desc, const ris_rope_desc* rope,
+                   void* stream) {
+    ris::PageStoreParams p;
+    int st = validate_page_store(desc, &p.map);
+    if (st != RIS_OK) return st;
+    const ris_page_store_desc& d = *desc;
+    if (!K || !V || !cu_seqlens || !table || !Kp || !Vp || (d.Hq > 0 && (!Q || !Qout))) return RIS_E_ARG;
+    if (!vector_rows(K, d.k_head, d.k_token, d.dtype) || !vector_rows(V, d.v_head, d.v_token, d.dtype) || !aligned(Kp, 16) ||
+        !aligned(Vp, 16))
+        return RIS_E_ARG;
+    if (d.Hq > 0 && (!vector_rows(Q, d.q_head, d.q_token, d.dtype) ||
+                     !output_rows(Qout, d.qo_head, d.qo_token, d.dtype, d.Hq, d.T)))
+        return RIS_E_ARG;
+    ris::RopeTable tab = {};
+    if (rope) {
+        if (rope->kind != RIS_ROPE_PLAIN && !(rope->factor > 0.0)) return RIS_E_ARG;
+        st = ris::make_rope_table(rope, d.D, 1, &tab);
+        if (st != RIS_OK) return st;
+    }
+    p.Q = Q; p.Qout = Qout; p.K = K; p.V = V; p.Kp = Kp; p.Vp = Vp;
+    p.cu = cu_seqlens; p.start = start;
+    p.map.table = table;
+    p.T = d.T;
+    p.q_head = d.q_head; p.q_token = d.q_token; p.qo_head = d.qo_head; p.qo_token = d.qo_token;
+    p.k_head = d.k_head; p.k_token = d.k_token; p.v_head = d.v_head; p.v_token = d.v_token;
+    p.Hq = d.Hq; p.Hkv = d.Hkv; p.D = d.D; p.batch = d.batch;
+    p.rotate = rope != nullptr;
+    return hip_status(ris::launch_page_store(p, tab, static_cast<hipStream_t>(stream)));
+}
+
+int64_t ris_page_attn_workspace_bytes(const ris_page_attn_desc* desc) {
+    ris::PageAttnParams p;
+    const int st = page_attn_params(desc, &p);
+    return st == RIS_OK ? 0 : st;
+}
+
+int ris_page_attn(const void* Q, const void* Kp, const void* Vp, const int32_t* table, const int64_t* cu_seqlens,
+                  const int64_t* start, void* out, void* workspace, int64_t workspace_bytes, const ris_page_attn_desc* desc,
+                  void* stream) {
+    ris::PageAttnParams p;
+    const int st = page_attn_params(desc, &p);
+    if (st != RIS_OK) return st;
+    if (!Q || !Kp || !Vp || !table || !cu_seqlens || !out) return RIS_E_ARG;
+    if (!vector_rows(Q, p.q_head, p.q_token, RIS_BF16) || !aligned(Kp, 16) || !aligned(Vp, 16) ||
+        !output_rows(out, p.o_head, p.o_token, desc->dtype_out, p.Hq, p.T))
+        return RIS_E_ARG;
+    (void)workspace; (void)workspace_bytes;
+    p.Q = Q; p.K = Kp; p.V = Vp; p.cu = cu_seqlens; p.start = start; p.out = out;
+    p.map.table = table;
+    return hip_status(ris::launch_page_attn(p, static_cast<hipStream_t>(stream)));
+}
+
+int ris_w4_pack(const void* W, int32_t dtype, int64_t N, int64_t K, int64_t row_stride, uint8_t* C, uint8_t* S, void* stream) {
+    const int st = w4_rows(W, dtype, N, K, row_stride, C, S);
+    if (st != RIS_OK) return st;
+    return hip_status(ris::launch_w4_pack(W, row_stride, dtype == RIS_BF16, (int32_t)N, (int32_t)K, C, S,
+                                          static_cast<hipStream_t>(stream)));
+}
+
+int ris_w4_load(const uint8_t* C, const uint8_t* S, void* W, int32_t dtype, int64_t N, int64_t K, int64_t row_stride, void* stream) {
+    const int st = w4_rows(W, dtype, N, K, row_stride, C, S);
+    if (st != RIS_OK) return st;
+    return hip_status(ris::launch_w4_load(C, S, (int32_t)N, (int32_t)K, W, row_stride, dtype == RIS_BF16,
+                                          static_cast<hipStream_t>(stream)));
+}
+
+int ris_w4_linear(const void* x, const uint8_t* C, const uint8_t* S, const void* bias, void* out, const ris_w4_desc* desc,
+                  void* stream) {
+    if (!desc) return RIS_E_ARG;
+    const ris_w4_desc& d = *desc;
+    const int st = w4_sizes(d.dtype, d.N, d.K);
+    if (st != RIS_OK) return st;
+    if (d.gated != 0 && d.gated != 1) return RIS_E_ARG;
+    if (d.gated && d.N % 32 != 0) return RIS_E_SHAPE;
+    if (d.rows < 1 || d.rows > kMaxTokens) return RIS_E_ARG;
+    const int64_t cols = d.gated ? d.N / 2 : d.N, e = elt_bytes(d.dtype);
+    if (d.x_stride < d.K || d.x_stride > (1ll << 40) || d.out_stride < cols || d.out_stride > (1ll << 40)) return RIS_E_ARG;
+    if (!x || !C || !S || !out || !vector_rows(x, 0, d.x_stride, d.dtype) || !aligned(C, 16) || !aligned(out, (uintptr_t)e) ||
+        !aligned(bias, (uintptr_t)e))
+        return RIS_E_ARG;
+    ris::W4Params p;
+    p.x = x; p.C = C; p.S = S; p.bias = bias; p.out = out;
+    p.x_stride = d.x_stride; p.out_stride = d.out_stride;
+    p.rows = (int32_t)d.rows; p.N = (int32_t)d.N; p.K = (int32_t)d.K;
+    p.f32 = d.dtype == RIS_F32; p.gated = d.gated;
+    p.vector_out = cols % 4 == 0 && d.out_stride % 4 == 0 && aligned(out, (uintptr_t)(4 * e));
+    if (!fits_dispatch(ris::w4_blocks(p), 256)) return RIS_E_UNSUPPORTED;
+    return hip_status(ris::launch_w4_linear(p, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -163,7 +163,82 @@ __global__ __launch_bounds__(kThreads) void k_rope_packed(const void* src, int64
     }
 }
 
+// The new rows of a paged cache: as k_rope_packed, with K rotated into its page, Q into
+// rows of its own beside it and V copied, one pass over the projection's output.  A token
+// without a place in the cache keeps its Q alone.
+template <int P>
+__global__ __launch_bounds__(kThreads) void k_page_store(PageStoreParams p, RopeTable tab) {
+    const int half = p.D >> 1, lanes = half / P;                  // lanes of a token
+    const int64_t gid = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    const int64_t t = gid / lanes;
+    const int i = P * (int)(gid - t * lanes);
+    const int64_t first = (gid - (threadIdx.x & 63)) / lanes;     // of the wave's tokens
+    if (first >= p.T) return;
+    int b = find_seq(p.cu, p.batch, first);
+    b = seq_from(p.cu, p.batch, b < 0 ? 0 : b, t);
+    if (t >= p.T || b >= p.batch || t < p.cu[b]) return;
+    const int64_t from = p.cu[b] > 0 ? p.cu[b] : 0;               // clipped
+    const int64_t pos = (int64_t)((uint64_t)(t - from) + (uint64_t)(p.start ? p.start[b] : 0));
+    const int64_t row = page_row(p.map, b, pos);
+    float c[P], s[P];
+    if (p.rotate) {
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            double sd, cd;
+            sincos((double)pos * tab.inv_freq[i + k], &sd, &cd);
+            c[k] = (float)(cd * tab.mscale);
+            s[k] = (float)(sd * tab.mscale);
+        }
+    }
+    // heads of Q, then of K, then of V
+    const int turned = p.Hq + p.Hkv, heads = row < 0 ? p.Hq : turned + p.Hkv;
+    const auto load = [&](int h, RopePairs<true, P>& x) __attribute__((always_inline)) {
+        if (h < p.Hq) load_pairs<true, P>(p.Q, h * p.q_head + t * p.q_token + i, half, x);
+        else if (h < turned) load_pairs<true, P>(p.K, (h - p.Hq) * p.k_head + t * p.k_token + i, half, x);
+        else load_pairs<true, P>(p.V, (h - turned) * p.v_head + t * p.v_token + i, half, x);
+    };
+    int h = blockIdx.y;
+    if (h >= heads) return;
+    RopePairs<true, P> x;
+    load(h, x);
+    while (true) {
+        const int nh = h + (int)gridDim.y;
+        RopePairs<true, P> nx = x, y = x;
+        if (nh < heads) load(nh, nx);
+        if (p.rotate && h < turned) {
+#pragma unroll
+            for (int k = 0; k < P; ++k) {
+                y.lo[k] = fmaf(x.lo[k], c[k], -(x.hi[k] * s[k]));
+                y.hi[k] = fmaf(x.lo[k], s[k], x.hi[k] * c[k]);
+            }
+        }
+        if (h < p.Hq) {
+            store_pairs<true, P>(p.Qout, h * p.qo_head + t * p.qo_token + i, half, y);
+        } else {
+            const int g = h < turned ? h - p.Hq : h - turned;
+            store_pairs<true, P>(h < turned ? p.Kp : p.Vp, (row + ((int64_t)g << p.map.shift)) * p.D + i, half, y);
+        }
+        if (nh >= heads) return;
+        h = nh;
+        x = nx;
+    }
+}
+
 }  // namespace
+
+hipError_t launch_page_store(const PageStoreParams& p, const RopeTable& tab, hipStream_t st) {
+    const int64_t pairs = p.T * (p.D / 2);
+    const bool four = pairs >= kManyPairs;
+    const int64_t blocks = (pairs / (four ? 4 : 1) + kThreads - 1) / kThreads;
+    const int heads = p.Hq + 2 * p.Hkv;
+    int64_t deal = kManyBlocks / blocks;
+    deal = deal < 1 ? 1 : (deal > heads ? heads : deal);
+    if (deal > 65535) deal = 65535;
+    const dim3 grid((unsigned)blocks, (unsigned)deal);
+    if (four) hipLaunchKernelGGL(k_page_store<4>, grid, dim3(kThreads), 0, st, p, tab);
+    else hipLaunchKernelGGL(k_page_store<1>, grid, dim3(kThreads), 0, st, p, tab);
+    return hipGetLastError();
+}
 
 hipError_t launch_rope_packed(const void* src, int64_t head_stride, int64_t token_stride, void* dst, int dtype_bf16,
                               int heads, int64_t T, int D, const int64_t* cu, const int64_t* start, int batch,

@@ -37,9 +37,38 @@ class LogprobDesc(ctypes.Structure):
                 ("rows", ctypes.c_int64), ("vocab", ctypes.c_int64), ("row_stride", ctypes.c_int64)]
 
 
+class PageMap(ctypes.Structure):
+    _fields_ = [("page", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("pages", ctypes.c_int64),
+                ("page_stride", ctypes.c_int64), ("table_stride", ctypes.c_int64)]
+
+
+class PageStoreDesc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("batch", ctypes.c_int32), ("T", ctypes.c_int64), ("map", PageMap),
+                ("q_head", ctypes.c_int64), ("q_token", ctypes.c_int64),
+                ("qo_head", ctypes.c_int64), ("qo_token", ctypes.c_int64),
+                ("k_head", ctypes.c_int64), ("k_token", ctypes.c_int64),
+                ("v_head", ctypes.c_int64), ("v_token", ctypes.c_int64)]
+
+
+class PageAttnDesc(ctypes.Structure):
+    _fields_ = [("dtype_in", ctypes.c_int32), ("dtype_out", ctypes.c_int32),
+                ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("batch", ctypes.c_int32), ("T", ctypes.c_int64), ("map", PageMap),
+                ("window", ctypes.c_int32), ("sink", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("q_head", ctypes.c_int64), ("q_token", ctypes.c_int64),
+                ("o_head", ctypes.c_int64), ("o_token", ctypes.c_int64)]
+
+
+class W4Desc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("gated", ctypes.c_int32), ("rows", ctypes.c_int64),
+                ("N", ctypes.c_int64), ("K", ctypes.c_int64), ("x_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64)]
+
+
 EXPORTS = ("ris_rope_packed", "ris_prompt_attn", "ris_kv4_store", "ris_kv4_load",
            "ris_kv4_decode_workspace_bytes", "ris_kv4_decode_attn", "ris_logprobs_workspace_bytes",
-           "ris_logprobs")
+           "ris_logprobs", "ris_page_store", "ris_page_attn_workspace_bytes", "ris_page_attn", "ris_w4_pack", "ris_w4_load",
+           "ris_w4_linear")
 
 _lib = None
 
@@ -58,6 +87,12 @@ def lib():
         L.ris_kv4_decode_attn.argtypes = [vp] * 9 + [i64, ptr(ris.DecodeDesc), vp]
         L.ris_logprobs_workspace_bytes.argtypes = [ptr(LogprobDesc)]
         L.ris_logprobs.argtypes = [vp] * 7 + [i64, ptr(LogprobDesc), vp]
+        L.ris_page_store.argtypes = [vp] * 9 + [ptr(PageStoreDesc), ptr(ris.RopeDesc), vp]
+        L.ris_page_attn_workspace_bytes.argtypes = [ptr(PageAttnDesc)]
+        L.ris_page_attn.argtypes = [vp] * 8 + [i64, ptr(PageAttnDesc), vp]
+        L.ris_w4_pack.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp]
+        L.ris_w4_load.argtypes = [vp, vp, vp, i32, i64, i64, i64, vp]
+        L.ris_w4_linear.argtypes = [vp] * 5 + [ptr(W4Desc), vp]
         for name in EXPORTS:
             getattr(L, name).restype = i64 if name.endswith("_bytes") else ctypes.c_int
         _lib = L
@@ -318,3 +353,166 @@ def logprobs(logits, targets, logprob, entropy, top_ids, top_logprob, workspace,
     _call(index, stream, "ris_logprobs", logits.data_ptr(), _at(targets), _at(logprob), _at(entropy), _at(top_ids),
           _at(top_logprob), _at(workspace), nbytes, desc)
     return logprob
+
+
+# ---- cache in pages
+
+def page_cache(pages, Hkv, page, D, device="cuda"):
+    """Empty pages Kp, Vp [pages, Hkv, page, D], bf16."""
+    return [torch.zeros(pages, Hkv, page, D, dtype=torch.bfloat16, device=device) for _ in range(2)]
+
+
+def _page_map(Kp, table):
+    """Map of pages [pages, Hkv, page, D], whose pages may lie apart, under a block table
+    [batch, max_pages] int32, whose rows may."""
+    pages, Hkv, page, D = Kp.shape
+    if table.dtype != torch.int32:
+        raise TypeError("the block table must be int32")
+    if table.dim() != 2 or table.stride(1) != 1 and table.shape[1] > 1:
+        raise ValueError("the block table must be [batch, max_pages] with unit stride along a row")
+    if Kp.stride()[1:] != (page * D, D, 1):
+        raise ValueError("pages must be [Hkv, page, D] contiguous")
+    stride = Hkv * page * D if pages == 1 else Kp.stride(0)
+    return PageMap(page, table.shape[1], pages, stride, table.shape[1] if table.shape[0] == 1 else table.stride(0))
+
+
+def _need_pages(Kp, Vp):
+    if Kp.dtype != torch.bfloat16 or Vp.dtype != torch.bfloat16:
+        raise TypeError("pages must be bfloat16")
+    if Kp.dim() != 4 or Vp.shape != Kp.shape or Vp.stride() != Kp.stride():
+        raise ValueError("Kp and Vp must be [pages, Hkv, page, D], of one shape and strides")
+
+
+def page_store(K, V, cu_seqlens, table, Kp, Vp, start=None, q=None, q_out=None, rope=None, stream=None):
+    """ris_page_store: rows K, V [Hkv, T, D] (views as in ``prompt_attn``) into the pages
+    that ``table`` names, token i of sequence b at position start[b] + i (start None: i).
+    rope: a ``ris.rope_desc`` that K, and q [Hq, T, D] into q_out, are rotated by (None: K and q
+    are copied)."""
+    index = _one_gpu(Kp, K, V, cu_seqlens, table, Vp, start, q, q_out)
+    _need_pages(Kp, Vp)
+    if K.dtype != V.dtype:
+        raise TypeError("K and V must share a dtype")
+    Hkv, T, D = shape = tuple(K.shape)
+    if Kp.shape[1] != Hkv or Kp.shape[3] != D:
+        raise ValueError("Kp and Vp must be [pages, Hkv, page, D] with the rows' Hkv and D")
+    batch = _bounds(cu_seqlens, start)
+    if table.shape[0] != batch:
+        raise ValueError("the block table must hold one row a sequence")
+    k_at, *k_strides = _rows(K, shape)
+    v_at, *v_strides = _rows(V, shape)
+    Hq, q_at, qo_at, q_strides = 0, 0, 0, [0] * 4
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    if q is not None:
+        Hq = q.shape[0]
+        if q.dtype != K.dtype or q_out.dtype != K.dtype:
+            raise TypeError("q and q_out must have the dtype of K and V")
+        q_at, *a = _rows(q, (Hq, T, D))
+        qo_at, *b = _rows(q_out, (Hq, T, D))
+        q_strides = a + b
+    desc = PageStoreDesc(_code(K), Hq, Hkv, D, batch, T, _page_map(Kp, table), *q_strides, *k_strides, *v_strides)
+    _call(index, stream, "ris_page_store", q_at, qo_at, k_at, v_at, cu_seqlens.data_ptr(), _at(start), table.data_ptr(),
+          Kp.data_ptr(), Vp.data_ptr(), desc, rope)
+
+
+def page_attn_desc(Q, Kp, table, cu_seqlens, out, window=None, sink=0, scale=0.0):
+    """Descriptor from views Q, out [Hq, T, D], pages Kp [pages, Hkv, page, D] and the block
+    table [batch, max_pages].  window None: every key up to a token."""
+    Hq, T, D = Q.shape
+    return PageAttnDesc(_code(Q), _code(out), Hq, Kp.shape[1], D, cu_seqlens.numel() - 1, T, _page_map(Kp, table),
+                        min(0x7FFFFFFF, table.shape[1] * Kp.shape[2] if window is None else window), sink, scale,
+                        *_rows(Q, Q.shape)[1:], *_rows(out, Q.shape)[1:])
+
+
+def page_attn_workspace_bytes(desc):
+    v = lib().ris_page_attn_workspace_bytes(ctypes.byref(desc))
+    if v < 0:
+        raise ris.RisError(int(v), "ris_page_attn_workspace_bytes")
+    return int(v)
+
+
+def page_attn(Q, Kp, Vp, table, cu_seqlens, out, workspace, desc, start=None, stream=None):
+    """ris_page_attn: attention of the new tokens Q [Hq, T, D] over the pages that hold
+    them already, token i of sequence b at position start[b] + i (start None: i).
+    workspace: at least page_attn_workspace_bytes(desc) bytes, None where that is 0."""
+    index = _one_gpu(out, Q, Kp, Vp, table, cu_seqlens, workspace, start)
+    _need_pages(Kp, Vp)
+    _need_dense(workspace)
+    if _code(Q) != desc.dtype_in or _code(out) != desc.dtype_out:
+        raise TypeError("Q and out dtypes must match the descriptor")
+    m, q = desc.map, (desc.Hq, desc.T, desc.D)
+    if (Kp.shape != (m.pages, desc.Hkv, m.page, desc.D) or m.pages > 1 and Kp.stride(0) != m.page_stride
+            or Kp.stride()[1:] != (m.page * desc.D, desc.D, 1)):
+        raise ValueError("Kp and Vp must be [pages, Hkv, page, D] as in the descriptor")
+    if (table.dtype != torch.int32 or table.shape != (desc.batch, m.max_pages) or table.stride(1) != 1 and m.max_pages > 1
+            or table.stride(0) != m.table_stride and desc.batch > 1):
+        raise ValueError("the block table must be int32 [batch, max_pages] as in the descriptor")
+    q_at, o_at = _placed(Q, q, (desc.q_head, desc.q_token, 1)), _placed(out, q, (desc.o_head, desc.o_token, 1))
+    if _bounds(cu_seqlens, start) != desc.batch:
+        raise ValueError("cu_seqlens must hold the descriptor's batch + 1 offsets")
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _call(index, stream, "ris_page_attn", q_at, Kp.data_ptr(), Vp.data_ptr(), table.data_ptr(), cu_seqlens.data_ptr(),
+          _at(start), o_at, _at(workspace), nbytes, desc)
+    return out
+
+
+# ---- weights in 4 bits
+
+def w4_weight(N, K, device="cuda"):
+    """Empty 4-bit weights of N outputs and K inputs: codes C [tiles of 16 outputs, tiles of
+    128 inputs, 4, 16, 16] and scales S [tiles, ceil(K / 512), 4, 16, 4], uint8."""
+    n = -(-N // 16)
+    return (torch.zeros(n, -(-K // 128), 4, 16, 16, dtype=torch.uint8, device=device),
+            torch.zeros(n, -(-K // 512), 4, 16, 4, dtype=torch.uint8, device=device))
+
+
+def _need_w4(C, S, N, K):
+    if C.dtype != torch.uint8 or S.dtype != torch.uint8:
+        raise TypeError("C and S must be uint8")
+    n = -(-N // 16)
+    if C.shape != (n, -(-K // 128), 4, 16, 16) or S.shape != (n, -(-K // 512), 4, 16, 4):
+        raise ValueError(f"C and S must be those of {N} outputs and {K} inputs")
+    _need_dense(C, S)
+
+
+def _matrix(t, rows, cols):
+    """Row stride of a [rows, cols] matrix with unit stride along a row."""
+    if t.shape != (rows, cols) or t.stride(1) != 1 and cols > 1:
+        raise ValueError(f"expected a [{rows}, {cols}] matrix with unit stride along its rows, got {tuple(t.shape)}")
+    return t.stride(0) if rows > 1 else cols
+
+
+def w4_pack(W, C, S, stream=None):
+    """ris_w4_pack: rows of W [N, K] quantised into the weights C, S."""
+    index = _one_gpu(W, C, S)
+    N, K = W.shape
+    _need_w4(C, S, N, K)
+    _call(index, stream, "ris_w4_pack", W.data_ptr(), _code(W), N, K, _matrix(W, N, K), C.data_ptr(), S.data_ptr())
+
+
+def w4_load(C, S, W, stream=None):
+    """ris_w4_load: the values that the weights C, S stand for into W [N, K]."""
+    index = _one_gpu(W, C, S)
+    N, K = W.shape
+    _need_w4(C, S, N, K)
+    _call(index, stream, "ris_w4_load", C.data_ptr(), S.data_ptr(), W.data_ptr(), _code(W), N, K, _matrix(W, N, K))
+    return W
+
+
+def w4_linear(x, C, S, out, bias=None, gated=False, stream=None):
+    """ris_w4_linear: out [rows, N] = x [rows, K] W^T + bias for the weights C, S; gated:
+    out [rows, N / 2] = silu(first half) * second half.  Rows of x lie multiples of 16
+    bytes apart."""
+    index = _one_gpu(out, x, C, S, bias)
+    (rows, K), cols = x.shape, out.shape[1]
+    N = 2 * cols if gated else cols
+    _need_w4(C, S, N, K)
+    if out.dtype != x.dtype or bias is not None and (bias.dtype != x.dtype or bias.shape != (N,)):
+        raise ValueError("out and bias [N] must have the dtype of x")
+    _need_dense(bias)
+    x_stride = _matrix(x, rows, K)
+    if rows == 1:
+        x_stride = -(-K // 8) * 8                       # whatever the stride of one row
+    desc = W4Desc(_code(x), int(gated), rows, N, K, x_stride, _matrix(out, rows, cols))
+    _call(index, stream, "ris_w4_linear", x.data_ptr(), C.data_ptr(), S.data_ptr(), _at(bias), out.data_ptr(), desc)
+    return out
