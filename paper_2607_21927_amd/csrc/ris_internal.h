@@ -223,11 +223,17 @@ struct PageAttnParams {
     int32_t tokens;               // of a row tile: `tokens` tokens of the G heads of a group
     int32_t window, sink;
     int32_t out_bf16;
+    int32_t parts;                // workgroups that share the key tiles of all row tiles; 0: one a row tile
+    int32_t part_rows;            // rows of a piece in the workspace
+    float* part_o;                // [2 parts, part_rows, D] unnormalised outputs
+    float* part_ml;               // [2 parts, part_rows, 4] their references, sums, whether anything was attended to
     float c;                      // score scale in the log2 domain
     float slack;                  // scores above the reference maximum before it moves
 };
 constexpr int kPageRows = 128;    // rows of a row tile at most
 int64_t page_attn_blocks(const PageAttnParams& p);
+int32_t page_attn_parts(const PageAttnParams& p);
+int64_t page_attn_workspace(const PageAttnParams& p);
 hipError_t launch_page_attn(const PageAttnParams& p, hipStream_t st);
 
 // Products with 4-bit weights, in tiles of 16 outputs x 128 inputs.

@@ -188,6 +188,8 @@ int page_attn_params(const ris_page_attn_desc* d, ris::PageAttnParams* p) {
     p->out_bf16 = d->dtype_out == RIS_BF16;
     p->c = (d->scale > 0.0f ? d->scale : 1.0f / sqrtf((float)d->D)) * kLog2e;
     p->slack = fminf(8.0f / p->c, FLT_MAX);       // -inf + slack stays -inf
+    p->parts = ris::page_attn_parts(*p);
+    p->part_rows = (int32_t)(d->T < p->tokens ? d->T : p->tokens) * p->G;
     if (!fits_dispatch(ris::page_attn_blocks(*p), 256)) return RIS_E_UNSUPPORTED;
     return RIS_OK;
 }
@@ -367,7 +369,7 @@ int ris_page_store(const void* Q, void* Qout, const void* K, const void* V, cons
 int64_t ris_page_attn_workspace_bytes(const ris_page_attn_desc* desc) {
     ris::PageAttnParams p;
     const int st = page_attn_params(desc, &p);
-    return st == RIS_OK ? 0 : st;
+    return st == RIS_OK ? ris::page_attn_workspace(p) : st;
 }
 
 int ris_page_attn(const void* Q, const void* Kp, const void* Vp, const int32_t* table, const int64_t* cu_seqlens,
@@ -380,7 +382,11 @@ int ris_page_attn(const void* Q, const void* Kp, const void* Vp, const int32_t* 
     if (!vector_rows(Q, p.q_head, p.q_token, RIS_BF16) || !aligned(Kp, 16) || !aligned(Vp, 16) ||
         !output_rows(out, p.o_head, p.o_token, desc->dtype_out, p.Hq, p.T))
         return RIS_E_ARG;
-    (void)workspace; (void)workspace_bytes;
+    const int64_t need = ris::page_attn_workspace(p);
+    if (need > 0 && (!workspace || !aligned(workspace, 16))) return RIS_E_ARG;
+    if (workspace_bytes < need) return RIS_E_CAPACITY;
+    p.part_o = static_cast<float*>(workspace);
+    p.part_ml = p.part_o + 2 * (int64_t)p.parts * p.part_rows * p.D;
     p.Q = Q; p.K = Kp; p.V = Vp; p.cu = cu_seqlens; p.start = start; p.out = out;
     p.map.table = table;
     return hip_status(ris::launch_page_attn(p, static_cast<hipStream_t>(stream)));

@@ -152,6 +152,7 @@ BATCHES = {
     "few": ([3, 1, 5, 0, 2], [10, 700, 61, 5, 0]),
     "chunk": ([70, 0, 129, 1], [0, 0, 333, 500]),
     "prompt": ([257], [0]),
+    "shared": ([70, 0, 30, 1, 1], [1200, 0, 0, 700, 2]),      # places enough for row tiles to be shared by workgroups
 }
 
 
