@@ -13,8 +13,7 @@
 // may attend to and whose page there is are a mask of 64 bits (`live`); the others are
 // never read: the first live key is loaded in their place.  Rows attend to bits of that
 // mask, so that what lies in unwritten places does not reach an output.
-#include "packed.h"
-#include "ris_internal.h"
+#include "page_rows.h"
 #include "softmax_tiles.h"
 
 namespace ris {
@@ -37,55 +36,48 @@ struct Piece {
     }
 };
 
-// The keys of a row tile: of the tokens at positions pmin .. pmax, as key tiles of which the
-// first `sinks` hold first tokens and the others lie side by side from `near` on.
-struct Span {
-    int pmin, pmax, lo;       // lo: first key of the window of pmin
-    int near, sinks, n;
-    __device__ __forceinline__ int key0(int v) const { return kKeys * (v < sinks ? v : near + v - sinks); }
-};
-
-// Of tokens at positions a .. z (any; those outside the cache attend to nothing).
-__device__ __forceinline__ Span span_of(const PageAttnParams& p, int64_t a, int64_t z) {
-    Span s{0, -1, 0, 0, 0, 0};
-    if (z < 0 || a >= p.map.places) return s;
-    s.pmin = a < 0 ? 0 : (int)a;
-    s.pmax = z >= p.map.places ? p.map.places - 1 : (int)z;
-    s.lo = s.pmin - p.window + 1 > 0 ? s.pmin - p.window + 1 : 0;
-    if (p.window == 0) s.lo = s.pmax + 1;
-    const int snk = p.sink < s.pmax + 1 ? p.sink : s.pmax + 1;
-    s.near = s.lo <= s.pmax ? s.lo / kKeys : s.pmax / kKeys + 1;
-    s.sinks = (snk + kKeys - 1) / kKeys;
-    if (s.sinks > s.near) s.sinks = s.near;
-    s.n = s.sinks + s.pmax / kKeys + 1 - s.near;
-    return s;
-}
-
-// Position of a sequence's first new token, near enough to the cache for sums with token
-// numbers (below 2^31).
-__device__ __forceinline__ int64_t first_pos(const PageAttnParams& p, int b) {
-    const int64_t at = p.start ? p.start[b] : 0, far = 1ll << 32;
-    return at < -far ? -far : (at > far ? far : at);
-}
-
 // ---------------------------------------------------------------------------
-// Few row tiles: the key tiles of all of them, one after another for each KV head, are
-// one line of units that the workgroups cut into equal parts.  A part may begin and end within a
-// row tile; such a row tile's pieces are left in the workspace, and a second launch joins
-// them.  Lengths and positions are on the device, so every workgroup works the line out.
+// Few row tiles: their key tiles, one after another for each KV head, are one line that the
+// workgroups cut into equal parts.  A part may begin and end within a row tile; the pieces of such a
+// row tile are left in the workspace, and a second launch joins them.  Lengths and positions are on
+// the device, so every workgroup works the line out.
+//
+// (Cutting sequences by slices of their keys, so that neighbouring parts read the same keys at one
+// time, gave nothing: 2,048 tokens after 30,000 486 -> 494 us, 600 with 31 other sequences 117 -> 162.
+// Nor did counting a key tile for half where one wave's rows read it: 106 for 112, such parts waiting
+// for memory.)
 // ---------------------------------------------------------------------------
 constexpr int kPlanThreads = 64 * kWaves;
 constexpr int kPlanSeqs = kPlanThreads;         // sequences at most
-constexpr int kPlanTiles = 4 * kPlanThreads;    // row tiles of a KV head at most
-constexpr int kMinUnits = 4;                    // of a part, where there are many workgroups
+constexpr int kMostTiles = 1024;                // row tiles of all KV heads
+static_assert(kPartList >= 4 * kMostTiles + 1);
+constexpr uint32_t kMinUnits = 4;               // of a part, where there are many workgroups
 constexpr int kMostParts = 768;
-constexpr int kMostPlanned = 1 << 27;           // and from which: units of all row tiles are counted in 32 bits
+constexpr int kMostPlanned = 1 << 27;           // places up to which the key tiles of all row tiles are counted in 32 bits
 constexpr int kSoloKeys = 512;                  // places to which a row tile is one workgroup's
 
 struct Plan {
     uint32_t tile0[kPlanSeqs + 1];      // a sequence's first row tile
-    uint32_t unit0[kPlanTiles + 1];     // a row tile's first unit
+    uint32_t unit0[kMostTiles + 1];     // a row tile's first unit
     uint32_t carry[kWaves];
+    // a sequence's first new token, its tokens and its first position, near enough to the cache
+    int32_t first[kPlanSeqs], len[kPlanSeqs];
+    int64_t pos[kPlanSeqs];
+    // Row tile `tile` of sequence b.
+    __device__ __forceinline__ RowTile row_tile(int b, int tile) const {
+        RowTile t;
+        t.seq = b;
+        t.first = first[b];
+        t.len = len[b];
+        t.tile = tile;
+        return t;
+    }
+};
+
+// What the second launch needs of a row tile of a KV head: its pieces are the end of part
+// `part` and the beginnings of the parts behind it.
+struct Pieces {
+    int32_t count, part, seq, tile;
 };
 
 // Sum of v over the threads before this one; total: over all.
@@ -117,7 +109,7 @@ __device__ __forceinline__ int last_upto(const uint32_t* x, int n, uint32_t v) {
 
 struct Line {
     uint32_t tiles;         // row tiles of a KV head
-    uint32_t head;          // units of a KV head
+    uint32_t head;          // units of a KV head: key tiles of its row tiles
     uint64_t units;         // of all
     uint32_t parts;
     __device__ __forceinline__ uint64_t first(uint32_t w) const { return w * units / parts; }
@@ -125,72 +117,58 @@ struct Line {
     __device__ __forceinline__ uint32_t owner(uint64_t u) const { return (uint32_t)(((u + 1) * parts - 1) / units); }
 };
 
-__device__ __forceinline__ int row_tiles(const PageAttnParams& p, int b) {
-    const int len = clip_offset(p.cu[b + 1], p.T) - clip_offset(p.cu[b], p.T);
-    return len > 0 ? (len + p.tokens - 1) / p.tokens : 0;
-}
-
-__device__ __forceinline__ RowTile row_tile(const PageAttnParams& p, int b, int tile) {
-    RowTile t;
-    t.seq = b;
-    t.first = clip_offset(p.cu[b], p.T);
-    t.len = clip_offset(p.cu[b + 1], p.T) - t.first;
-    t.tile = tile;
-    return t;
-}
-
-// Positions of the tokens of a row tile.
-__device__ __forceinline__ int tile_tokens(const PageAttnParams& p, const RowTile& t) {
-    return t.len - t.tile * p.tokens < p.tokens ? t.len - t.tile * p.tokens : p.tokens;
-}
-__device__ __forceinline__ int64_t tile_pos(const PageAttnParams& p, const RowTile& t) {
-    return first_pos(p, t.seq) + (int64_t)t.tile * p.tokens;
-}
-
 __device__ __forceinline__ Line make_plan(const PageAttnParams& p, Plan& plan) {
     const int tid = threadIdx.x;
     Line line;
-    const uint32_t mine = tid < p.batch ? (uint32_t)row_tiles(p, tid) : 0u;
+    uint32_t mine = 0;
+    if (tid < p.batch) {
+        const int64_t from = p.cu[tid], to = p.cu[tid + 1], pos = first_pos(p, tid);
+        plan.first[tid] = clip_offset(from, p.T);
+        plan.len[tid] = clip_offset(to, p.T) - plan.first[tid];
+        plan.pos[tid] = pos;
+        if (plan.len[tid] > 0) mine = (uint32_t)(plan.len[tid] + p.tokens - 1) / (uint32_t)p.tokens;
+    }
     const uint32_t at = block_scan(mine, plan.carry, line.tiles);
     if (tid < p.batch) plan.tile0[tid] = at;
     if (tid == 0) plan.tile0[p.batch] = line.tiles;
     __syncthreads();
-    // four neighbouring row tiles a thread; one that attends to nothing counts as one unit
-    uint32_t n[4] = {0u, 0u, 0u, 0u};
-    const uint32_t t0 = 4u * tid;
+    // kEach neighbouring row tiles a thread; one that attends to nothing counts as one key tile
+    constexpr int kEach = kMostTiles / kPlanThreads;
+    uint32_t n[kEach], sum = 0;
+    const uint32_t t0 = (uint32_t)kEach * tid;
+    int b = 0;
     if (t0 < line.tiles) {
-        int lo = 0, hi = p.batch;               // tile0[lo] <= t0 < tile0[hi]
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if (plan.tile0[mid] <= t0) lo = mid;
+        int hi = p.batch;                       // tile0[b] <= t0 < tile0[hi]
+        while (hi - b > 1) {
+            const int mid = (b + hi) / 2;
+            if (plan.tile0[mid] <= t0) b = mid;
             else hi = mid;
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (t0 + i >= line.tiles) break;
-            while (plan.tile0[lo + 1] <= t0 + i) ++lo;
-            const RowTile t = row_tile(p, lo, (int)(t0 + i - plan.tile0[lo]));
-            const int64_t pos = tile_pos(p, t);
-            const int units = span_of(p, pos, pos + tile_tokens(p, t) - 1).n;
-            n[i] = units > 0 ? (uint32_t)units : 1u;
-        }
     }
-    uint32_t before = block_scan(n[0] + n[1] + n[2] + n[3], plan.carry, line.head);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kEach; ++i) {
+        n[i] = 0;
+        if (t0 + i >= line.tiles) continue;
+        while (plan.tile0[b + 1] <= t0 + i) ++b;
+        const RowTile t = plan.row_tile(b, (int)(t0 + i - plan.tile0[b]));
+        const int64_t pos = tile_pos(p, plan.pos[b], t);
+        const int tokens = tile_tokens(p, t), keys = span_of<kKeys>(p, pos, pos + tokens - 1).n;
+        n[i] = keys > 0 ? (uint32_t)keys : 1u;
+        sum += n[i];
+    }
+    uint32_t before = block_scan(sum, plan.carry, line.head);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
         if (t0 + i < line.tiles) plan.unit0[t0 + i] = before;
         before += n[i];
     }
     if (tid == 0) plan.unit0[line.tiles] = line.head;
     __syncthreads();
     line.units = (uint64_t)line.head * (uint32_t)p.Hkv;
-    const uint64_t most = line.units / kMinUnits;
-    line.parts = most < 1 ? 1u : (most < (uint64_t)p.parts ? (uint32_t)most : (uint32_t)p.parts);
+    const uint64_t fill = line.units / kMinUnits;
+    line.parts = fill < 1 ? 1u : (fill < (uint64_t)p.parts ? (uint32_t)fill : (uint32_t)p.parts);
     return line;
 }
-
-// The lowest n bits.
-__device__ __forceinline__ uint64_t below(int n) { return n <= 0 ? 0ull : (n >= 64 ? ~0ull : (1ull << n) - 1); }
 
 // Where the lanes' pieces of a key tile lie, and which of its keys are live.
 template <int D>
@@ -198,13 +176,6 @@ struct Places {
     uint32_t row[Piece<D>::kCount];
     uint64_t live;
 };
-
-__device__ __forceinline__ void store4(const PageAttnParams& p, int64_t at, float a, float b, float c, float d) {
-    if (p.out_bf16)
-        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + at) = make_uint2(pack_bf16x2(a, b), pack_bf16x2(c, d));
-    else
-        *reinterpret_cast<f32x4_t*>(static_cast<float*>(p.out) + at) = f32x4_t{a, b, c, d};
-}
 
 template <int D, bool kSplit>
 __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void k_page_attn(PageAttnParams p) {
@@ -224,12 +195,12 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void k_page_attn(Page
     const int v_row = 4 * lh + ((lane & 15) >> 2);
     const uint32_t v_at = 2 * D * v_row + 16 * ((2 * (lane >> 4 & 1) + ((lane & 3) >> 1)) ^ swizzle<D>(v_row)) + 8 * (lane & 1);
 
-    // The virtual key tiles [begin, end) of row tile t of KV head g (end < 0: all of them): to out,
-    // or to piece `piece` of the workspace where that is not negative.
-    const auto run = [&](const RowTile& t, int g, int begin, int end, int piece) __attribute__((always_inline)) {
-        const int64_t pos0 = tile_pos(p, t);            // of the tile's first token
+    // The virtual key tiles [begin, end) of row tile t, whose tokens' positions begin at pos0, of KV head g
+    // (end < 0: all of them): to out
+    // where they are all of its, else to piece `piece` of the workspace.
+    const auto run = [&](const RowTile& t, int64_t pos0, int g, int begin, int end, int piece) __attribute__((always_inline)) {
         const int ntok = tile_tokens(p, t);
-        const Span s = span_of(p, pos0, pos0 + ntok - 1);
+        const Span<kKeys> s = span_of<kKeys>(p, pos0, pos0 + ntok - 1);
         if (end < 0) end = s.n;
 
         // The lane's row: a token of the tile and a head of the group.
@@ -467,7 +438,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void k_page_attn(Page
         l = pair_sum32(l);
         if (!mine_row) return;
         seen &= pos >= 0;
-        if (kSplit && piece >= 0) {
+        if (kSplit && (begin > 0 || end < s.n)) {
             const int64_t at = (int64_t)piece * p.part_rows + r;
             if (lh == 0) *reinterpret_cast<f32x4_t*>(p.part_ml + 4 * at) = f32x4_t{ref.m, ref.mc, l, seen ? 1.f : 0.f};
             float* to = p.part_o + at * D + 4 * lh;
@@ -499,80 +470,127 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void k_page_attn(Page
         // neighbouring parts on one XCD, all XCDs alike
         const uint32_t each = (line.parts + 7) / 8, w = (blockIdx.x & 7u) * each + (blockIdx.x >> 3);
         if ((blockIdx.x >> 3) >= each || w >= line.parts) return;
+        Pieces* const list = reinterpret_cast<Pieces*>(p.part_list);
+        if (w == 0 && threadIdx.x == 0) p.part_list[4 * kMostTiles] = (int32_t)line.tiles;
         const uint64_t stop = line.first(w + 1);
         for (uint64_t u = line.first(w); u < stop;) {
             const uint32_t g = (uint32_t)(u / line.head), at = (uint32_t)(u - (uint64_t)g * line.head);
-            const int tile = __builtin_amdgcn_readfirstlane(last_upto(plan.unit0, (int)line.tiles, at));
-            const int b = __builtin_amdgcn_readfirstlane(last_upto(plan.tile0, p.batch, (uint32_t)tile));
-            const uint32_t begin = at - plan.unit0[tile], all = plan.unit0[tile + 1] - plan.unit0[tile];
+            const int i = __builtin_amdgcn_readfirstlane(last_upto(plan.unit0, (int)line.tiles, at));
+            const int b = __builtin_amdgcn_readfirstlane(last_upto(plan.tile0, p.batch, (uint32_t)i));
+            const RowTile t = plan.row_tile(b, i - (int)plan.tile0[b]);
+            const uint32_t begin = at - plan.unit0[i], all = plan.unit0[i + 1] - plan.unit0[i];
             const uint32_t end = begin + (stop - u) < all ? (uint32_t)(begin + (stop - u)) : all;
-            const int piece = begin == 0 && end == all ? -1 : 2 * (int)w + (begin == 0);
-            run(row_tile(p, b, tile - (int)plan.tile0[b]), (int)g, (int)begin, (int)end, piece);
+            if (begin == 0 && threadIdx.x == 0)
+                list[(uint32_t)i * p.Hkv + g] = Pieces{(int32_t)(line.owner(u + all - 1) - w) + 1, (int32_t)w, b, t.tile};
+            run(t, tile_pos(p, plan.pos[b], t), (int)g, (int)begin, (int)end, 2 * (int)w + (begin == 0));
             u += end - begin;
         }
     } else {
         RowTile t;
         if (!find_tile(p.cu, p.batch, p.T, p.tokens, blockIdx.x / p.Hkv, t)) return;
-        run(t, (int)(blockIdx.x % p.Hkv), 0, -1, -1);
+        run(t, tile_pos(p, first_pos(p, t.seq), t), (int)(blockIdx.x % p.Hkv), 0, -1, -1);
     }
 }
 
-// The pieces of the row tiles that several parts share, joined: a workgroup takes a row tile of a
-// KV head and its rows blockIdx.y, + gridDim.y, ...; the threads find the largest reference and
-// each piece's factor together, then D / 4 lanes of four dims each sum over every kGroups-th
-// piece.
+// The pieces of the row tiles that are in several, joined: a workgroup takes a row tile of a KV
+// head and its rows from blockIdx.y on.  Few pieces: a wave a row.  Many: the threads find
+// the largest reference and each piece's factor together, then D / 4 lanes of four dims each sum
+// over every kGroups-th piece.
+constexpr int kFewPieces = 16;
+
+struct RowRef {
+    float top, topc;
+    bool far;
+    __device__ __forceinline__ void meet(const f32x4_t& ml) {
+        topc = top < ml[0] ? ml[1] : topc;
+        top = fmaxf(top, ml[0]);
+        far |= far_ref(ml[1]);
+    }
+    // Over the wave.
+    __device__ __forceinline__ void join() {
+        const float all = wave_max(top);
+        topc = __shfl(topc, (int)__builtin_ctzll(__ballot(top == all)));
+        top = all;
+        far = __any(far);
+    }
+};
+
 template <int D>
 __global__ __launch_bounds__(kPlanThreads) void k_page_join(PageAttnParams p) {
     constexpr int kLanes = D / 4, kGroups = kPlanThreads / kLanes;
-    __shared__ Plan plan;
     __shared__ float factor[kMostParts];
     __shared__ float red[kWaves][4];
     __shared__ __align__(16) float osum[kGroups][D];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const Line line = make_plan(p, plan);
     const uint32_t tile = blockIdx.x / p.Hkv, g = blockIdx.x % p.Hkv;
-    if (tile >= line.tiles) return;
-    const uint64_t u = (uint64_t)g * line.head + plan.unit0[tile];
-    const uint32_t w0 = line.owner(u), n = line.owner(u + (plan.unit0[tile + 1] - plan.unit0[tile]) - 1) - w0 + 1;
+    if (tile >= (uint32_t)p.part_list[4 * kMostTiles]) return;
+    const Pieces all = reinterpret_cast<const Pieces*>(p.part_list)[blockIdx.x];
+    const int n = all.count;
     if (n == 1) return;
-    const int b = __builtin_amdgcn_readfirstlane(last_upto(plan.tile0, p.batch, tile));
-    const RowTile t = row_tile(p, b, (int)(tile - plan.tile0[b]));
+    RowTile t;
+    t.seq = all.seq;
+    t.first = clip_offset(p.cu[all.seq], p.T);
+    t.len = clip_offset(p.cu[all.seq + 1], p.T) - t.first;
+    t.tile = all.tile;
     const int rows = tile_tokens(p, t) * p.G;
-    // the first piece is the end of part w0, the others begin their parts
-    const auto piece = [&](uint32_t i) { return (int64_t)(2 * (w0 + i) + (i == 0)) * p.part_rows; };
-    for (int r = blockIdx.y; r < rows; r += gridDim.y) {
-        float top = -INFINITY, topc = 0.f;
-        bool far = false;
-        for (uint32_t i = tid; i < n; i += kPlanThreads) {
-            const f32x4_t ml = *reinterpret_cast<const f32x4_t*>(p.part_ml + 4 * (piece(i) + r));
-            topc = top < ml[0] ? ml[1] : topc;
-            top = fmaxf(top, ml[0]);
-            far |= far_ref(ml[1]);
+    const auto piece = [&](int i) __attribute__((always_inline)) { return (int64_t)(2 * (all.part + i) + (i == 0)) * p.part_rows; };
+    const auto sums = [&](int i, int r) __attribute__((always_inline)) {
+        return *reinterpret_cast<const f32x4_t*>(p.part_ml + 4 * (piece(i) + r));
+    };
+    const auto place = [&](int r) __attribute__((always_inline)) {
+        const int tok = r / p.G, h = (int)g * p.G + (r - tok * p.G);
+        return h * p.o_head + (int64_t)(t.first + t.tile * p.tokens + tok) * p.o_token;
+    };
+    if (n <= kFewPieces) {
+        constexpr int kEach = D / 64;           // dims of a lane
+        for (int r = (int)blockIdx.y * kWaves + wave; r < rows; r += (int)gridDim.y * kWaves) {
+            f32x4_t ml = {-INFINITY, 0.f, 0.f, 0.f};
+            if (lane < n) ml = sums(lane, r);
+            RowRef ref{-INFINITY, 0.f, false};
+            ref.meet(ml);
+            ref.join();
+            const float a = join_factor<false>(ml[0], ml[1], ref.top, ref.topc, ref.far, p.c);
+            const float l = wave_sum(ml[2] * a), seen = wave_sum(ml[3]);
+            float y[kEach] = {};
+#pragma unroll 4
+            for (int i = 0; i < n; ++i) {
+                const float* x = p.part_o + (piece(i) + r) * D + kEach * lane;
+                const float f = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(a), i));
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) y[e] = add_scaled<true>(y[e], x[e], f);
+            }
+            const int64_t at = place(r) + kEach * lane;
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) {
+                const float v = seen == 0.f ? 0.f : y[e] / l;
+                if (p.out_bf16) static_cast<uint16_t*>(p.out)[at + e] = f32_to_bf16(v);
+                else static_cast<float*>(p.out)[at + e] = v;
+            }
         }
-        const float wtop = wave_max(top);
-        const uint64_t has = __ballot(top == wtop);         // none where top is NaN: not raised to one
-        topc = __shfl(topc, has ? (int)__builtin_ctzll(has) : 0);
-        far = __any(far);
+        return;
+    }
+    for (int r = blockIdx.y; r < rows; r += gridDim.y) {
+        RowRef ref{-INFINITY, 0.f, false};
+        for (int i = tid; i < n; i += kPlanThreads) ref.meet(sums(i, r));
+        ref.join();
         __syncthreads();
         if (lane == 0) {
-            red[wave][0] = wtop;
-            red[wave][1] = topc;
-            red[wave][2] = far ? 1.f : 0.f;
+            red[wave][0] = ref.top;
+            red[wave][1] = ref.topc;
+            red[wave][2] = ref.far ? 1.f : 0.f;
         }
         __syncthreads();
-        top = -INFINITY;
-        topc = 0.f;
-        far = false;
+        ref = RowRef{-INFINITY, 0.f, false};
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-            topc = top < red[w][0] ? red[w][1] : topc;
-            top = fmaxf(top, red[w][0]);
-            far |= red[w][2] != 0.f;
+            ref.topc = ref.top < red[w][0] ? red[w][1] : ref.topc;
+            ref.top = fmaxf(ref.top, red[w][0]);
+            ref.far |= red[w][2] != 0.f;
         }
         float l = 0.f, seen = 0.f;
-        for (uint32_t i = tid; i < n; i += kPlanThreads) {
-            const f32x4_t ml = *reinterpret_cast<const f32x4_t*>(p.part_ml + 4 * (piece(i) + r));
-            const float a = join_factor<false>(ml[0], ml[1], top, topc, far, p.c);
+        for (int i = tid; i < n; i += kPlanThreads) {
+            const f32x4_t ml = sums(i, r);
+            const float a = join_factor<false>(ml[0], ml[1], ref.top, ref.topc, ref.far, p.c);
             factor[i] = a;
             l = fmaf(ml[2], a, l);
             seen += ml[3];
@@ -588,7 +606,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_page_join(PageAttnParams p) {
         __syncthreads();
         f32x4_t o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-        for (uint32_t i = grp; i < n; i += kGroups) {
+        for (int i = grp; i < n; i += kGroups) {
             const f32x4_t x = *reinterpret_cast<const f32x4_t*>(p.part_o + (piece(i) + r) * D + d4);
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[e] = add_scaled<true>(o[e], x[e], factor[i]);
@@ -605,8 +623,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_page_join(PageAttnParams p) {
             f32x4_t y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int k = 0; k < kGroups; ++k) y += *reinterpret_cast<const f32x4_t*>(&osum[k][d4]);
-            const int tok = r / p.G, h = g * p.G + (r - tok * p.G);
-            const int64_t at = h * p.o_head + (int64_t)(t.first + t.tile * p.tokens + tok) * p.o_token + d4;
+            const int64_t at = place(r) + d4;
             if (seen == 0.f) store4(p, at, 0.f, 0.f, 0.f, 0.f);
             else store4(p, at, y[0] / l, y[1] / l, y[2] / l, y[3] / l);
         }
@@ -620,14 +637,15 @@ int64_t page_attn_blocks(const PageAttnParams& p) { return tile_places(p.T, p.ba
 // Workgroups that share the units, as many as the card holds at once; 0: a workgroup to a
 // row tile.
 int32_t page_attn_parts(const PageAttnParams& p) {
-    if (p.batch > kPlanSeqs || p.T / p.tokens + p.batch > kPlanTiles) return 0;
+    if (p.batch > kPlanSeqs) return 0;
     if (p.map.places <= kSoloKeys || p.map.places > kMostPlanned) return 0;
-    if (page_attn_blocks(p) >= 1024) return 0;      // they fill the card by themselves
+    if ((p.T / p.tokens + p.batch) * p.Hkv >= kMostTiles) return 0;      // they fill the card by themselves
     return p.D == 128 ? 512 : 768;
 }
 
-int64_t page_attn_workspace(const PageAttnParams& p) {
-    return 2 * (int64_t)p.parts * p.part_rows * (p.D + 4) * (int64_t)sizeof(float);
+int64_t page_attn_pieces(const PageAttnParams& p) {
+    if (!p.step) return 2 * (int64_t)p.parts;
+    return p.parts > p.part_waves ? page_attn_blocks(p) * (p.parts / p.part_waves) : 0;        // a row tile's only workgroup writes out itself
 }
 
 template <int D>
@@ -640,13 +658,14 @@ static hipError_t launch_page_attn_d(const PageAttnParams& p, hipStream_t st) {
     hipLaunchKernelGGL((k_page_attn<D, true>), dim3((unsigned)p.parts), dim3(64 * kWaves), 0, st, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    int64_t deal = 1024 / tiles;                    // rows side by side where row tiles are few
+    int64_t deal = 2048 / tiles;                    // rows side by side where row tiles are few
     deal = deal < 1 ? 1 : (deal > p.part_rows ? p.part_rows : deal);
     hipLaunchKernelGGL(k_page_join<D>, dim3((unsigned)tiles, (unsigned)deal), dim3(kPlanThreads), 0, st, p);
     return hipGetLastError();
 }
 
 hipError_t launch_page_attn(const PageAttnParams& p, hipStream_t st) {
+    if (p.step) return launch_page_step(p, st);
     return p.D == 128 ? launch_page_attn_d<128>(p, st) : launch_page_attn_d<64>(p, st);
 }
 

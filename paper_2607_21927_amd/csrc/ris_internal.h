@@ -223,18 +223,26 @@ struct PageAttnParams {
     int32_t tokens;               // of a row tile: `tokens` tokens of the G heads of a group
     int32_t window, sink;
     int32_t out_bf16;
-    int32_t parts;                // workgroups that share the key tiles of all row tiles; 0: one a row tile
+    int32_t step;                 // step form: row tiles of up to 16 rows, `parts` waves to each
+    int32_t parts;                // else: workgroups that share the key tiles of all row tiles; 0: one a row tile
+    int32_t part_waves;           // step form: waves of a workgroup
     int32_t part_rows;            // rows of a piece in the workspace
-    float* part_o;                // [2 parts, part_rows, D] unnormalised outputs
-    float* part_ml;               // [2 parts, part_rows, 4] their references, sums, whether anything was attended to
+    float* part_o;                // [pieces, part_rows, D] unnormalised outputs
+    float* part_ml;               // [pieces, part_rows, 4] their references, sums, whether anything was attended to
+    int32_t* part_list;           // kPartList of them, what the second launch needs
     float c;                      // score scale in the log2 domain
     float slack;                  // scores above the reference maximum before it moves
 };
+constexpr int kPartList = 4 * 1024 + 4;
 constexpr int kPageRows = 128;    // rows of a row tile at most
 int64_t page_attn_blocks(const PageAttnParams& p);
 int32_t page_attn_parts(const PageAttnParams& p);
-int64_t page_attn_workspace(const PageAttnParams& p);
+int64_t page_attn_pieces(const PageAttnParams& p);
 hipError_t launch_page_attn(const PageAttnParams& p, hipStream_t st);
+constexpr int kMostStepGroups = 256;                                      // workgroups of a row tile
+int32_t page_step_tokens(int64_t T, int32_t batch, int32_t G);            // tokens of its row tiles; 0: not for the step form
+void page_step_waves(PageAttnParams* p);
+hipError_t launch_page_step(const PageAttnParams& p, hipStream_t st);
 
 // Products with 4-bit weights, in tiles of 16 outputs x 128 inputs.
 struct W4Params {

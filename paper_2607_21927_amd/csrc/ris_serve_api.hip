@@ -183,15 +183,26 @@ int page_attn_params(const ris_page_attn_desc* d, ris::PageAttnParams* p) {
     p->q_head = d->q_head; p->q_token = d->q_token; p->o_head = d->o_head; p->o_token = d->o_token;
     p->Hq = d->Hq; p->Hkv = d->Hkv; p->G = d->Hq / d->Hkv; p->D = d->D;
     p->batch = d->batch;
-    p->tokens = ris::kPageRows / p->G;
+    p->tokens = ris::page_step_tokens(d->T, d->batch, p->G);
+    p->step = p->tokens > 0;
+    if (!p->step) p->tokens = ris::kPageRows / p->G;
     p->window = d->window; p->sink = d->sink;
     p->out_bf16 = d->dtype_out == RIS_BF16;
     p->c = (d->scale > 0.0f ? d->scale : 1.0f / sqrtf((float)d->D)) * kLog2e;
     p->slack = fminf(8.0f / p->c, FLT_MAX);       // -inf + slack stays -inf
-    p->parts = ris::page_attn_parts(*p);
+    if (p->step) ris::page_step_waves(p);
+    else p->parts = ris::page_attn_parts(*p);
     p->part_rows = (int32_t)(d->T < p->tokens ? d->T : p->tokens) * p->G;
-    if (!fits_dispatch(ris::page_attn_blocks(*p), 256)) return RIS_E_UNSUPPORTED;
+    const int64_t blocks = ris::page_attn_blocks(*p);
+    if (!fits_dispatch(blocks, 256) || (p->step && !fits_dispatch(blocks * p->parts, 64)) ||
+        (ris::page_attn_pieces(*p) > 0 && !fits_dispatch(blocks * p->part_rows, 256)))
+        return RIS_E_UNSUPPORTED;
     return RIS_OK;
+}
+
+int64_t page_attn_workspace(const ris::PageAttnParams& p) {
+    const int64_t pieces = ris::page_attn_pieces(p);
+    return pieces > 0 ? (pieces * p.part_rows * (p.D + 4) + ris::kPartList) * (int64_t)sizeof(float) : 0;
 }
 
 // Sizes of 4-bit weights whose tiles a launch can count.
@@ -369,7 +380,7 @@ int ris_page_store(const void* Q, void* Qout, const void* K, const void* V, cons
 int64_t ris_page_attn_workspace_bytes(const ris_page_attn_desc* desc) {
     ris::PageAttnParams p;
     const int st = page_attn_params(desc, &p);
-    return st == RIS_OK ? ris::page_attn_workspace(p) : st;
+    return st == RIS_OK ? page_attn_workspace(p) : st;
 }
 
 int ris_page_attn(const void* Q, const void* Kp, const void* Vp, const int32_t* table, const int64_t* cu_seqlens,
@@ -382,11 +393,12 @@ int ris_page_attn(const void* Q, const void* Kp, const void* Vp, const int32_t* 
     if (!vector_rows(Q, p.q_head, p.q_token, RIS_BF16) || !aligned(Kp, 16) || !aligned(Vp, 16) ||
         !output_rows(out, p.o_head, p.o_token, desc->dtype_out, p.Hq, p.T))
         return RIS_E_ARG;
-    const int64_t need = ris::page_attn_workspace(p);
+    const int64_t need = page_attn_workspace(p);
     if (need > 0 && (!workspace || !aligned(workspace, 16))) return RIS_E_ARG;
     if (workspace_bytes < need) return RIS_E_CAPACITY;
     p.part_o = static_cast<float*>(workspace);
-    p.part_ml = p.part_o + 2 * (int64_t)p.parts * p.part_rows * p.D;
+    p.part_ml = p.part_o + ris::page_attn_pieces(p) * p.part_rows * p.D;
+    p.part_list = reinterpret_cast<int32_t*>(p.part_ml + ris::page_attn_pieces(p) * p.part_rows * 4);
     p.Q = Q; p.K = Kp; p.V = Vp; p.cu = cu_seqlens; p.start = start; p.out = out;
     p.map.table = table;
     return hip_status(ris::launch_page_attn(p, static_cast<hipStream_t>(stream)));

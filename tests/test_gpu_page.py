@@ -225,9 +225,10 @@ def test_what_is_not_attended_to_does_not_count():
     check(serve, q, Kp, Vp, table, cu, start, window=20, sink=2, what="in some rows' windows")
 
 
-def test_infinite_values_count_whatever_their_weight():
+@pytest.mark.parametrize("n,p", [(3, 400), (1, 3000), (100, 400), (40, 5000)])
+def test_infinite_values_count_whatever_their_weight(n, p):
     serve = need_serve()
-    q, Kp, Vp, table, cu, start = held([3], [400], 64, 2, 1, 64, seed=8)
+    q, Kp, Vp, table, cu, start = held([n], [p], 64, 2, 1, 64, seed=8)
     Kp *= 40.0
     where = o_srv.page_places(table[0], 64, Kp.shape[0])
     Vp[where[7, 0], :, where[7, 1], 11] = math.inf
@@ -239,20 +240,24 @@ def test_scores_far_from_zero():
     """Scores around +-30,000 with differences of a few units: weights are those differences'."""
     serve = need_serve()
     for sign in (1.0, -1.0):
-        q, Kp, Vp, table, cu, start = held([2, 70], [900, 0], 32, 4, 1, 64, seed=9)
-        Kp[..., 0], q[..., 0] = 512.0, sign * 512.0
-        check(serve, q, Kp, Vp, table, cu, start, scale=0.125, what=f"far {sign}")
+        for lens, start in (([2, 70], [900, 0]), ([2, 1], [900, 3]), ([60, 1], [10, 100])):
+            q, Kp, Vp, table, cu, start = held(lens, start, 32, 4, 1, 64, seed=9)
+            Kp[..., 0], q[..., 0] = 512.0, sign * 512.0
+            check(serve, q, Kp, Vp, table, cu, start, scale=0.125, what=f"far {sign} {lens}")
+            check(serve, q, Kp, Vp, table, cu, start, scale=2.0**14, what=f"farther {sign} {lens}")
 
 
-def test_scores_of_minus_infinity_alone():
+@pytest.mark.parametrize("n,p", [(1, 70), (1, 5000), (90, 70), (90, 3000)])
+def test_scores_of_minus_infinity_alone(n, p):
+    """NaN, though zeros where there is no score at all; a NaN query is its own row's alone."""
     serve = need_serve()
-    q, Kp, Vp, table, cu, start = held([1, 1], [70, 30], 16, 2, 1, 64, seed=2)
-    for j in range(71):
-        w = o_srv.page_places(table[0], 16, Kp.shape[0])[j]
-        Kp[w[0], 0, w[1], 0] = -math.inf
-    q[:, 0, 0], q[0, 1] = 1.0, math.nan
+    q, Kp, Vp, table, cu, start = held([n, 1, n], [p, 30, 0], 16, 2, 1, 64, seed=2)
+    where = o_srv.page_places(table[0], 16, Kp.shape[0])[:p + n]
+    Kp[where[:, 0], 0, where[:, 1], 0] = -math.inf
+    q[:, :n, 0], q[0, n] = 1.0, math.nan
+    table[2] = -1
     out = attend(serve, q, Kp, Vp, ids(table, torch.int32), cu, ids(start))
-    assert out[:, 0].isnan().all() and out[0, 1].isnan().all() and out[1, 1].isfinite().all()
+    assert out[:, :n].isnan().all() and out[0, n].isnan().all() and out[1, n].isfinite().all() and not out[:, n + 1:].any()
 
 
 def test_scales():
