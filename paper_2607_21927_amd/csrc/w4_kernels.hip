@@ -6,11 +6,16 @@
 // That is the A operand of four v_mfma_f32_16x16x32_bf16 as it stands, eight codes each
 // (their contraction slots 8 (l / 16) .. hold the inputs 32 (l / 16) + 8 s ..); one
 // instruction makes two codes bf16, scale included, exactly.  x is the B operand: lane l holds row
-// l % 16 at the same inputs.  The waves of a workgroup deal the chunks of 128 inputs among them
-// and meet in LDS.  All products are exact, sums are float32.
+// l % 16 at the same inputs.  All products are exact, sums are float32.
 //
 // float32 rows are taken as three bf16 parts, cut off and not rounded, whose sum is the
 // float32 value exactly: three products for one.
+//
+// Two forms.  k_w4_narrow: a workgroup takes one set of 16 outputs, its waves deal the chunks of
+// 128 inputs among them, each reads the rows itself, and meet in LDS: enough workgroups where outputs
+// are few, nothing to wait for but the loads.  k_w4_wide: four waves side by side take NT sets each and
+// share the rows through LDS, since reading them for every 16 outputs would take longer than the
+// weights do.
 #include "mxfp4.h"
 #include "ris_internal.h"
 
@@ -35,160 +40,328 @@ __device__ __forceinline__ uint32_t two(float lo, float hi) {      // the upper 
 }
 __device__ __forceinline__ float cut(float x) { return __uint_as_float(__float_as_uint(x) & 0xFFFF0000u); }
 
+// The same as they lie in memory, and into parts.
 template <bool F32>
-__device__ __forceinline__ void load_part(const void* x, int64_t row, int k, int K, Part<F32>& p) {
+struct Raw {
+    u32x4_t v[F32 ? 2 : 1];
+};
+
+template <bool F32>
+__device__ __forceinline__ void load_raw(const void* x, int64_t row, int k, int K, Raw<F32>& r) {
     if constexpr (!F32) {
         const uint16_t* q = static_cast<const uint16_t*>(x) + row + k;
         if (k + 8 <= K) {
-            p.b[0] = *reinterpret_cast<const u32x4_t*>(q);
+            r.v[0] = *reinterpret_cast<const u32x4_t*>(q);
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                p.b[0][i] = (k + 2 * i < K ? q[2 * i] : 0u) | (k + 2 * i + 1 < K ? (uint32_t)q[2 * i + 1] << 16 : 0u);
+                r.v[0][i] = (k + 2 * i < K ? q[2 * i] : 0u) | (k + 2 * i + 1 < K ? (uint32_t)q[2 * i + 1] << 16 : 0u);
         }
     } else {
-        const float* q = static_cast<const float*>(x) + row + k;
-        float f[8];
+        const uint32_t* q = static_cast<const uint32_t*>(x) + row + k;
         if (k + 8 <= K) {
-            const f32x4_t a = *reinterpret_cast<const f32x4_t*>(q), b = *reinterpret_cast<const f32x4_t*>(q + 4);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                f[i] = a[i];
-                f[4 + i] = b[i];
-            }
+            r.v[0] = *reinterpret_cast<const u32x4_t*>(q);
+            r.v[1] = *reinterpret_cast<const u32x4_t*>(q + 4);
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = k + i < K ? q[i] : 0.f;
+            for (int i = 0; i < 8; ++i) r.v[i / 4][i % 4] = k + i < K ? q[i] : 0u;
         }
+    }
+}
+
+template <bool F32>
+__device__ __forceinline__ Part<F32> parts_of(const Raw<F32>& r) {
+    Part<F32> p;
+    if constexpr (!F32) {
+        p.b[0] = r.v[0];
+    } else {
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
-            float v[2] = {f[i], f[i + 1]}, mid[2], low[2];
+            float v[2] = {__uint_as_float(r.v[i / 4][i % 4]), __uint_as_float(r.v[i / 4][i % 4 + 1])}, mid[2], low[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 if (v[e] != v[e]) v[e] = __uint_as_float(0x7FC00000u);       // a NaN's upper half may be an infinity's
-                const float r = isfinite(v[e]) ? v[e] - cut(v[e]) : 0.f;
-                mid[e] = r;
-                low[e] = r - cut(r);
+                const float rest = isfinite(v[e]) ? v[e] - cut(v[e]) : 0.f;
+                mid[e] = rest;
+                low[e] = rest - cut(rest);
             }
             p.b[0][i / 2] = two(v[0], v[1]);
             p.b[1][i / 2] = two(mid[0], mid[1]);
             p.b[2][i / 2] = two(low[0], low[1]);
         }
     }
+    return p;
 }
 
 __device__ __forceinline__ float silu(float g) { return g / (1.f + __expf(-g)); }
 
-// MT tiles of 16 rows of x, NT of 16 outputs (gated: NT of the gate's and the same of the
-// other half's), WV waves.
-template <bool F32, bool GATED, int MT, int NT, int WV>
-__global__ __launch_bounds__(64 * WV) void k_w4_linear(W4Params p) {
-    constexpr int NS = GATED ? 2 * NT : NT;             // sets of 16 outputs
-    __shared__ __align__(16) f32x4_t sum[WV > 1 ? WV - 1 : 1][NS * MT][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, lg = lane >> 4;
+// Where lane `lane` finds its part of a tile, and of chunk kc's scales.
+__device__ __forceinline__ const u32x4_t* codes_at(const W4Params& p, int tile, int chunks, int kc, int lane) {
+    return reinterpret_cast<const u32x4_t*>(p.C + (((int64_t)tile * chunks + kc) * 64 + lane) * 16);
+}
+__device__ __forceinline__ uint32_t scale_at(const W4Params& p, int tile, int quads, int kc, int lane) {
+    return p.S[(((int64_t)tile * quads + (kc >> 2)) * 64 + lane) * 4 + (kc & 3)];
+}
+
+template <bool F32>
+__device__ __forceinline__ f32x4_t product(u32x4_t w, const Part<F32>& x, f32x4_t acc) {
+#pragma unroll
+    for (int i = Part<F32>::kCount - 1; i >= 0; --i)
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(w), as_bf16x8(x.b[i]), acc, 0, 0, 0);
+    return acc;
+}
+
+// The outputs 4 (l / 16) .. of tile t of row r (of the first half, and of the second, gated).
+template <bool F32, bool GATED>
+__device__ __forceinline__ void store_outputs(const W4Params& p, int r, int t, f32x4_t acc, f32x4_t up) {
+    const int N = GATED ? p.N / 2 : p.N, o = 16 * t + 4 * ((threadIdx.x & 63) >> 4);
+    if (r >= p.rows || o >= N) return;
+    const auto biased = [&](float v, int col) __attribute__((always_inline)) {
+        if (!p.bias) return v;
+        return v + (F32 ? static_cast<const float*>(p.bias)[col] : bf16_to_f32(static_cast<const uint16_t*>(p.bias)[col]));
+    };
+    float y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int at = o + i < N ? o + i : N - 1;
+        y[i] = biased(acc[i], at);
+        if constexpr (GATED) y[i] = silu(y[i]) * biased(up[i], N + at);
+    }
+    const int64_t to = (int64_t)r * p.out_stride + o;
+    if constexpr (F32) {
+        float* q = static_cast<float*>(p.out) + to;
+        if (p.vector_out) {
+            *reinterpret_cast<f32x4_t*>(q) = f32x4_t{y[0], y[1], y[2], y[3]};
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (o + i < N) q[i] = y[i];
+        }
+    } else {
+        uint16_t* q = static_cast<uint16_t*>(p.out) + to;
+        if (p.vector_out) {
+            *reinterpret_cast<uint2*>(q) = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (o + i < N) q[i] = f32_to_bf16(y[i]);
+        }
+    }
+}
+
+// Set t of 16 outputs as tiles: itself, and gated the one of the other half.
+template <bool GATED>
+struct Sets {
+    static constexpr int kCount = GATED ? 2 : 1;
+    static __device__ __forceinline__ int tile(int t, int i, int sets) { return GATED && i ? sets + t : t; }
+};
+
+// MT tiles of 16 rows of x; WV waves, each with a chunk of the rows in LDS at a time and the loads of U - 1 more on
+// their way.
+template <bool F32, bool GATED, int MT, int WV, int U>
+__global__ __launch_bounds__(64 * WV) void k_w4_narrow(W4Params p) {
+    constexpr int NS = Sets<GATED>::kCount, kParts = Part<F32>::kCount, kPlane = 16 * MT * kChunk, NP = 4 * MT;
+    constexpr int kStage = WV * kParts * kPlane * 2, kMeet = WV * NS * MT * 64 * 16;
+    __shared__ __align__(16) uint8_t mem[kStage > kMeet ? kStage : kMeet];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15, lg = lane >> 4;
     const int chunks = (int)chunks_of(p.K), quads = (int)quads_of(p.K);
-    const int tiles = (int)tiles_of(GATED ? p.N / 2 : p.N);
-    // row blocks of one set of tiles one after another on one XCD
+    const int sets = (int)tiles_of(GATED ? p.N / 2 : p.N);
+    // row blocks of one set one after another on one XCD
     const int blocks = (p.rows + 16 * MT - 1) / (16 * MT);
     const uint32_t xcd = blockIdx.x & 7u, slot = blockIdx.x >> 3;
-    const int t0 = (int)(slot / blocks * 8u + xcd) * NT, m0 = (int)(slot % blocks) * 16 * MT;
-    if (t0 >= tiles) return;
+    const int t = (int)(slot / blocks * 8u + xcd), m0 = (int)(slot % blocks) * 16 * MT;
+    if (t >= sets) return;
+    f32x4_t acc[NS][MT];
+#pragma unroll
+    for (int n = 0; n < NS; ++n)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[n][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    // Piece i of a lane: eight inputs of row lane / 16 + 4 i of a chunk, 16-byte place c of the row at c ^ row % 16.
+    // Rows that are not there are not loaded: what is in their place reaches outputs that are not there alone.
+    uint16_t* const stage = reinterpret_cast<uint16_t*>(mem) + wave * kParts * kPlane;
+    const int have = p.rows - m0, pk = 8 * li;
+    const char* const x0 = static_cast<const char*>(p.x) + (int64_t)m0 * p.x_stride * (F32 ? 4 : 2);
+    u32x4_t code[U][NS];
+    uint32_t byte[U][NS];
+    Raw<F32> x[U][NP];
+    const auto load = [&](int k, int u) __attribute__((always_inline)) {
+        const int kc = k < chunks ? k : chunks - 1;
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+            code[u][n] = *codes_at(p, Sets<GATED>::tile(t, n, sets), chunks, kc, lane);
+            byte[u][n] = scale_at(p, Sets<GATED>::tile(t, n, sets), quads, kc, lane);
+        }
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+            if (4 * i < have) {
+                const int r = lg + 4 * i < have ? lg + 4 * i : have - 1;
+                load_raw<F32>(x0, r * p.x_stride, kc * kChunk + pk, p.K, x[u][i]);
+            }
+    };
+#pragma unroll
+    for (int u = 0; u < U - 1; ++u) load(wave + u * WV, u);
+    for (int k0 = wave; k0 < chunks; k0 += U * WV) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int kc = k0 + u * WV;
+            if (kc >= chunks) break;
+            load(kc + (U - 1) * WV, (u + U - 1) % U);
+#pragma unroll
+            for (int i = 0; i < NP; ++i)
+                if (4 * i < have) {
+                    const Part<F32> b = parts_of<F32>(x[u][i]);
+                    const int r = lg + 4 * i;
+#pragma unroll
+                    for (int e = 0; e < kParts; ++e)
+                        *reinterpret_cast<u32x4_t*>(stage + e * kPlane + r * kChunk + 8 * (li ^ (r & 15))) = b.b[e];
+                }
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                Part<F32> b[MT];
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int e = 0; e < kParts; ++e)
+                        b[m].b[e] = *reinterpret_cast<const u32x4_t*>(stage + e * kPlane + (16 * m + li) * kChunk + 8 * ((4 * lg + s) ^ li));
+#pragma unroll
+                for (int n = 0; n < NS; ++n) {
+                    const u32x4_t w = decode8(code[u][n][s], scale_of(byte[u][n]));
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) acc[n][m] = product<F32>(w, b[m], acc[n][m]);
+                }
+            }
+        }
+    }
+    f32x4_t* const sum = reinterpret_cast<f32x4_t*>(mem) + lane;
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < NS; ++n)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) sum[((wave * NS + n) * MT + m) * 64] = acc[n][m];
+    __syncthreads();
+    if (wave >= MT) return;                 // wave m adds up row tile m
+    f32x4_t all[NS];
+#pragma unroll
+    for (int n = 0; n < NS; ++n) {
+        all[n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < WV; ++w) all[n] += sum[((w * NS + n) * MT + wave) * 64];
+    }
+    store_outputs<F32, GATED>(p, m0 + 16 * wave + li, t, all[0], all[NS - 1]);
+}
+
+// MT tiles of 16 rows of x in LDS, one chunk of inputs after another, two deep; KW groups of four waves deal the
+// chunks among them, a wave has NT sets of 16 outputs.
+template <bool F32, bool GATED, int MT, int NT, int KW>
+__global__ __launch_bounds__(256 * KW) void k_w4_wide(W4Params p) {
+    constexpr int NS = Sets<GATED>::kCount * NT, kParts = Part<F32>::kCount, kPlane = 16 * MT * kChunk;
+    constexpr int kStage = 2 * KW * kParts * kPlane * 2, kMeet = (KW - 1) * 4 * NS * MT * 64 * 16;
+    __shared__ __align__(16) uint8_t mem[kStage > kMeet ? kStage : kMeet];
+    const int lane = threadIdx.x & 63, li = lane & 15, lg = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6 & 3), way = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
+    const int tid = threadIdx.x & 255;
+    const int chunks = (int)chunks_of(p.K), quads = (int)quads_of(p.K);
+    const int sets = (int)tiles_of(GATED ? p.N / 2 : p.N);
+    const int blocks = (p.rows + 16 * MT - 1) / (16 * MT);
+    const uint32_t xcd = blockIdx.x & 7u, slot = blockIdx.x >> 3;
+    const int t0 = ((int)(slot / blocks * 8u + xcd) * 4 + wave) * NT, m0 = (int)(slot % blocks) * 16 * MT;
+    if (t0 - wave * NT >= sets) return;
     int tile[NS];
 #pragma unroll
     for (int n = 0; n < NS; ++n) {
-        const int t = t0 + n % NT < tiles ? t0 + n % NT : tiles - 1;
-        tile[n] = GATED && n >= NT ? tiles + t : t;
+        const int t = t0 + n % NT < sets ? t0 + n % NT : sets - 1;
+        tile[n] = Sets<GATED>::tile(t, n / NT, sets);
     }
     f32x4_t acc[NS][MT];
 #pragma unroll
     for (int n = 0; n < NS; ++n)
 #pragma unroll
         for (int m = 0; m < MT; ++m) acc[n][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    // Piece i of a thread: eight inputs of row tid / 16 + 16 i of a chunk, 16-byte place c of the row at c ^ row % 16.
+    uint16_t* const stage = reinterpret_cast<uint16_t*>(mem) + way * 2 * kParts * kPlane;
+    const int pr = tid >> 4, pk = 8 * (tid & 15);
     int64_t row[MT];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-        const int r = m0 + 16 * m + li;
+        const int r = m0 + 16 * m + pr;
         row[m] = (int64_t)(r < p.rows ? r : p.rows - 1) * p.x_stride;
     }
-    for (int kc = wave; kc < chunks; kc += WV) {
-        u32x4_t code[NS];
-        uint32_t byte[NS];
+    const int put = pr * kChunk + 8 * ((tid & 15) ^ pr);
+    Raw<F32> x[MT];
+    u32x4_t code[NS], next[NS];
+    uint32_t byte[NS], next_byte[NS];
+    const auto load_x = [&](int kc) __attribute__((always_inline)) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) load_raw<F32>(p.x, row[m], kc * kChunk + pk, p.K, x[m]);
+    };
+    const auto load_w = [&](int kc, u32x4_t (&c)[NS], uint32_t (&b)[NS]) __attribute__((always_inline)) {
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
-            code[n] = *reinterpret_cast<const u32x4_t*>(p.C + (((int64_t)tile[n] * chunks + kc) * 64 + lane) * 16);
-            byte[n] = p.S[(((int64_t)tile[n] * quads + (kc >> 2)) * 64 + lane) * 4 + (kc & 3)];
+            c[n] = *codes_at(p, tile[n], chunks, kc, lane);
+            b[n] = scale_at(p, tile[n], quads, kc, lane);
         }
-        Part<F32> x[MT][4];
+    };
+    const int steps = (chunks + KW - 1) / KW;
+    const auto chunk = [&](int i) { return i * KW + way < chunks ? i * KW + way : chunks - 1; };
+    load_x(chunk(0));
+    load_w(chunk(0), next, next_byte);
+    for (int i = 0; i < steps; ++i) {
+        uint16_t* const to = stage + (i & 1) * kParts * kPlane;
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int m = 0; m < MT; ++m) {
+            const Part<F32> b = parts_of<F32>(x[m]);
 #pragma unroll
-            for (int s = 0; s < 4; ++s) load_part<F32>(p.x, row[m], kc * kChunk + 32 * lg + 8 * s, p.K, x[m][s]);
+            for (int e = 0; e < kParts; ++e) *reinterpret_cast<u32x4_t*>(to + e * kPlane + 16 * m * kChunk + put) = b.b[e];
+        }
 #pragma unroll
-        for (int n = 0; n < NS; ++n)
+        for (int n = 0; n < NS; ++n) {
+            code[n] = next[n];
+            byte[n] = next_byte[n];
+        }
+        if (i + 1 < steps) {
+            load_x(chunk(i + 1));
+            load_w(chunk(i + 1), next, next_byte);
+        }
+        __syncthreads();
+        if (i * KW + way >= chunks) continue;
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
+        for (int s = 0; s < 4; ++s) {
+            Part<F32> b[MT];
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int e = 0; e < kParts; ++e)
+                    b[m].b[e] = *reinterpret_cast<const u32x4_t*>(to + e * kPlane + (16 * m + li) * kChunk + 8 * ((4 * lg + s) ^ li));
+#pragma unroll
+            for (int n = 0; n < NS; ++n) {
                 const u32x4_t w = decode8(code[n][s], scale_of(byte[n]));
 #pragma unroll
-                for (int m = 0; m < MT; ++m)
-#pragma unroll
-                    for (int i = Part<F32>::kCount - 1; i >= 0; --i)
-                        acc[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(w), as_bf16x8(x[m][s].b[i]), acc[n][m], 0, 0, 0);
+                for (int m = 0; m < MT; ++m) acc[n][m] = product<F32>(w, b[m], acc[n][m]);
             }
+        }
     }
-    if (WV > 1 && wave > 0) {
+    if constexpr (KW > 1) {
+        f32x4_t* const sum = reinterpret_cast<f32x4_t*>(mem) + (wave * NS * MT) * 64 + lane;
+        __syncthreads();
+        if (way > 0) {
 #pragma unroll
-        for (int n = 0; n < NS; ++n)
+            for (int n = 0; n < NS; ++n)
 #pragma unroll
-            for (int m = 0; m < MT; ++m) sum[wave - 1][n * MT + m][lane] = acc[n][m];
+                for (int m = 0; m < MT; ++m) sum[((way - 1) * 4 * NS * MT + n * MT + m) * 64] = acc[n][m];
+        }
+        __syncthreads();
+        if (way > 0) return;
+#pragma unroll
+        for (int w = 0; w < KW - 1; ++w)
+#pragma unroll
+            for (int n = 0; n < NS; ++n)
+#pragma unroll
+                for (int m = 0; m < MT; ++m) acc[n][m] += sum[(w * 4 * NS * MT + n * MT + m) * 64];
     }
-    __syncthreads();
-    if (wave > 0) return;
-#pragma unroll
-    for (int w = 0; w < WV - 1; ++w)
-#pragma unroll
-        for (int n = 0; n < NS; ++n)
-#pragma unroll
-            for (int m = 0; m < MT; ++m) acc[n][m] += sum[w][n * MT + m][lane];
-    // lane l holds row l % 16 at the outputs 4 (l / 16) .. of a tile
-    const int N = GATED ? p.N / 2 : p.N;
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            const int r = m0 + 16 * m + li, o = 16 * (t0 + n) + 4 * lg;
-            if (r >= p.rows || o >= N) continue;
-            float y[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int at = o + i;
-                const auto biased = [&](float v, int col) __attribute__((always_inline)) {
-                    if (!p.bias || at >= N) return v;
-                    return v + (F32 ? static_cast<const float*>(p.bias)[col] : bf16_to_f32(static_cast<const uint16_t*>(p.bias)[col]));
-                };
-                y[i] = biased(acc[n][m][i], at);
-                if constexpr (GATED) y[i] = silu(y[i]) * biased(acc[NT + n][m][i], N + at);
-            }
-            const int64_t to = (int64_t)r * p.out_stride + o;
-            if constexpr (F32) {
-                float* q = static_cast<float*>(p.out) + to;
-                if (p.vector_out) {
-                    *reinterpret_cast<f32x4_t*>(q) = f32x4_t{y[0], y[1], y[2], y[3]};
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (o + i < N) q[i] = y[i];
-                }
-            } else {
-                uint16_t* q = static_cast<uint16_t*>(p.out) + to;
-                if (p.vector_out) {
-                    *reinterpret_cast<uint2*>(q) = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (o + i < N) q[i] = f32_to_bf16(y[i]);
-                }
-            }
-        }
+        for (int m = 0; m < MT; ++m) store_outputs<F32, GATED>(p, m0 + 16 * m + li, t0 + n, acc[n][m], acc[NS - NT + n][m]);
 }
 
 // A workgroup takes 16 outputs and 16 blocks of 32 inputs: four tiles.  Outputs from N on and
@@ -261,26 +434,55 @@ __global__ __launch_bounds__(256) void k_w4_load(const uint8_t* C, const uint8_t
     }
 }
 
-template <int MT, int NT, int WV>
-hipError_t launch_shape(const W4Params& p, hipStream_t st) {
-    const int64_t tiles = tiles_of(p.gated ? p.N / 2 : p.N), sets = (tiles + NT - 1) / NT;
-    const int64_t blocks = (p.rows + 16 * MT - 1) / (16 * MT);
-    const dim3 grid((unsigned)((sets + 7) / 8 * 8 * blocks));
-    const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * WV), 0, st, p); };
-    if (p.f32) p.gated ? run(k_w4_linear<true, true, MT, NT, WV>) : run(k_w4_linear<true, false, MT, NT, WV>);
-    else p.gated ? run(k_w4_linear<false, true, MT, NT, WV>) : run(k_w4_linear<false, false, MT, NT, WV>);
+// Grid of row blocks of `rows` rows beside `sets` sets of outputs, the sets dealt to the XCDs.
+int64_t grid_of(const W4Params& p, int64_t sets, int rows) { return (sets + 7) / 8 * 8 * (((int64_t)p.rows + rows - 1) / rows); }
+
+template <bool F32, int MT, int WV, int U>
+hipError_t narrow(const W4Params& p, hipStream_t st) {
+    const dim3 grid((unsigned)grid_of(p, tiles_of(p.gated ? p.N / 2 : p.N), 16 * MT));
+    if (p.gated) hipLaunchKernelGGL((k_w4_narrow<F32, true, MT, WV, U>), grid, dim3(64 * WV), 0, st, p);
+    else hipLaunchKernelGGL((k_w4_narrow<F32, false, MT, WV, U>), grid, dim3(64 * WV), 0, st, p);
+    return hipGetLastError();
+}
+
+template <bool F32, int MT, int NT, int KW>
+hipError_t wide(const W4Params& p, hipStream_t st) {
+    const int64_t sets = tiles_of(p.gated ? p.N / 2 : p.N);
+    constexpr int kGated = NT > 1 ? NT / 2 : 1;             // sets of either half
+    if (p.gated) {
+        const dim3 grid((unsigned)grid_of(p, (sets + 4 * kGated - 1) / (4 * kGated), 16 * MT));
+        hipLaunchKernelGGL((k_w4_wide<F32, true, MT, kGated, KW>), grid, dim3(256 * KW), 0, st, p);
+    } else {
+        const dim3 grid((unsigned)grid_of(p, (sets + 4 * NT - 1) / (4 * NT), 16 * MT));
+        hipLaunchKernelGGL((k_w4_wide<F32, false, MT, NT, KW>), grid, dim3(256 * KW), 0, st, p);
+    }
     return hipGetLastError();
 }
 
 }  // namespace
 
-int64_t w4_blocks(const W4Params& p) {
-    const int64_t tiles = tiles_of(p.gated ? p.N / 2 : p.N);
-    return (tiles + 7) / 8 * 8 * (((int64_t)p.rows + 15) / 16);
-}
+int64_t w4_blocks(const W4Params& p) { return grid_of(p, tiles_of(p.gated ? p.N / 2 : p.N), 16) * 4; }
 
+// The wide form from 512 tiles of outputs on, and for more than 128 rows (float32: 64), where the narrow one reads
+// the rows for every 16 outputs (us, bf16, narrow and wide: 2,048 outputs of 1,536 inputs, 16 rows 4.0, 6.0, 64
+// 6.5, 10.0, 256 14, 10.2; 1,536 of 8,960, 1 row 5.8, 22, 64 20.6, 40; 17,920 gated of 1,536, 1 row 8.4, 7.0, 32
+// 18, 8.2; 151,936 of 1,536, 1 row 65, 26.0, 64 227, 47).  Waves of the narrow form: by the chunks there are (1
+// row of 1,536 inputs 4.6 with 8, 5.3 with 16).  Ways of the wide form: two, so that few sets keep more waves busy (17,920
+// gated, 32 rows 10.1 with one, 7.4 with two, 7.5 with four; 151,936, 64 rows 45.5, 45.3, 65), float32's rows of more than 16 one,
+// for room in LDS.
 hipError_t launch_w4_linear(const W4Params& p, hipStream_t st) {
-    return p.rows <= 16 ? launch_shape<1, 1, 4>(p, st) : launch_shape<2, 1, 4>(p, st);
+    const int64_t tiles = tiles_of(p.N), chunks = chunks_of(p.K);
+    if (tiles >= 512 || p.rows > (p.f32 ? 64 : 128)) {
+        if (p.f32) return p.rows <= 16 ? wide<true, 1, 2, 2>(p, st) : wide<true, 2, 2, 1>(p, st);
+        if (p.rows <= 16) return wide<false, 1, 2, 2>(p, st);
+        return p.rows <= 32 ? wide<false, 2, 2, 2>(p, st) : wide<false, 4, 2, 2>(p, st);
+    }
+    if (p.f32) return p.rows <= 16 ? narrow<true, 1, 8, 2>(p, st) : narrow<true, 2, 4, 1>(p, st);
+    if (p.rows <= 16) {
+        if (chunks > 32) return narrow<false, 1, 16, 2>(p, st);
+        return chunks > 8 ? narrow<false, 1, 8, 2>(p, st) : narrow<false, 1, 4, 2>(p, st);
+    }
+    return p.rows <= 32 ? narrow<false, 2, 8, 2>(p, st) : narrow<false, 4, 8, 1>(p, st);
 }
 
 hipError_t launch_w4_pack(const void* W, int64_t stride, int bf16, int32_t N, int32_t K, uint8_t* C, uint8_t* S, hipStream_t st) {
