@@ -22,6 +22,9 @@ Around that pass (``serve``): ``prefill_packed`` runs prompts of different
 lengths through the stack at full density, the paper's dense baseline, and can
 fill a 4-bit key/value cache; ``decode_step`` generates over that cache; ``score``
 and ``score_prompts`` give log probabilities of tokens under the LM head.
+``extend`` takes any number of new tokens of each sequence over a cache in pages:
+prompts in pieces, drafts, single tokens, or all of them in one batch, with a sliding
+window if asked.  With ``weight_bits=4`` the projections are held in 4 bits.
 """
 import torch
 import torch.nn.functional as F
@@ -37,10 +40,13 @@ class PrefillModel:
     ``synth.model_weights`` (numpy arrays or tensors; linear weights
     [out, in]); they are copied to the device in ``dtype``.  The LM head is
     ``weights["lm_head"]`` [vocab, hidden], or the embedding where the weights tie
-    the two.
+    the two.  weight_bits 4: the layers' projections and the LM head are quantised to 4
+    bits (``serve.w4_pack``); the embedding, norms and biases stay as they are.
     """
 
-    def __init__(self, cfg, weights, device="cuda", dtype=torch.bfloat16):
+    def __init__(self, cfg, weights, device="cuda", dtype=torch.bfloat16, weight_bits=16):
+        if weight_bits not in (4, 16):
+            raise ValueError("weight_bits must be 4 or 16")
         self.cfg = cfg
         self.dtype = dtype
         self.device = torch.device(device)
@@ -48,16 +54,17 @@ class PrefillModel:
         def t(a):
             return torch.as_tensor(a).to(device=self.device, dtype=dtype).contiguous()
 
+        held = (lambda w: w) if weight_bits == 16 else W4Weight
         self.embed = t(weights["embed"])
-        self.lm_head = t(weights["lm_head"]) if "lm_head" in weights else self.embed
+        self.lm_head = held(t(weights["lm_head"]) if "lm_head" in weights else self.embed)
         self.layers = []
         for L in weights["layers"]:
             layer = {
-                "wqkv": torch.cat([t(L["q"]), t(L["k"]), t(L["v"])], 0).contiguous(),   # [(Hq + 2 Hkv) D, hidden]
+                "wqkv": held(torch.cat([t(L["q"]), t(L["k"]), t(L["v"])], 0).contiguous()),   # [(Hq + 2 Hkv) D, hidden]
                 "bqkv": torch.cat([t(L["bq"]), t(L["bk"]), t(L["bv"])]) if cfg.qkv_bias else None,
-                "wo": t(L["o"]),                                                        # [hidden, Hq D]
-                "wgu": torch.cat([t(L["gate"]), t(L["up"])], 0).contiguous(),          # [2 I, hidden]
-                "wd": t(L["down"]),                                                     # [hidden, I]
+                "wo": held(t(L["o"])),                                                  # [hidden, Hq D]
+                "wgu": held(torch.cat([t(L["gate"]), t(L["up"])], 0).contiguous()),    # [2 I, hidden]
+                "wd": held(t(L["down"])),                                               # [hidden, I]
                 "ln1": t(L["ln1"]),
                 "ln2": t(L["ln2"]),
             }
@@ -76,7 +83,7 @@ class PrefillModel:
     def attention(self, h, layer, l, mask, rope_desc, algo, timers=None):
         cfg = self.cfg
         N, D, Hq, Hkv = h.shape[0], cfg.head_dim, cfg.heads, cfg.kv_heads
-        qkv = F.linear(h, layer["wqkv"], layer["bqkv"])
+        qkv = linear(h, layer["wqkv"], layer["bqkv"])
         v = qkv[:, (Hq + Hkv) * D:].view(N, Hkv, D).transpose(0, 1).contiguous()
         if timers:
             timers.mark("proj")
@@ -104,13 +111,16 @@ class PrefillModel:
         if timers:
             timers.mark("attention")
         a = out.transpose(0, 1).reshape(N, Hq * D)
-        return F.linear(a, layer["wo"])
+        return linear(a, layer["wo"])
 
     def mlp(self, h, layer):
-        gu = F.linear(h, layer["wgu"])
         m = torch.empty(h.shape[0], self.cfg.inter, dtype=self.dtype, device=self.device)
-        ris.swiglu(gu, m)
-        return F.linear(m, layer["wd"])
+        wgu = layer["wgu"]
+        if isinstance(wgu, W4Weight) and wgu.direct(h) and self.cfg.inter % 16 == 0:
+            serve.w4_linear(h, *wgu.tiles, m, gated=True)
+        else:
+            ris.swiglu(linear(h, wgu), m)
+        return linear(m, layer["wd"])
 
     def prefill(self, ids, mask, rope_desc=None, algo=ris.ATTN_AUTO, timers=None):
         """Final hidden states [N, hidden] for token ids (a device int64 tensor).
@@ -145,7 +155,7 @@ class PrefillModel:
         """Rotated Q [Hq, T, D] and K [Hkv, T, D], and V as a view of the projection."""
         cfg = self.cfg
         T, D, Hq, Hkv = h.shape[0], cfg.head_dim, cfg.heads, cfg.kv_heads
-        qkv = F.linear(h, layer["wqkv"], layer["bqkv"]).view(T, Hq + 2 * Hkv, D).transpose(0, 1)
+        qkv = linear(h, layer["wqkv"], layer["bqkv"]).view(T, Hq + 2 * Hkv, D).transpose(0, 1)
         qk = qkv[:Hq + Hkv]
         if rope_desc is not None:
             qk = serve.rope_packed(qk, torch.empty(Hq + Hkv, T, D, dtype=qkv.dtype, device=qkv.device), cu_seqlens,
@@ -159,7 +169,7 @@ class PrefillModel:
         h = torch.empty_like(res)
         ris.rmsnorm(res, self.layers[0]["ln1"], h, cfg.eps)
         for l, layer in enumerate(self.layers):
-            a = F.linear(attention(l, layer, h), layer["wo"])
+            a = linear(attention(l, layer, h), layer["wo"])
             ris.rmsnorm(a, layer["ln2"], h, cfg.eps, residual=res)
             m = self.mlp(h, layer)
             nxt = self.layers[l + 1]["ln1"] if l + 1 < len(self.layers) else self.norm
@@ -226,6 +236,40 @@ class PrefillModel:
 
         return self._stack(ids, attention)
 
+    def paged_cache(self, batch, max_len, pages=None, page=64):
+        """A cache in pages of ``page`` tokens for ``batch`` sequences of up to ``max_len``
+        tokens that share ``pages`` pages (None: as many as all of them can need)."""
+        return PagedCache(self, batch, max_len, pages, page)
+
+    def extend(self, ids, cu_seqlens, start, cache, rope_desc=None, window=None, sink=0):
+        """Final hidden states [T, hidden] of new tokens ids [T] packed by cu_seqlens
+        [batch + 1], the first one of sequence b at position start[b] (device int64):
+        their keys and values join the ``paged_cache``, whose table has to name their pages
+        (``cache.reserve``), and each token attends to its sequence up to itself, or to
+        its last ``window`` tokens and the ``sink`` first ones.  Rows of tokens outside
+        every sequence hold nothing of use.  bf16 models only.
+        """
+        cfg = self.cfg
+        T, D, Hq, Hkv = ids.shape[0], cfg.head_dim, cfg.heads, cfg.kv_heads
+        if cu_seqlens.numel() != cache.batch + 1 or start.numel() != cache.batch:
+            raise ValueError(f"cu_seqlens and start must be those of the cache's {cache.batch} sequences")
+
+        def attention(l, layer, h):
+            qkv = linear(h, layer["wqkv"], layer["bqkv"]).view(T, Hq + 2 * Hkv, D).transpose(0, 1)
+            q, k, v = qkv[:Hq], qkv[Hq:Hq + Hkv], qkv[Hq + Hkv:]
+            a = torch.empty(T, Hq * D, dtype=h.dtype, device=h.device)
+            out = a.view(T, Hq, D).transpose(0, 1)
+            Kp, Vp = cache.layers[l]
+            desc = serve.page_attn_desc(q, Kp, cache.table, cu_seqlens, out, window=window, sink=sink)
+            # refuses what the step cannot do before the cache changes
+            workspace = torch.empty(serve.page_attn_workspace_bytes(desc), dtype=torch.uint8, device=h.device)
+            turned = dict(q=q, q_out=q) if rope_desc is not None else {}
+            serve.page_store(k, v, cu_seqlens, cache.table, Kp, Vp, start=start, rope=rope_desc, **turned)
+            serve.page_attn(q, Kp, Vp, cache.table, cu_seqlens, out, workspace, desc, start=start)
+            return a
+
+        return self._stack(ids, attention)
+
     def score(self, h, targets=None, top_k=0, rows=2048):
         """Log probabilities under the LM head at hidden states h [n, hidden]: of
         the tokens ``targets`` [n, m] (negative: padding, 0), with the entropy and
@@ -239,7 +283,7 @@ class PrefillModel:
         if targets is not None:
             targets = targets.contiguous()
         for r in range(0, n, rows):
-            logits = F.linear(h[r:r + rows], self.lm_head)
+            logits = linear(h[r:r + rows], self.lm_head)
             desc = serve.logprob_desc(logits, m, top_k)
             ws = torch.empty(serve.logprobs_workspace_bytes(desc), dtype=torch.uint8, device=h.device)
             serve.logprobs(logits, targets[r:r + rows] if m else None, *(out[x][r:r + rows] for x in (
@@ -257,6 +301,84 @@ class PrefillModel:
         none = ends[1:] | (at <= cu_seqlens[0]) | (at > cu_seqlens[-1])
         targets = torch.where(none, -1, ids.roll(-1))
         return self.score(self.prefill_packed(ids, cu_seqlens, rope_desc), targets[:, None], top_k)
+
+
+def linear(x, w, bias=None):
+    """x W^T + bias for rows x and a weight [out, in], held in 16 or 32 bits or as a ``W4Weight``."""
+    return w(x, bias) if isinstance(w, W4Weight) else F.linear(x, w, bias)
+
+
+class W4Weight:
+    """A weight matrix held in 4 bits (codes and scales of ``serve.w4_weight``)."""
+
+    # Rows up to which the product reads the 4-bit weights itself.  For more they are written out for a library
+    # product (1,024 rows in bf16: 17,920 outputs of 1,536 inputs 70 us by itself, 26 + 70 written out, 151,936 of
+    # 1,536 553 and 194 + 445, 1,536 of 8,960 50 and 19 + 46; from there on its time doubles with the rows).
+    MOST_ROWS = 1024
+
+    def __init__(self, w):
+        self.shape, self.dtype = w.shape, w.dtype
+        self.tiles = serve.w4_weight(*w.shape, device=w.device)
+        serve.w4_pack(w, *self.tiles)
+
+    def direct(self, x):
+        return x.shape[0] <= self.MOST_ROWS
+
+    def values(self):
+        """The matrix of the values that it stands for."""
+        return serve.w4_load(*self.tiles, torch.empty(self.shape, dtype=self.dtype, device=self.tiles[0].device))
+
+    def __call__(self, x, bias=None):
+        if not self.direct(x):
+            return F.linear(x, self.values(), bias)
+        out = torch.empty(x.shape[0], self.shape[0], dtype=x.dtype, device=x.device)
+        return serve.w4_linear(x, *self.tiles, out, bias=bias)
+
+
+class PagedCache:
+    """The layers' pages of a batch of sequences and the block table that names them
+    (``PrefillModel.paged_cache``).  Which pages are free is kept on the host."""
+
+    def __init__(self, model, batch, max_len, pages=None, page=64):
+        cfg = model.cfg
+        self.batch, self.page = batch, page
+        self.max_pages = -(-max_len // page)
+        pages = batch * self.max_pages if pages is None else pages
+        self.layers = [serve.page_cache(pages, cfg.kv_heads, page, cfg.head_dim, model.device) for _ in model.layers]
+        self.table = torch.full((batch, self.max_pages), -1, dtype=torch.int32, device=model.device)
+        self.free = list(range(pages - 1, -1, -1))
+        self.held = [{} for _ in range(batch)]          # of a sequence: entry of the table -> page
+
+    def reserve(self, lens, first=None):
+        """Pages for the positions below lens[b] of every sequence b (host integers; those
+        that it has stay), but for those before first[b] alone, which a window has left.
+        Raises, taking none, where there are not enough."""
+        first = [0] * self.batch if first is None else first
+        if len(lens) != self.batch or any(not 0 <= n <= self.max_pages * self.page for n in lens):
+            raise ValueError(f"lens must hold {self.batch} lengths of at most {self.max_pages * self.page}")
+        if len(first) != self.batch or any(f < 0 for f in first):
+            raise ValueError(f"first must hold {self.batch} positions")
+        need = [[i for i in range(f // self.page, -(-n // self.page)) if i not in held]
+                for n, f, held in zip(lens, first, self.held)]
+        if sum(map(len, need)) > len(self.free):
+            raise RuntimeError(f"{sum(map(len, need))} pages are needed and {len(self.free)} free")
+        for b, entries in enumerate(need):
+            for i in entries:
+                self.held[b][i] = self.free.pop()
+            self._write(b, entries, [self.held[b][i] for i in entries])
+
+    def release(self, b, first=0, end=None):
+        """Give back the pages of sequence b that hold positions [first, end) alone (end
+        None: to the last one): all of them, or those that a window has left."""
+        last = self.max_pages if end is None else end // self.page
+        entries = [i for i in self.held[b] if -(-first // self.page) <= i < last]
+        self.free += [self.held[b].pop(i) for i in entries]
+        self._write(b, entries, [-1] * len(entries))
+
+    def _write(self, b, entries, pages):
+        if entries:
+            at, to = (torch.tensor(v, device=self.table.device) for v in (entries, pages))
+            self.table[b, at] = to.to(torch.int32)
 
 
 class KV4Cache:

@@ -366,21 +366,24 @@ def _page_map(Kp, table):
     """Map of pages [pages, Hkv, page, D], whose pages may lie apart, under a block table
     [batch, max_pages] int32, whose rows may."""
     pages, Hkv, page, D = Kp.shape
+    stride, *within = Kp.stride()
+    if within != [page * D, D, 1]:
+        raise ValueError("pages must be [Hkv, page, D] contiguous")
     if table.dtype != torch.int32:
         raise TypeError("the block table must be int32")
-    if table.dim() != 2 or table.stride(1) != 1 and table.shape[1] > 1:
+    rows, row = table.shape, table.stride()
+    if len(rows) != 2 or row[1] != 1 and rows[1] > 1:
         raise ValueError("the block table must be [batch, max_pages] with unit stride along a row")
-    if Kp.stride()[1:] != (page * D, D, 1):
-        raise ValueError("pages must be [Hkv, page, D] contiguous")
-    stride = Hkv * page * D if pages == 1 else Kp.stride(0)
-    return PageMap(page, table.shape[1], pages, stride, table.shape[1] if table.shape[0] == 1 else table.stride(0))
+    return PageMap(page, rows[1], pages, Hkv * page * D if pages == 1 else stride, rows[1] if rows[0] == 1 else row[0])
 
 
 def _need_pages(Kp, Vp):
     if Kp.dtype != torch.bfloat16 or Vp.dtype != torch.bfloat16:
         raise TypeError("pages must be bfloat16")
-    if Kp.dim() != 4 or Vp.shape != Kp.shape or Vp.stride() != Kp.stride():
+    shape = Kp.shape
+    if len(shape) != 4 or Vp.shape != shape or Vp.stride() != Kp.stride():
         raise ValueError("Kp and Vp must be [pages, Hkv, page, D], of one shape and strides")
+    return shape
 
 
 def page_store(K, V, cu_seqlens, table, Kp, Vp, start=None, q=None, q_out=None, rope=None, stream=None):
@@ -389,29 +392,32 @@ def page_store(K, V, cu_seqlens, table, Kp, Vp, start=None, q=None, q_out=None, 
     rope: a ``ris.rope_desc`` that K, and q [Hq, T, D] into q_out, are rotated by (None: K and q
     are copied)."""
     index = _one_gpu(Kp, K, V, cu_seqlens, table, Vp, start, q, q_out)
-    _need_pages(Kp, Vp)
-    if K.dtype != V.dtype:
+    pages = _need_pages(Kp, Vp)
+    dtype, shape = K.dtype, K.shape
+    if V.dtype != dtype:
         raise TypeError("K and V must share a dtype")
-    Hkv, T, D = shape = tuple(K.shape)
-    if Kp.shape[1] != Hkv or Kp.shape[3] != D:
+    k_at, k_head, k_token = _rows(K, shape)
+    v_at, v_head, v_token = _rows(V, shape)
+    Hkv, T, D = shape
+    if pages[1] != Hkv or pages[3] != D:
         raise ValueError("Kp and Vp must be [pages, Hkv, page, D] with the rows' Hkv and D")
     batch = _bounds(cu_seqlens, start)
+    where = _page_map(Kp, table)
     if table.shape[0] != batch:
         raise ValueError("the block table must hold one row a sequence")
-    k_at, *k_strides = _rows(K, shape)
-    v_at, *v_strides = _rows(V, shape)
-    Hq, q_at, qo_at, q_strides = 0, 0, 0, [0] * 4
-    if (q is None) != (q_out is None):
-        raise ValueError("q and q_out go together")
-    if q is not None:
-        Hq = q.shape[0]
-        if q.dtype != K.dtype or q_out.dtype != K.dtype:
+    Hq = q_at = q_head = q_token = o_at = o_head = o_token = 0
+    if q is not None and q_out is not None:
+        if q.dtype != dtype or q_out.dtype != dtype:
             raise TypeError("q and q_out must have the dtype of K and V")
-        q_at, *a = _rows(q, (Hq, T, D))
-        qo_at, *b = _rows(q_out, (Hq, T, D))
-        q_strides = a + b
-    desc = PageStoreDesc(_code(K), Hq, Hkv, D, batch, T, _page_map(Kp, table), *q_strides, *k_strides, *v_strides)
-    _call(index, stream, "ris_page_store", q_at, qo_at, k_at, v_at, cu_seqlens.data_ptr(), _at(start), table.data_ptr(),
+        Hq = q.shape[0]
+        of = (Hq, T, D)
+        q_at, q_head, q_token = _rows(q, of)
+        o_at, o_head, o_token = _rows(q_out, of)
+    elif q is not q_out:
+        raise ValueError("q and q_out go together")
+    desc = PageStoreDesc(_code(K), Hq, Hkv, D, batch, T, where, q_head, q_token, o_head, o_token, k_head, k_token, v_head,
+                         v_token)
+    _call(index, stream, "ris_page_store", q_at, o_at, k_at, v_at, cu_seqlens.data_ptr(), _at(start), table.data_ptr(),
           Kp.data_ptr(), Vp.data_ptr(), desc, rope)
 
 
@@ -436,19 +442,20 @@ def page_attn(Q, Kp, Vp, table, cu_seqlens, out, workspace, desc, start=None, st
     them already, token i of sequence b at position start[b] + i (start None: i).
     workspace: at least page_attn_workspace_bytes(desc) bytes, None where that is 0."""
     index = _one_gpu(out, Q, Kp, Vp, table, cu_seqlens, workspace, start)
-    _need_pages(Kp, Vp)
+    shape = _need_pages(Kp, Vp)
     _need_dense(workspace)
     if _code(Q) != desc.dtype_in or _code(out) != desc.dtype_out:
         raise TypeError("Q and out dtypes must match the descriptor")
-    m, q = desc.map, (desc.Hq, desc.T, desc.D)
-    if (Kp.shape != (m.pages, desc.Hkv, m.page, desc.D) or m.pages > 1 and Kp.stride(0) != m.page_stride
-            or Kp.stride()[1:] != (m.page * desc.D, desc.D, 1)):
+    m, q, batch, D = desc.map, (desc.Hq, desc.T, desc.D), desc.batch, desc.D
+    pages, page, stride = m.pages, m.page, Kp.stride()
+    if shape != (pages, desc.Hkv, page, D) or stride != (m.page_stride, page * D, D, 1) and (pages > 1 or stride[1:] != (page * D, D, 1)):
         raise ValueError("Kp and Vp must be [pages, Hkv, page, D] as in the descriptor")
-    if (table.dtype != torch.int32 or table.shape != (desc.batch, m.max_pages) or table.stride(1) != 1 and m.max_pages > 1
-            or table.stride(0) != m.table_stride and desc.batch > 1):
+    most, row = m.max_pages, table.stride()
+    if table.dtype != torch.int32 or table.shape != (batch, most) or row != (m.table_stride, 1) and (
+            row[1] != 1 and most > 1 or row[0] != m.table_stride and batch > 1):
         raise ValueError("the block table must be int32 [batch, max_pages] as in the descriptor")
     q_at, o_at = _placed(Q, q, (desc.q_head, desc.q_token, 1)), _placed(out, q, (desc.o_head, desc.o_token, 1))
-    if _bounds(cu_seqlens, start) != desc.batch:
+    if _bounds(cu_seqlens, start) != batch:
         raise ValueError("cu_seqlens must hold the descriptor's batch + 1 offsets")
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _call(index, stream, "ris_page_attn", q_at, Kp.data_ptr(), Vp.data_ptr(), table.data_ptr(), cu_seqlens.data_ptr(),
