@@ -300,19 +300,13 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void k_page_attn(Page
                 for (int i = 0; i < 16; ++i) mx = fmaxf(mx, st[b][i]);
             mx = pair_max32(mx);
             if (__any(mx > ref.m + p.slack)) {
-                const float al = safe ? ref.template raise<true>(mx, p.c) : ref.template raise<false>(mx, p.c);
+                float al = safe ? ref.template raise<true>(mx, p.c) : ref.template raise<false>(mx, p.c);
                 l *= al;
-                if (safe) {
+                if (safe) al = kept_infinite(al);
 #pragma unroll
-                    for (int d = 0; d < DB; ++d)
+                for (int d = 0; d < DB; ++d)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) o[d][i] = scaled<true>(o[d][i], al);
-                } else {
-#pragma unroll
-                    for (int d = 0; d < DB; ++d)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) o[d][i] *= al;
-                }
+                    for (int i = 0; i < 16; ++i) o[d][i] *= al;
             }
             // Exponents are s c - mc; of rows apart, (s - m) c - 0.
             float mc = ref.mc;
@@ -324,30 +318,43 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void k_page_attn(Page
 #pragma unroll
                     for (int i = 0; i < 16; ++i) st[b][i] -= m;
             }
-            u32x4_t pf[4];
+            // O^T += V^T P^T over 16 keys at a time, u: slot e of lane half lh holds key 16 u + 4 lh + e (e < 4) or 16 u +
+            // 8 + 4 lh + e - 4.  Values and weights of the next 16 keys are made beside a product.
+            u32x4_t pf[2], vf[2][DB];
+            const auto weigh = [&](int u) __attribute__((always_inline)) {
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; i += 2) {
-                    const float x = __builtin_amdgcn_exp2f(fmaf(st[b][i], p.c, -mc));
-                    const float y = __builtin_amdgcn_exp2f(fmaf(st[b][i + 1], p.c, -mc));
+                for (int i = 0; i < 8; i += 2) {
+                    const float x = __builtin_amdgcn_exp2f(fmaf(st[u / 2][8 * (u % 2) + i], p.c, -mc));
+                    const float y = __builtin_amdgcn_exp2f(fmaf(st[u / 2][8 * (u % 2) + i + 1], p.c, -mc));
                     l += x + y;
-                    pf[2 * b + i / 8][i % 8 / 2] = pack_bf16x2(x, y);
+                    pf[u % 2][i / 2] = pack_bf16x2(x, y);
                 }
-            // O^T += V^T P^T over 16 keys at a time: slot e of lane half lh holds
-            // key 16 u + 4 lh + e (e < 4) or 16 u + 8 + 4 lh + e - 4.
+            };
             uint32_t at = v_at;
             asm volatile("" : "+v"(at));
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
+            const auto read = [&](int u) __attribute__((always_inline)) {
 #pragma unroll
                 for (int d = 0; d < DB; ++d) {
                     const char* x = reinterpret_cast<const char*>(vl) + 32 * D * u;
                     const uint2 a = lds_read_tr16(reinterpret_cast<const uint16_t*>(x + (at ^ (64 * d))));
                     const uint2 e = lds_read_tr16(reinterpret_cast<const uint16_t*>(x + 16 * D + (at ^ (64 * d) ^ 32)));
-                    const u32x4_t v = {a.x, a.y, e.x, e.y};
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v), as_bf16x8(pf[u]), o[d], 0, 0, 0);
+                    vf[u % 2][d] = u32x4_t{a.x, a.y, e.x, e.y};
                 }
+            };
+            read(0);
+            weigh(0);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                if (u < 3) {
+                    read(u + 1);
+                    weigh(u + 1);
+                }
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vf[u % 2][d]), as_bf16x8(pf[u % 2]), o[d], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         };
         // A weight of 0, masked or too small for float32, times an infinity or NaN of V would be NaN: in the safe
         // pass such elements are added, whatever their weight, where they are attended to, and taken out

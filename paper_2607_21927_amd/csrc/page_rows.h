@@ -53,6 +53,10 @@ __device__ __forceinline__ int64_t tile_pos(const PageAttnParams& p, int64_t fir
     return first + (int64_t)t.tile * p.tokens;
 }
 
+// A factor that may have fallen to 0, for sums that an infinity has to stay in: the least float32
+// number in its place, which takes any finite sum (below 2^128) below 2^-21.
+__device__ __forceinline__ float kept_infinite(float a) { return fmaxf(a, __uint_as_float(1u)); }
+
 // Four neighbouring elements of out.
 __device__ __forceinline__ void store4(const PageAttnParams& p, int64_t at, float a, float b, float c, float d) {
     if (p.out_bf16)

@@ -188,13 +188,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_page_step(PageAttnParams p) 
             if (__any(mx > m + p.slack)) {
                 const float was = m;
                 m = fmaxf(m, mx);
-                const float al = meet(p, was, m);
+                float al = meet(p, was, m);
                 l *= al;
+                if (safe) al = kept_infinite(al);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float a = __shfl(al, 4 * lg + i);
 #pragma unroll
-                    for (int db = 0; db < DB; ++db) o[db][i] = safe ? scaled<true>(o[db][i], a) : o[db][i] * a;
+                    for (int db = 0; db < DB; ++db) o[db][i] *= a;
                 }
             }
             float w[2][4];

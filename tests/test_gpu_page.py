@@ -385,3 +385,53 @@ def test_another_stream():
         got = attend(serve, q, Kp, Vp, t, cu, s0)
     torch.cuda.current_stream().wait_stream(s)
     assert torch.equal(got, want)
+
+
+def on_the_gpu(q, Kp, Vp, table, cu, start, window, sink):
+    """The oracle's formula with torch in float64, for batches that are too large for it."""
+    Hq, T, D = q.shape
+    pages, Hkv, page, _ = Kp.shape
+    out = torch.zeros(Hq, T, D, dtype=torch.float64, device="cuda")
+    for b, (a, z) in enumerate(zip(cu.tolist()[:-1], cu.tolist()[1:])):
+        at = torch.tensor(o_srv.page_places(table[b], page, pages), device="cuda")
+        p = torch.arange(start[b], start[b] + z - a, device="cuda")[:, None]
+        j = torch.arange(len(at), device="cuda")
+        keep = (j <= p) & ((j > p - window) | (j < sink)) & (at[:, 0] >= 0) & (p >= 0) & (p < len(at))
+        at = at.clamp(min=0)
+        for h in range(Hq):
+            k, v = (x[at[:, 0], h // (Hq // Hkv), at[:, 1]].double().nan_to_num(0, 0, 0) for x in (Kp, Vp))
+            w = torch.where(keep, q[h, a:z].double() @ k.t().contiguous() * D**-0.5, -math.inf).softmax(1).nan_to_num(0)
+            out[h, a:z] = w @ v
+    return out
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,lens", [(16, 16, 128, [5000, 3300]), (16, 16, 64, [8300]), (24, 8, 128, [2700, 1, 2700, 0, 460]),
+                                           (16, 16, 64, [9000, 3100])])
+def test_many_row_tiles(Hq, Hkv, D, lens):
+    """So many row tiles that they are not shared, with little and much left for the last round;
+    positions without a place and infinities among what is."""
+    serve = need_serve()
+    start = [600] + [40] * (len(lens) - 1)
+    q, Kp, Vp, table, cu, start = held(lens, start, 64, Hq, Hkv, D, seed=3)
+    if len(lens) > 1:
+        start[-1] = -10                                              # the first ten tokens have no place
+    for window, sink in ((300, 5), (EVERY, 0)):
+        want = on_the_gpu(q, Kp, Vp, table, cu, start, window, sink)
+        got = attend(serve, q, Kp, Vp, ids(table, torch.int32), cu, ids(start), window, sink)
+        bar = attn_bar(q, Kp, Vp, max(start) + max(lens), D**-0.5, want, BF16, F32)
+        worst = float(((got.double() - want).abs() / bar).max())
+        say(f"{lens} {Hq}/{Hkv} D={D} window {window}: off by {worst:.3f} of the bar")
+        assert worst <= 1.0
+        assert len(lens) == 1 or not got[:, -lens[-1]:][:, :10].any()
+    # an infinite value that the first and last tokens of a sequence attend to, and one that few do
+    w = o_srv.page_places(table[0], 64, Kp.shape[0])
+    Vp[w[2, 0], :, w[2, 1], 7], Vp[w[-70, 0], :, w[-70, 1], 9] = math.inf, math.nan
+    got = attend(serve, q, Kp, Vp, ids(table, torch.int32), cu, ids(start), 300, 5)
+    n, first = lens[0], start[0]
+    assert torch.isinf(got[:, :n, 7]).all()
+    hit = torch.zeros(n, dtype=torch.bool, device="cuda")
+    j = len(w) - 70
+    p = torch.arange(first, first + n, device="cuda")
+    hit[(p >= j) & (p < j + 300)] = True                       # w[j] is a page of the sequence's: it is its last
+    assert torch.equal(got[:, :n, 9].isnan(), hit.expand(Hq, n))
+    assert got[:, n:].isfinite().all() and got[:, :n, 10:].isfinite().all()
