@@ -93,6 +93,10 @@ __device__ __forceinline__ Part<F32> parts_of(const Raw<F32>& r) {
     return p;
 }
 
+// Where row r keeps its 16-byte places in LDS, place c at c ^ turn(r): 16 rows at one place and four rows at
+// four places spread over all banks.
+__device__ __forceinline__ int turn(int r) { return (r & 3) << 2 | (r >> 2 & 3); }
+
 __device__ __forceinline__ float silu(float g) { return g / (1.f + __expf(-g)); }
 
 // Where lane `lane` finds its part of a tile, and of chunk kc's scales.
@@ -176,7 +180,7 @@ __global__ __launch_bounds__(64 * WV) void k_w4_narrow(W4Params p) {
     for (int n = 0; n < NS; ++n)
 #pragma unroll
         for (int m = 0; m < MT; ++m) acc[n][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    // Piece i of a lane: eight inputs of row lane / 16 + 4 i of a chunk, 16-byte place c of the row at c ^ row % 16.
+    // Piece i of a lane: eight inputs of row lane / 16 + 4 i of a chunk, 16-byte place c of the row at c ^ turn(row).
     // Rows that are not there are not loaded: what is in their place reaches outputs that are not there alone.
     uint16_t* const stage = reinterpret_cast<uint16_t*>(mem) + wave * kParts * kPlane;
     const int have = p.rows - m0, pk = 8 * li;
@@ -213,7 +217,7 @@ __global__ __launch_bounds__(64 * WV) void k_w4_narrow(W4Params p) {
                     const int r = lg + 4 * i;
 #pragma unroll
                     for (int e = 0; e < kParts; ++e)
-                        *reinterpret_cast<u32x4_t*>(stage + e * kPlane + r * kChunk + 8 * (li ^ (r & 15))) = b.b[e];
+                        *reinterpret_cast<u32x4_t*>(stage + e * kPlane + r * kChunk + 8 * (li ^ turn(r))) = b.b[e];
                 }
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
@@ -222,7 +226,7 @@ __global__ __launch_bounds__(64 * WV) void k_w4_narrow(W4Params p) {
                 for (int m = 0; m < MT; ++m)
 #pragma unroll
                     for (int e = 0; e < kParts; ++e)
-                        b[m].b[e] = *reinterpret_cast<const u32x4_t*>(stage + e * kPlane + (16 * m + li) * kChunk + 8 * ((4 * lg + s) ^ li));
+                        b[m].b[e] = *reinterpret_cast<const u32x4_t*>(stage + e * kPlane + (16 * m + li) * kChunk + 8 * ((4 * lg + s) ^ turn(li)));
 #pragma unroll
                 for (int n = 0; n < NS; ++n) {
                     const u32x4_t w = decode8(code[u][n][s], scale_of(byte[u][n]));
@@ -277,7 +281,7 @@ __global__ __launch_bounds__(256 * KW) void k_w4_wide(W4Params p) {
     for (int n = 0; n < NS; ++n)
 #pragma unroll
         for (int m = 0; m < MT; ++m) acc[n][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    // Piece i of a thread: eight inputs of row tid / 16 + 16 i of a chunk, 16-byte place c of the row at c ^ row % 16.
+    // Piece i of a thread: eight inputs of row tid / 16 + 16 i of a chunk, 16-byte place c of the row at c ^ turn(row).
     uint16_t* const stage = reinterpret_cast<uint16_t*>(mem) + way * 2 * kParts * kPlane;
     const int pr = tid >> 4, pk = 8 * (tid & 15);
     int64_t row[MT];
@@ -286,7 +290,7 @@ __global__ __launch_bounds__(256 * KW) void k_w4_wide(W4Params p) {
         const int r = m0 + 16 * m + pr;
         row[m] = (int64_t)(r < p.rows ? r : p.rows - 1) * p.x_stride;
     }
-    const int put = pr * kChunk + 8 * ((tid & 15) ^ pr);
+    const int put = pr * kChunk + 8 * ((tid & 15) ^ turn(pr));
     Raw<F32> x[MT];
     u32x4_t code[NS], next[NS];
     uint32_t byte[NS], next_byte[NS];
@@ -331,7 +335,7 @@ __global__ __launch_bounds__(256 * KW) void k_w4_wide(W4Params p) {
             for (int m = 0; m < MT; ++m)
 #pragma unroll
                 for (int e = 0; e < kParts; ++e)
-                    b[m].b[e] = *reinterpret_cast<const u32x4_t*>(to + e * kPlane + (16 * m + li) * kChunk + 8 * ((4 * lg + s) ^ li));
+                    b[m].b[e] = *reinterpret_cast<const u32x4_t*>(to + e * kPlane + (16 * m + li) * kChunk + 8 * ((4 * lg + s) ^ turn(li)));
 #pragma unroll
             for (int n = 0; n < NS; ++n) {
                 const u32x4_t w = decode8(code[n][s], scale_of(byte[n]));
