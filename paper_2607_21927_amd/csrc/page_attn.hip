@@ -129,7 +129,10 @@ __device__ __forceinline__ Line make_plan(const PageAttnParams& p, Plan& plan) {
         if (plan.len[tid] > 0) mine = (uint32_t)(plan.len[tid] + p.tokens - 1) / (uint32_t)p.tokens;
     }
     const uint32_t at = block_scan(mine, plan.carry, line.tiles);
-    if (tid < p.batch) plan.tile0[tid] = at;
+    // offsets that do not ascend could make more row tiles than there is room for: those are left out
+    const uint32_t room = (uint32_t)(kMostTiles / p.Hkv);
+    line.tiles = line.tiles < room ? line.tiles : room;
+    if (tid < p.batch) plan.tile0[tid] = at < room ? at : room;
     if (tid == 0) plan.tile0[p.batch] = line.tiles;
     __syncthreads();
     // kEach neighbouring row tiles a thread; one that attends to nothing counts as one key tile

@@ -435,3 +435,22 @@ def test_many_row_tiles(Hq, Hkv, D, lens):
     hit[(p >= j) & (p < j + 300)] = True                       # w[j] is a page of the sequence's: it is its last
     assert torch.equal(got[:, :n, 9].isnan(), hit.expand(Hq, n))
     assert got[:, n:].isfinite().all() and got[:, :n, 10:].isfinite().all()
+
+
+@pytest.mark.parametrize("lens,Hq", [((400, 600), 12), ((3, 2), 4)])
+def test_offsets_that_do_not_ascend(lens, Hq):
+    """Sequences that overlap have no result, but every access stays in place: 1,500 row tiles where
+    the host counted on 100, no memory but out's own written."""
+    serve = need_serve()
+    lens, start = list(lens), [700, 30]
+    q, Kp, Vp, table, cu, start = held(lens, start, 64, Hq, 2, 128, seed=15)
+    T = sum(lens)
+    wide = np.concatenate([table, np.full((30, table.shape[1]), -1, np.int32), table[:1]])
+    bad = torch.tensor([0, lens[0], T] + [0, T] * 15 + [0], dtype=torch.int64, device="cuda")
+    starts = start + [0] * 31
+    room = torch.full((Hq, 3 * T, 128), 7.0, dtype=F32, device="cuda")
+    keep = Kp.clone()
+    attend(serve, q, Kp, Vp, ids(wide, torch.int32), bad, ids(starts), out=room[:, T:2 * T])
+    serve.page_store(q[:2], q[:2], bad, ids(np.full_like(wide, -1), torch.int32), Kp, Vp, start=ids(starts))
+    torch.cuda.synchronize()
+    assert (room[:, :T] == 7).all() and (room[:, 2 * T:] == 7).all() and torch.equal(Kp.nan_to_num(9), keep.nan_to_num(9))
