@@ -163,6 +163,44 @@ __global__ __launch_bounds__(kThreads) void k_rope_packed(const void* src, int64
     }
 }
 
+// A lane's pairs of a bf16 row as they lie.
+template <int P>
+struct PairBits {
+    uint32_t lo[(P + 1) / 2], hi[(P + 1) / 2];
+};
+template <int P>
+__device__ __forceinline__ PairBits<P> load_bits(const uint16_t* p, int half) {
+    PairBits<P> x;
+    if constexpr (P == 4) {
+        const uint2 a = *reinterpret_cast<const uint2*>(p), b = *reinterpret_cast<const uint2*>(p + half);
+        x.lo[0] = a.x; x.lo[1] = a.y; x.hi[0] = b.x; x.hi[1] = b.y;
+    } else {
+        x.lo[0] = p[0];
+        x.hi[0] = p[half];
+    }
+    return x;
+}
+template <int P>
+__device__ __forceinline__ void store_bits(uint16_t* p, int half, const PairBits<P>& x) {
+    if constexpr (P == 4) {
+        *reinterpret_cast<uint2*>(p) = make_uint2(x.lo[0], x.lo[1]);
+        *reinterpret_cast<uint2*>(p + half) = make_uint2(x.hi[0], x.hi[1]);
+    } else {
+        p[0] = (uint16_t)x.lo[0];
+        p[half] = (uint16_t)x.hi[0];
+    }
+}
+template <int P>
+__device__ __forceinline__ RopePairs<true, P> values_of(const PairBits<P>& x) {
+    RopePairs<true, P> v;
+#pragma unroll
+    for (int k = 0; k < P; ++k) {
+        v.lo[k] = bf16_to_f32((uint16_t)(x.lo[k / 2] >> (16 * (k & 1))));
+        v.hi[k] = bf16_to_f32((uint16_t)(x.hi[k / 2] >> (16 * (k & 1))));
+    }
+    return v;
+}
+
 // The new rows of a paged cache: as k_rope_packed, with K rotated into its page, Q into
 // rows of its own beside it and V copied, one pass over the projection's output.  A token
 // without a place in the cache keeps its Q alone.
@@ -190,33 +228,37 @@ __global__ __launch_bounds__(kThreads) void k_page_store(PageStoreParams p, Rope
             s[k] = (float)(sd * tab.mscale);
         }
     }
-    // heads of Q, then of K, then of V
-    const int turned = p.Hq + p.Hkv, heads = row < 0 ? p.Hq : turned + p.Hkv;
-    const auto load = [&](int h, RopePairs<true, P>& x) __attribute__((always_inline)) {
-        if (h < p.Hq) load_pairs<true, P>(p.Q, h * p.q_head + t * p.q_token + i, half, x);
-        else if (h < turned) load_pairs<true, P>(p.K, (h - p.Hq) * p.k_head + t * p.k_token + i, half, x);
-        else load_pairs<true, P>(p.V, (h - turned) * p.v_head + t * p.v_token + i, half, x);
+    // heads of Q, then of K, then of V, whose bits stay as they are
+    const int turned = p.rotate ? p.Hq + p.Hkv : 0, of_k = p.Hq + p.Hkv, heads = row < 0 ? p.Hq : of_k + p.Hkv;
+    const auto source = [&](int h) __attribute__((always_inline)) {
+        const void* x = h < p.Hq ? p.Q : (h < of_k ? p.K : p.V);
+        const int64_t at = h < p.Hq ? h * p.q_head + t * p.q_token
+                                    : (h < of_k ? (h - p.Hq) * p.k_head + t * p.k_token : (h - of_k) * p.v_head + t * p.v_token);
+        return static_cast<const uint16_t*>(x) + at + i;
+    };
+    const auto target = [&](int h) __attribute__((always_inline)) {
+        void* y = h < p.Hq ? p.Qout : (h < of_k ? p.Kp : p.Vp);
+        const int64_t g = h < of_k ? h - p.Hq : h - of_k;
+        return static_cast<uint16_t*>(y) + (h < p.Hq ? h * p.qo_head + t * p.qo_token : (row + (g << p.map.shift)) * p.D) + i;
     };
     int h = blockIdx.y;
     if (h >= heads) return;
-    RopePairs<true, P> x;
-    load(h, x);
+    PairBits<P> x = load_bits<P>(source(h), half);
     while (true) {
         const int nh = h + (int)gridDim.y;
-        RopePairs<true, P> nx = x, y = x;
-        if (nh < heads) load(nh, nx);
-        if (p.rotate && h < turned) {
+        PairBits<P> nx = x;
+        if (nh < heads) nx = load_bits<P>(source(nh), half);
+        if (h < turned) {
+            const RopePairs<true, P> v = values_of<P>(x);
+            RopePairs<true, P> y;
 #pragma unroll
             for (int k = 0; k < P; ++k) {
-                y.lo[k] = fmaf(x.lo[k], c[k], -(x.hi[k] * s[k]));
-                y.hi[k] = fmaf(x.lo[k], s[k], x.hi[k] * c[k]);
+                y.lo[k] = fmaf(v.lo[k], c[k], -(v.hi[k] * s[k]));
+                y.hi[k] = fmaf(v.lo[k], s[k], v.hi[k] * c[k]);
             }
-        }
-        if (h < p.Hq) {
-            store_pairs<true, P>(p.Qout, h * p.qo_head + t * p.qo_token + i, half, y);
+            store_pairs<true, P>(target(h), 0, half, y);
         } else {
-            const int g = h < turned ? h - p.Hq : h - turned;
-            store_pairs<true, P>(h < turned ? p.Kp : p.Vp, (row + ((int64_t)g << p.map.shift)) * p.D + i, half, y);
+            store_bits<P>(target(h), half, x);
         }
         if (nh >= heads) return;
         h = nh;

@@ -100,6 +100,24 @@ def test_store_keeps_infinities_and_nan():
         assert torch.equal(got[1, :, :10].view(torch.int16), x.view(torch.int16)) and not got[0].any()
 
 
+@pytest.mark.parametrize("n", [10, 2100])
+def test_store_copies_bits(n):
+    """What is not rotated keeps its bits: every bf16 pattern, signalling NaN and denormals among
+    them."""
+    serve = need_serve()
+    bits = torch.arange(n * 2 * 64, dtype=torch.int32, device="cuda").mul_(40503).to(torch.int16).view(BF16).view(2, n, 64)
+    k, q = bits.flip(1).contiguous(), bits.flip(0).contiguous()
+    page = 64
+    table = torch.arange(-(-n // page), dtype=torch.int32, device="cuda").flip(0)[None].contiguous()
+    Kp, Vp = serve.page_cache(table.shape[1], 2, page, 64)
+    q_out = torch.zeros_like(q)
+    serve.page_store(k, bits, bounds([n]), table, Kp, Vp, q=q, q_out=q_out)
+    for got, x in ((Kp, k), (Vp, bits)):
+        rows = got[table[0].long()].transpose(1, 2).flatten(0, 1)[:n].transpose(0, 1)
+        assert torch.equal(rows.contiguous().view(torch.int16), x.view(torch.int16))
+    assert torch.equal(q_out.view(torch.int16), q.view(torch.int16))
+
+
 def attend(serve, q, Kp, Vp, table, cu, start, window=None, sink=0, scale=0.0, out=None, dtype=F32):
     Hq, T, D = q.shape
     if out is None:
