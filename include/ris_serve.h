@@ -306,7 +306,7 @@ typedef struct {
     int32_t dtype;           /* ris_dtype of x, bias and out                    */
     int32_t gated;           /* 1: SwiGLU of the two halves of the outputs      */
     int64_t rows;            /* rows of x and out, 1..2^31 - 1                  */
-    int64_t N, K;            /* outputs and inputs of W, up to 2^28 and 2^24;   */
+    int64_t N, K;            /* outputs and inputs of W, up to 2^27 and 2^24;   */
                              /*   gated: N a multiple of 32                     */
     int64_t x_stride;        /* elements between rows of x, >= K; it and x      */
                              /*   multiples of 16 bytes                         */

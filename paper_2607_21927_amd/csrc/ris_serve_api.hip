@@ -209,7 +209,7 @@ int64_t page_attn_workspace(const ris::PageAttnParams& p) {
 int w4_sizes(int32_t dtype, int64_t N, int64_t K) {
     if (!known_dtype(dtype)) return RIS_E_DTYPE;
     if (N < 1 || K < 1) return RIS_E_ARG;
-    if (N > (1ll << 28) || K > (1ll << 24)) return RIS_E_UNSUPPORTED;
+    if (N > (1ll << 27) || K > (1ll << 24)) return RIS_E_UNSUPPORTED;
     return RIS_OK;
 }
 
@@ -438,7 +438,7 @@ int ris_w4_linear(const void* x, const uint8_t* C, const uint8_t* S, const void*
     p.rows = (int32_t)d.rows; p.N = (int32_t)d.N; p.K = (int32_t)d.K;
     p.f32 = d.dtype == RIS_F32; p.gated = d.gated;
     p.vector_out = cols % 4 == 0 && d.out_stride % 4 == 0 && aligned(out, (uintptr_t)(4 * e));
-    if (!fits_dispatch(ris::w4_blocks(p), 256)) return RIS_E_UNSUPPORTED;
+    if (ris::w4_items(p) > 0xFFFFFFFFll) return RIS_E_UNSUPPORTED;
     return hip_status(ris::launch_w4_linear(p, static_cast<hipStream_t>(stream)));
 }
 

@@ -465,8 +465,6 @@ hipError_t wide(const W4Params& p, hipStream_t st) {
 
 }  // namespace
 
-int64_t w4_blocks(const W4Params& p) { return grid_of(p, tiles_of(p.gated ? p.N / 2 : p.N), 16) * 4; }
-
 // The wide form from 512 tiles of outputs on, and for more than 128 rows (float32: 64), where the narrow one reads
 // the rows for every 16 outputs (us, bf16, narrow and wide: 2,048 outputs of 1,536 inputs, 16 rows 4.0, 6.0, 64
 // 6.5, 10.0, 256 14, 10.2; 1,536 of 8,960, 1 row 5.8, 22, 64 20.6, 40; 17,920 gated of 1,536, 1 row 8.4, 7.0, 32
@@ -474,9 +472,18 @@ int64_t w4_blocks(const W4Params& p) { return grid_of(p, tiles_of(p.gated ? p.N 
 // row of 1,536 inputs 4.6 with 8, 5.3 with 16).  Ways of the wide form: two, so that few sets keep more waves busy (17,920
 // gated, 32 rows 10.1 with one, 7.4 with two, 7.5 with four; 151,936, 64 rows 45.5, 45.3, 65), float32's rows of more than 16 one,
 // for room in LDS.
+static bool takes_wide(const W4Params& p) { return tiles_of(p.N) >= 512 || p.rows > (p.f32 ? 64 : 128); }
+
+int64_t w4_items(const W4Params& p) {
+    const int64_t sets = tiles_of(p.gated ? p.N / 2 : p.N);
+    if (!takes_wide(p)) return grid_of(p, sets, 16) * 1024;             // at most
+    const int rows = p.rows <= 16 ? 16 : (p.f32 || p.rows <= 32 ? 32 : 64), each = p.gated ? 4 : 8;
+    return grid_of(p, (sets + each - 1) / each, rows) * 512;
+}
+
 hipError_t launch_w4_linear(const W4Params& p, hipStream_t st) {
-    const int64_t tiles = tiles_of(p.N), chunks = chunks_of(p.K);
-    if (tiles >= 512 || p.rows > (p.f32 ? 64 : 128)) {
+    const int64_t chunks = chunks_of(p.K);
+    if (takes_wide(p)) {
         if (p.f32) return p.rows <= 16 ? wide<true, 1, 2, 2>(p, st) : wide<true, 2, 2, 1>(p, st);
         if (p.rows <= 16) return wide<false, 1, 2, 2>(p, st);
         return p.rows <= 32 ? wide<false, 2, 2, 2>(p, st) : wide<false, 4, 2, 2>(p, st);

@@ -201,3 +201,15 @@ def test_many_outputs():
     got = serve.w4_linear(x, C, S, torch.empty(2, N, dtype=BF16, device="cuda"))
     want = serve.w4_linear(x, c, s, torch.empty(2, 64, dtype=BF16, device="cuda"))
     assert torch.equal(got[:, -64:], want) and not got[:, :-64].any()
+
+
+def test_many_rows():
+    """Rows beyond what a form of few rows can launch."""
+    serve = need_serve()
+    C, S, W = weights(serve, 48, 64)
+    x = randn(300_000, 64)
+    out = serve.w4_linear(x, C, S, torch.empty(300_000, 48, dtype=BF16, device="cuda"))
+    few = serve.w4_linear(x[-64:], C, S, torch.empty(64, 48, dtype=BF16, device="cuda"))
+    want = x.double() @ W.t().cuda()
+    assert bool(((out.double() - want).abs() <= bar(x.double(), W.cuda(), None, want, BF16) + rounded(want, BF16)).all())
+    assert bool(((out[-64:].double() - few.double()).abs() <= 2 * rounded(want[-64:], BF16)).all())

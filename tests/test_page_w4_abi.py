@@ -110,7 +110,7 @@ def linear(serve, **kw):
     (dict(dtype=3), -3), (dict(gated=2), -1), (dict(gated=1), -2), (dict(rows=0), -1), (dict(rows=2**31), -1), (dict(N=0), -1),
     (dict(K=0), -1), (dict(N=2**28 + 1, out_stride=2**29), -5), (dict(K=2**24 + 1, x_stride=2**25), -5), (dict(x_stride=248), -1),
     (dict(x_stride=260), -1), (dict(dtype=0, x_stride=258), -1), (dict(out_stride=99), -1), (dict(out_stride=2**41), -1),
-    (dict(rows=2**31 - 1, N=2**20, out_stride=2**20), -5),
+    (dict(rows=2**31 - 1, N=2**20, out_stride=2**20), -5), (dict(N=2**27 + 16, out_stride=2**28), -5),
 ])
 def test_linear_refusals(serve, bad, code):
     assert serve.lib().ris_w4_linear(P, P, P, None, P, ctypes.byref(linear(serve, **bad)), None) == code
@@ -164,6 +164,11 @@ def test_bindings_refuse(serve):
     with pytest.raises(ValueError, match="contiguous"):
         serve._page_map(Kp.transpose(1, 2), table)
     assert serve._page_map(torch.zeros(3, 2, 2, 16, 64)[:, 0], table).page_stride == 2 * 2 * 16 * 64
+    # a dimension of one element may have any stride; windows and sinks beyond 32 bits are all of it
+    odd = torch.zeros(3, 1, 16, 64).as_strided((3, 1, 16, 64), (1024, 7, 64, 1))
+    assert serve._page_map(odd, table).page_stride == 1024
+    far = serve.page_attn_desc(q, Kp, table, cu, q, window=2**40, sink=2**40)
+    assert far.window == far.sink == 2**31 - 1
     for bad in ((Kp, Vp[:, :1]), (Kp, Vp[:2]), (Kp[0], Vp[0])):
         with pytest.raises(ValueError):
             serve._need_pages(*bad)
