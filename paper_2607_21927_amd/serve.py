@@ -367,7 +367,7 @@ def _page_map(Kp, table):
     [batch, max_pages] int32, whose rows may."""
     pages, Hkv, page, D = Kp.shape
     stride, *within = Kp.stride()
-    if within != [page * D, D, 1]:
+    if within != [page * D, D, 1] and not Kp[0].is_contiguous():
         raise ValueError("pages must be [Hkv, page, D] contiguous")
     if table.dtype != torch.int32:
         raise TypeError("the block table must be int32")
@@ -426,7 +426,7 @@ def page_attn_desc(Q, Kp, table, cu_seqlens, out, window=None, sink=0, scale=0.0
     table [batch, max_pages].  window None: every key up to a token."""
     Hq, T, D = Q.shape
     return PageAttnDesc(_code(Q), _code(out), Hq, Kp.shape[1], D, cu_seqlens.numel() - 1, T, _page_map(Kp, table),
-                        min(0x7FFFFFFF, table.shape[1] * Kp.shape[2] if window is None else window), sink, scale,
+                        min(0x7FFFFFFF, table.shape[1] * Kp.shape[2] if window is None else window), min(0x7FFFFFFF, sink), scale,
                         *_rows(Q, Q.shape)[1:], *_rows(out, Q.shape)[1:])
 
 
@@ -448,7 +448,8 @@ def page_attn(Q, Kp, Vp, table, cu_seqlens, out, workspace, desc, start=None, st
         raise TypeError("Q and out dtypes must match the descriptor")
     m, q, batch, D = desc.map, (desc.Hq, desc.T, desc.D), desc.batch, desc.D
     pages, page, stride = m.pages, m.page, Kp.stride()
-    if shape != (pages, desc.Hkv, page, D) or stride != (m.page_stride, page * D, D, 1) and (pages > 1 or stride[1:] != (page * D, D, 1)):
+    if shape != (pages, desc.Hkv, page, D) or stride != (m.page_stride, page * D, D, 1) and (
+            pages > 1 and stride[0] != m.page_stride or stride[1:] != (page * D, D, 1) and not Kp[0].is_contiguous()):
         raise ValueError("Kp and Vp must be [pages, Hkv, page, D] as in the descriptor")
     most, row = m.max_pages, table.stride()
     if table.dtype != torch.int32 or table.shape != (batch, most) or row != (m.table_stride, 1) and (
