@@ -232,7 +232,8 @@ typedef struct {
  * is copied to its place, K rotated to its position there, and Q rotated into Qout,
  * as ris_rope_packed rotates (the same bits); rope NULL: no rotation, linear and YaRN
  * need the factor.  A token without a place in the cache keeps its Q alone.  Places that
- * no token goes to stay as they were.  Qout may be Q itself with the same strides, and
+ * no token goes to stay as they were; one that several go to (sequences that share a page
+ * they write to) holds a mix of theirs.  Qout may be Q itself with the same strides, and
  * must not overlap the inputs otherwise.  Q and Qout may be NULL where Hq is 0.
  */
 int ris_page_store(const void* Q, void* Qout, const void* K, const void* V, const int64_t* cu_seqlens,

@@ -317,6 +317,8 @@ class W4Weight:
     MOST_ROWS = 1024
 
     def __init__(self, w):
+        if w.shape[1] * w.element_size() % 16:
+            raise ValueError("a weight in 4 bits needs rows of inputs that are multiples of 16 bytes")
         self.shape, self.dtype = w.shape, w.dtype
         self.tiles = serve.w4_weight(*w.shape, device=w.device)
         serve.w4_pack(w, *self.tiles)

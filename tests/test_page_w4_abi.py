@@ -191,3 +191,10 @@ def test_bindings_refuse(serve):
     with pytest.raises(ValueError, match="unit stride"):
         serve._matrix(x[:, ::2], 2, 150)
     assert serve._matrix(x[:1, :7], 1, 7) == 7 and serve._matrix(x[:, :7], 2, 7) == 300
+
+
+def test_model_refuses_weights_without_whole_pieces():
+    from paper_2607_21927_amd.model import W4Weight
+    for w in (torch.zeros(16, 36, dtype=torch.bfloat16), torch.zeros(16, 34)):
+        with pytest.raises(ValueError, match="multiples of 16 bytes"):
+            W4Weight(w)
