@@ -13,6 +13,14 @@
 // may attend to and whose page there is are a mask of 64 bits (`live`); the others are
 // never read: the first live key is loaded in their place.  Rows attend to bits of that
 // mask, so that what lies in unwritten places does not reach an output.
+// Bound by the matrix unit where it is fed: 4 D flops a (query head, key) pair at 0.84 to 0.86 PFLOP/s (2,048 tokens after
+// 30,000, 12/2 heads of 128: 456 us for 390 GFLOP; 16,384 of three sequences under a window of 4,096: 490 for 413), the unit
+// busy 42% and 38% of the time.  A wave's exponentials and its products follow each other, and of two waves a SIMD
+// one is often at a barrier for the next tile (in the first case 71% of the requests for K and V miss
+// L2: 2.4 GB of them a pass).  Weights and values of the next 16 keys are made beside a product.
+// Measured and not kept: eight waves of 256 rows with three tiles in LDS, half the reads (438 for 475 there, but 537 for
+// 502 under the window and 112 for 92 in a mixed batch); the next tile's scores beside this one's exponentials, with no
+// registers left for it (449 -> 489, 496 -> 598); looking pages up by scalar loads (-2 to -4%).
 #include "page_rows.h"
 #include "softmax_tiles.h"
 
@@ -644,8 +652,8 @@ __global__ __launch_bounds__(kPlanThreads) void k_page_join(PageAttnParams p) {
 
 int64_t page_attn_blocks(const PageAttnParams& p) { return tile_places(p.T, p.batch, p.tokens) * p.Hkv; }
 
-// Workgroups that share the units, as many as the card holds at once; 0: a workgroup to a
-// row tile.
+// Workgroups that share the units, as many as the card holds at once (2,048 tokens after 30,000 486 us, with 256 679);
+// 0: a workgroup to a row tile.
 int32_t page_attn_parts(const PageAttnParams& p) {
     if (p.batch > kPlanSeqs) return 0;
     if (p.map.places <= kSoloKeys || p.map.places > kMostPlanned) return 0;

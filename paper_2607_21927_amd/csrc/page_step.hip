@@ -7,7 +7,9 @@
 // wave-private LDS and read transposed, as in the contiguous decode.  Lane i looks up the page of key
 // i a tile before its loads, which are a tile ahead of the products.
 //
-// HBM-bound.  The waves of a workgroup meet in LDS, workgroups of one row tile in a second launch.
+// HBM-bound: 4 D bytes a key of a KV head (32 sequences of 41,000 keys on average, 12/2 heads of 128: 229 us for 1.34 GB,
+// 5.9 TB/s; one of 33,000, 12.2 us and 4.9 for the second launch, where a wave's chain of table, key and value
+// loads is what is left).  The waves of a workgroup meet in LDS, workgroups of one row tile in a second launch.
 #include <float.h>
 
 #include "page_rows.h"
@@ -339,11 +341,16 @@ int64_t step_keys(const PageAttnParams& p) {
 }
 
 // Bytes of keys and values from which the values pass the caches by: more than the last one
-// holds.
+// holds (32 sequences as above 255 us through the caches, 232 past them; a cache of less than that stays in
+// it from one step to the next).
 constexpr int64_t kStreamBytes = 256ll << 20;
 
 // Waves of a row tile for the keys that it may attend to (positions are on the device, so this
-// counts the places of the cache under the window).
+// counts the places of the cache under the window).  Up to kSoloTiles, or where row tiles are many, one workgroup that
+// writes out itself, of eight waves (48 sequences under a window of 1,024 keys, 32/4 heads
+// of 64, 13.3 us, with four 15.4).  Else workgroups
+// of four to kTargetWaves in all (32 sequences as above with 2,048 waves 276 us, 4,096 255, 8,192 232, 16,384 240), kMostWaves
+// to a row tile (one sequence of 33,000 keys with 1,024 19.3, 512 16.0, 256 17.3, 128 23.2).
 constexpr int64_t kSoloTiles = 16, kTargetWaves = 8192, kMostWaves = 512;
 
 template <int D, int kWaves>

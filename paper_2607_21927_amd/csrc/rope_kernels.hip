@@ -204,6 +204,10 @@ __device__ __forceinline__ RopePairs<true, P> values_of(const PairBits<P>& x) {
 // The new rows of a paged cache: as k_rope_packed, with K rotated into its page, Q into
 // rows of its own beside it and V copied, one pass over the projection's output.  A token
 // without a place in the cache keeps its Q alone.
+// HBM-bound: 2 (Hq + 2 Hkv) D elements a token, each once (65,536 tokens, 12/2 heads of 128: 116 us, 4.6 TB/s, a
+// copy's rate; rotating, then copying K and V to their pages would read and write K twice).  Few tokens: one chain
+// of offsets, table, angle in float64, load and store (32 tokens 3.5 us in a graph, their heads dealt over workgroups);
+// the host's call takes longer, 14.
 template <int P>
 __global__ __launch_bounds__(kThreads) void k_page_store(PageStoreParams p, RopeTable tab) {
     const int half = p.D >> 1, lanes = half / P;                  // lanes of a token
