@@ -11,7 +11,7 @@
 // float32 rows are taken as three bf16 parts, cut off and not rounded, whose sum is the
 // float32 value exactly: three products for one.
 //
-// Two forms.  k_w4_narrow: a workgroup takes one set of 16 outputs, its waves deal the chunks of
+// Two forms.  k_w4_narrow: a workgroup takes one set of 16 outputs and 16 rows, its waves deal the chunks of
 // 128 inputs among them, each reads the rows itself, and meet in LDS: enough workgroups where outputs
 // are few, nothing to wait for but the loads.  k_w4_wide: four waves side by side take NT sets each and
 // share the rows through LDS, since reading them for every 16 outputs would take longer than the
@@ -20,7 +20,7 @@
 // Bound by the bytes of the weights, N K (1/2 + 1/32), where rows are few, and from some 64 rows on by the matrix
 // unit; the unit is fed by decoding: a code is decoded once for the 16 MT rows of a workgroup.  151,936 outputs
 // of 1,536 inputs, 64 rows: 45 us, 3.2 TB/s and 0.66 PFLOP/s (matrix unit 26% busy, no bank conflicts).  17,920
-// of 1,536, gated, 32 rows: 7.4 us.  1,536 of 8,960 in float32, 5 rows: 12 us, of which most is
+// of 1,536, gated, 32 rows: 7.4 us.  1,536 of 8,960 in float32, 5 rows: 10.0 us, of which a third is
 // taking rows apart, again for every 16 outputs.  One row of 1,536 inputs, 2,048 outputs: 3.4 us in a graph, a chain of a few loads.
 #include "mxfp4.h"
 #include "ris_internal.h"
@@ -81,19 +81,25 @@ __device__ __forceinline__ Part<F32> parts_of(const Raw<F32>& r) {
     if constexpr (!F32) {
         p.b[0] = r.v[0];
     } else {
+        float v[8], rest[8], odd[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            v[i] = __uint_as_float(r.v[i / 4][i % 4]);
+            rest[i] = v[i] - cut(v[i]);                 // NaN of an infinity
+            odd[i & 1] += rest[i];
+        }
+        if (__any(odd[0] + odd[1] != odd[0] + odd[1])) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (v[i] != v[i]) v[i] = __uint_as_float(0x7FC00000u);       // a NaN's upper half may be an infinity's
+                rest[i] = isfinite(v[i]) ? rest[i] : 0.f;
+            }
+        }
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
-            float v[2] = {__uint_as_float(r.v[i / 4][i % 4]), __uint_as_float(r.v[i / 4][i % 4 + 1])}, mid[2], low[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                if (v[e] != v[e]) v[e] = __uint_as_float(0x7FC00000u);       // a NaN's upper half may be an infinity's
-                const float rest = isfinite(v[e]) ? v[e] - cut(v[e]) : 0.f;
-                mid[e] = rest;
-                low[e] = rest - cut(rest);
-            }
-            p.b[0][i / 2] = two(v[0], v[1]);
-            p.b[1][i / 2] = two(mid[0], mid[1]);
-            p.b[2][i / 2] = two(low[0], low[1]);
+            p.b[0][i / 2] = two(v[i], v[i + 1]);
+            p.b[1][i / 2] = two(rest[i], rest[i + 1]);
+            p.b[2][i / 2] = two(rest[i] - cut(rest[i]), rest[i + 1] - cut(rest[i + 1]));
         }
     }
     return p;
@@ -166,26 +172,23 @@ struct Sets {
     static __device__ __forceinline__ int tile(int t, int i, int sets) { return GATED && i ? sets + t : t; }
 };
 
-// MT tiles of 16 rows of x; WV waves, each with a chunk of the rows in LDS at a time and the loads of U - 1 more on
-// their way.
-template <bool F32, bool GATED, int MT, int WV, int U>
+// 16 rows of x; WV waves, each with a chunk of the rows in LDS at a time and the loads of the next on their way.
+template <bool F32, bool GATED, int WV>
 __global__ __launch_bounds__(64 * WV) void k_w4_narrow(W4Params p) {
-    constexpr int NS = Sets<GATED>::kCount, kParts = Part<F32>::kCount, kPlane = 16 * MT * kChunk, NP = 4 * MT;
-    constexpr int kStage = WV * kParts * kPlane * 2, kMeet = WV * NS * MT * 64 * 16;
+    constexpr int NS = Sets<GATED>::kCount, kParts = Part<F32>::kCount, kPlane = 16 * kChunk, NP = 4, U = 2;
+    constexpr int kStage = WV * kParts * kPlane * 2, kMeet = WV * NS * 64 * 16;
     __shared__ __align__(16) uint8_t mem[kStage > kMeet ? kStage : kMeet];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15, lg = lane >> 4;
     const int chunks = (int)chunks_of(p.K), quads = (int)quads_of(p.K);
     const int sets = (int)tiles_of(GATED ? p.N / 2 : p.N);
     // row blocks of one set one after another on one XCD
-    const int blocks = (p.rows + 16 * MT - 1) / (16 * MT);
+    const int blocks = (p.rows + 15) / 16;
     const uint32_t xcd = blockIdx.x & 7u, slot = blockIdx.x >> 3;
-    const int t = (int)(slot / blocks * 8u + xcd), m0 = (int)(slot % blocks) * 16 * MT;
+    const int t = (int)(slot / blocks * 8u + xcd), m0 = (int)(slot % blocks) * 16;
     if (t >= sets) return;
-    f32x4_t acc[NS][MT];
+    f32x4_t acc[NS];
 #pragma unroll
-    for (int n = 0; n < NS; ++n)
-#pragma unroll
-        for (int m = 0; m < MT; ++m) acc[n][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int n = 0; n < NS; ++n) acc[n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     // Piece i of a lane: eight inputs of row lane / 16 + 4 i of a chunk, 16-byte place c of the row at c ^ turn(row).
     // Rows that are not there are not loaded: what is in their place reaches outputs that are not there alone.
     uint16_t* const stage = reinterpret_cast<uint16_t*>(mem) + wave * kParts * kPlane;
@@ -227,37 +230,30 @@ __global__ __launch_bounds__(64 * WV) void k_w4_narrow(W4Params p) {
                 }
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
-                Part<F32> b[MT];
+                Part<F32> b;
 #pragma unroll
-                for (int m = 0; m < MT; ++m)
+                for (int e = 0; e < kParts; ++e)
+                    b.b[e] = *reinterpret_cast<const u32x4_t*>(stage + e * kPlane + li * kChunk + 8 * ((4 * lg + s) ^ turn(li)));
 #pragma unroll
-                    for (int e = 0; e < kParts; ++e)
-                        b[m].b[e] = *reinterpret_cast<const u32x4_t*>(stage + e * kPlane + (16 * m + li) * kChunk + 8 * ((4 * lg + s) ^ turn(li)));
-#pragma unroll
-                for (int n = 0; n < NS; ++n) {
-                    const u32x4_t w = decode8(code[u][n][s], scale_of(byte[u][n]));
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) acc[n][m] = product<F32>(w, b[m], acc[n][m]);
-                }
+                for (int n = 0; n < NS; ++n)
+                    acc[n] = product<F32>(decode8(code[u][n][s], scale_of(byte[u][n])), b, acc[n]);
             }
         }
     }
     f32x4_t* const sum = reinterpret_cast<f32x4_t*>(mem) + lane;
     __syncthreads();
 #pragma unroll
-    for (int n = 0; n < NS; ++n)
-#pragma unroll
-        for (int m = 0; m < MT; ++m) sum[((wave * NS + n) * MT + m) * 64] = acc[n][m];
+    for (int n = 0; n < NS; ++n) sum[(wave * NS + n) * 64] = acc[n];
     __syncthreads();
-    if (wave >= MT) return;                 // wave m adds up row tile m
+    if (wave > 0) return;
     f32x4_t all[NS];
 #pragma unroll
     for (int n = 0; n < NS; ++n) {
         all[n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < WV; ++w) all[n] += sum[((w * NS + n) * MT + wave) * 64];
+        for (int w = 0; w < WV; ++w) all[n] += sum[(w * NS + n) * 64];
     }
-    store_outputs<F32, GATED>(p, m0 + 16 * wave + li, t, all[0], all[NS - 1]);
+    store_outputs<F32, GATED>(p, m0 + li, t, all[0], all[NS - 1]);
 }
 
 // MT tiles of 16 rows of x in LDS, one chunk of inputs after another, two deep; KW groups of four waves deal the
@@ -447,11 +443,11 @@ __global__ __launch_bounds__(256) void k_w4_load(const uint8_t* C, const uint8_t
 // Grid of row blocks of `rows` rows beside `sets` sets of outputs, the sets dealt to the XCDs.
 int64_t grid_of(const W4Params& p, int64_t sets, int rows) { return (sets + 7) / 8 * 8 * (((int64_t)p.rows + rows - 1) / rows); }
 
-template <bool F32, int MT, int WV, int U>
+template <bool F32, int WV>
 hipError_t narrow(const W4Params& p, hipStream_t st) {
-    const dim3 grid((unsigned)grid_of(p, tiles_of(p.gated ? p.N / 2 : p.N), 16 * MT));
-    if (p.gated) hipLaunchKernelGGL((k_w4_narrow<F32, true, MT, WV, U>), grid, dim3(64 * WV), 0, st, p);
-    else hipLaunchKernelGGL((k_w4_narrow<F32, false, MT, WV, U>), grid, dim3(64 * WV), 0, st, p);
+    const dim3 grid((unsigned)grid_of(p, tiles_of(p.gated ? p.N / 2 : p.N), 16));
+    if (p.gated) hipLaunchKernelGGL((k_w4_narrow<F32, true, WV>), grid, dim3(64 * WV), 0, st, p);
+    else hipLaunchKernelGGL((k_w4_narrow<F32, false, WV>), grid, dim3(64 * WV), 0, st, p);
     return hipGetLastError();
 }
 
@@ -471,14 +467,19 @@ hipError_t wide(const W4Params& p, hipStream_t st) {
 
 }  // namespace
 
-// The wide form from 512 tiles of outputs on, and for more than 128 rows (float32: 64), where the narrow one reads
-// the rows for every 16 outputs (us, bf16, narrow and wide: 2,048 outputs of 1,536 inputs, 16 rows 4.0, 6.0, 64
-// 6.5, 10.0, 256 14, 10.2; 1,536 of 8,960, 1 row 5.8, 22, 64 20.6, 40; 17,920 gated of 1,536, 1 row 8.4, 7.0, 32
-// 18, 8.2; 151,936 of 1,536, 1 row 65, 26.0, 64 227, 47).  Waves of the narrow form: by the chunks there are (1
-// row of 1,536 inputs 4.6 with 8, 5.3 with 16).  Ways of the wide form: two, so that few sets keep more waves busy (17,920
+// The wide form from 512 tiles of outputs on, where the narrow one reads the rows for every 16 outputs (us, bf16, narrow
+// and wide: 17,920 gated of 1,536, 1 row 8.4, 7.0, 32 18, 8.2; 151,936 of 1,536, 1 row 65, 26.0, 64 227, 47), and for
+// many rows, where the narrow one reads the weights for every 16 of them (1,536 outputs of 8,960 inputs, 256 rows
+// 29.6, 40, 512 98, 42; 4,096 of 4,096, 128 rows 18.1, 21.4, 256 31, 21; float32 39, 82 at 128 rows and 222, 85 at
+// 512).  Waves of the narrow form: as many as the chunks keep busy where a CU has one workgroup (1,536 of 8,960, 1 row 5.8
+// with 16, 6.7 with 8, 9.3 with 4; float32 8.7 with 12, 9.8, 15), fewer where it has several (128 rows 18.3, 17.1, 16.0;
+// float32 44, 50, 39).  More than 16 rows to a workgroup save decoding and lose by what they hold in registers and LDS
+// (1,536 of 8,960, 64 rows 11.7, with 64 to a workgroup 20.4; float32 30, with 32 to a workgroup 46).
+// Ways of the wide form: two, so that few sets keep more waves busy (17,920
 // gated, 32 rows 10.1 with one, 7.4 with two, 7.5 with four; 151,936, 64 rows 45.5, 45.3, 65), float32's rows of more than 16 one,
 // for room in LDS.
-static bool takes_wide(const W4Params& p) { return tiles_of(p.N) >= 512 || p.rows > (p.f32 ? 64 : 128); }
+static int64_t row_tiles(const W4Params& p) { return tiles_of(p.N) * (((int64_t)p.rows + 15) / 16); }
+static bool takes_wide(const W4Params& p) { return tiles_of(p.N) >= 512 || row_tiles(p) > (p.f32 ? 1536 : 2048); }
 
 int64_t w4_items(const W4Params& p) {
     const int64_t sets = tiles_of(p.gated ? p.N / 2 : p.N);
@@ -494,12 +495,10 @@ hipError_t launch_w4_linear(const W4Params& p, hipStream_t st) {
         if (p.rows <= 16) return wide<false, 1, 2, 2>(p, st);
         return p.rows <= 32 ? wide<false, 2, 2, 2>(p, st) : wide<false, 4, 2, 2>(p, st);
     }
-    if (p.f32) return p.rows <= 16 ? narrow<true, 1, 8, 2>(p, st) : narrow<true, 2, 4, 1>(p, st);
-    if (p.rows <= 16) {
-        if (chunks > 32) return narrow<false, 1, 16, 2>(p, st);
-        return chunks > 8 ? narrow<false, 1, 8, 2>(p, st) : narrow<false, 1, 4, 2>(p, st);
-    }
-    return p.rows <= 32 ? narrow<false, 2, 8, 2>(p, st) : narrow<false, 4, 8, 1>(p, st);
+    const int64_t units = row_tiles(p);
+    if (p.f32) return units <= 256 && chunks > 8 ? narrow<true, 12>(p, st) : narrow<true, 4>(p, st);
+    if (units <= 256 && chunks > 32) return narrow<false, 16>(p, st);
+    return units <= 512 && chunks > 8 ? narrow<false, 8>(p, st) : narrow<false, 4>(p, st);
 }
 
 hipError_t launch_w4_pack(const void* W, int64_t stride, int bf16, int32_t N, int32_t K, uint8_t* C, uint8_t* S, hipStream_t st) {
