@@ -213,3 +213,23 @@ def test_many_rows():
     want = x.double() @ W.t().cuda()
     assert bool(((out.double() - want).abs() <= bar(x.double(), W.cuda(), None, want, BF16) + rounded(want, BF16)).all())
     assert bool(((out[-64:].double() - few.double()).abs() <= 2 * rounded(want[-64:], BF16)).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows", [3, 70, 130, 300])
+def test_many_inputs(rows, dtype):
+    """40 tiles of inputs, the last one not whole, for every number of waves that deal them."""
+    serve = need_serve()
+    N, K = 1504, 5000
+    C, S, W = weights(serve, N, K, seed=9)
+    x = randn(rows, K, dtype=dtype, seed=rows)
+    want = x.double().cpu() @ W.t()
+    lim = bar(x.double().cpu(), W, None, want, dtype)
+    out = serve.w4_linear(x, C, S, torch.empty(rows, N, dtype=dtype, device="cuda"))
+    assert bool(((out.double().cpu() - want).abs() <= lim + rounded(want, dtype)).all())
+    out = serve.w4_linear(x, C, S, torch.empty(rows, N // 2, dtype=dtype, device="cuda"), gated=True)
+    a, up = want.chunk(2, 1)
+    da, du = lim.chunk(2, 1)
+    want = a * torch.sigmoid(a) * up
+    lim = (1.1 * da) * (up.abs() + du) + a.abs() * du + want.abs() * (a.abs() + 8) * 2 * U + rounded(want, dtype)
+    assert bool(((out.double().cpu() - want).abs() <= lim).all())
