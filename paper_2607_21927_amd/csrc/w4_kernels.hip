@@ -467,8 +467,9 @@ hipError_t wide(const W4Params& p, hipStream_t st) {
 
 }  // namespace
 
-// The wide form from 512 tiles of outputs on, where the narrow one reads the rows for every 16 outputs (us, bf16, narrow
-// and wide: 17,920 gated of 1,536, 1 row 8.4, 7.0, 32 18, 8.2; 151,936 of 1,536, 1 row 65, 26.0, 64 227, 47), and for
+// The wide form from 1,024 tiles of outputs on, where the narrow one reads the rows for every 16 outputs (us, bf16, narrow
+// and wide: 9,216 outputs of 8,192 inputs, 1 row 12.8, 26, 32 28, 29; 17,920 of 1,536, 1 row 5.8, 6.6, 16 7.5, 6.7,
+// 64 18, 11; 32,768 of 4,096, 1 row 17.3, 18.1, 16 27, 18), and for
 // many rows, where the narrow one reads the weights for every 16 of them (1,536 outputs of 8,960 inputs, 256 rows
 // 29.6, 40, 512 98, 42; 4,096 of 4,096, 128 rows 18.1, 21.4, 256 31, 21; float32 39, 82 at 128 rows and 222, 85 at
 // 512).  Waves of the narrow form: as many as the chunks keep busy where a CU has one workgroup (1,536 of 8,960, 1 row 5.8
@@ -479,7 +480,7 @@ hipError_t wide(const W4Params& p, hipStream_t st) {
 // gated, 32 rows 10.1 with one, 7.4 with two, 7.5 with four; 151,936, 64 rows 45.5, 45.3, 65), float32's rows of more than 16 one,
 // for room in LDS.
 static int64_t row_tiles(const W4Params& p) { return tiles_of(p.N) * (((int64_t)p.rows + 15) / 16); }
-static bool takes_wide(const W4Params& p) { return tiles_of(p.N) >= 512 || row_tiles(p) > (p.f32 ? 1536 : 2048); }
+static bool takes_wide(const W4Params& p) { return tiles_of(p.N) >= 1024 || row_tiles(p) > (p.f32 ? 1536 : 2048); }
 
 int64_t w4_items(const W4Params& p) {
     const int64_t sets = tiles_of(p.gated ? p.N / 2 : p.N);

@@ -216,11 +216,12 @@ def test_many_rows():
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("rows", [3, 70, 130, 300])
-def test_many_inputs(rows, dtype):
-    """40 tiles of inputs, the last one not whole, for every number of waves that deal them."""
+@pytest.mark.parametrize("rows,N,K", [(3, 1504, 5000), (70, 1504, 5000), (130, 1504, 5000), (300, 1504, 5000),
+                                      (1, 16_416, 200), (20, 16_416, 200), (50, 16_416, 200), (2, 16_480, 1032)])
+def test_every_form(rows, N, K, dtype):
+    """40 tiles of inputs, the last one not whole, for every number of waves that deal them; outputs
+    enough for the form that shares rows, their last tiles no whole workgroup's."""
     serve = need_serve()
-    N, K = 1504, 5000
     C, S, W = weights(serve, N, K, seed=9)
     x = randn(rows, K, dtype=dtype, seed=rows)
     want = x.double().cpu() @ W.t()
