@@ -256,7 +256,7 @@ struct W4Params {
     int32_t f32, gated;
     int32_t vector_out;           // rows of out take four neighbouring outputs in one store
 };
-int64_t w4_items(const W4Params& p);           // work-items of a launch, at most
+int64_t w4_items(const W4Params& p);           // work-items of a launch, at most, where they are many
 hipError_t launch_w4_linear(const W4Params& p, hipStream_t st);
 hipError_t launch_w4_pack(const void* W, int64_t stride, int bf16, int32_t N, int32_t K, uint8_t* C, uint8_t* S, hipStream_t st);
 hipError_t launch_w4_load(const uint8_t* C, const uint8_t* S, int32_t N, int32_t K, void* W, int64_t stride, int bf16,

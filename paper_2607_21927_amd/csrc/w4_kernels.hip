@@ -471,30 +471,44 @@ hipError_t wide(const W4Params& p, hipStream_t st) {
 // and wide: 9,216 outputs of 8,192 inputs, 1 row 12.8, 26, 32 28, 29; 17,920 of 1,536, 1 row 5.8, 6.6, 16 7.5, 6.7,
 // 64 18, 11; 32,768 of 4,096, 1 row 17.3, 18.1, 16 27, 18), and for
 // many rows, where the narrow one reads the weights for every 16 of them (1,536 outputs of 8,960 inputs, 256 rows
-// 29.6, 40, 512 98, 42; 4,096 of 4,096, 128 rows 18.1, 21.4, 256 31, 21; float32 39, 82 at 128 rows and 222, 85 at
-// 512).  Waves of the narrow form: as many as the chunks keep busy where a CU has one workgroup (1,536 of 8,960, 1 row 5.8
+// 29.6, 33, 512 98, 33; 4,096 of 4,096, 96 rows 15.5, 16.4, 128 18.1, 16.4; float32 128 rows 39, 62, 256 77, 62; 4,096 of
+// 4,096, 64 rows 27, 28, 96 36, 28; gated, where a workgroup takes its rows apart for two sets, bf16 128 rows 13.5, 20.8,
+// float32 96 rows 23, 28).  Waves of the narrow form: as many as the chunks keep busy where a CU has one workgroup (1,536 of 8,960, 1 row 5.8
 // with 16, 6.7 with 8, 9.3 with 4; float32 8.7 with 12, 9.8, 15), fewer where it has several (128 rows 18.3, 17.1, 16.0;
 // float32 44, 50, 39).  More than 16 rows to a workgroup save decoding and lose by what they hold in registers and LDS
 // (1,536 of 8,960, 64 rows 11.7, with 64 to a workgroup 20.4; float32 30, with 32 to a workgroup 46).
 // Ways of the wide form: two, so that few sets keep more waves busy (17,920
-// gated, 32 rows 10.1 with one, 7.4 with two, 7.5 with four; 151,936, 64 rows 45.5, 45.3, 65), float32's rows of more than 16 one,
-// for room in LDS.
+// gated, 32 rows 10.1 with one, 7.4 with two, 7.5 with four; 151,936, 64 rows 45.5, 45.3, 65), but one for more than 16
+// rows of float32 where a CU has more than one workgroup, and LDS room for no more than one of two ways (one and two ways:
+// 1,536 of 8,960, 512 rows 84, 62, 768 115, 114; 151,936, 32 rows 58, 63).  Sets of a wave: two, in bf16 one where
+// workgroups would leave half of the CUs empty (two and one: 1,536 of 8,960, 512 rows 41, 33, 768 42, 46; 4,096 of 4,096,
+// 256 rows 21.4, 16.9, 512 23, 26).
 static int64_t row_tiles(const W4Params& p) { return tiles_of(p.N) * (((int64_t)p.rows + 15) / 16); }
-static bool takes_wide(const W4Params& p) { return tiles_of(p.N) >= 1024 || row_tiles(p) > (p.f32 ? 1536 : 2048); }
+static bool takes_wide(const W4Params& p) {
+    return tiles_of(p.N) >= 1024 || row_tiles(p) > (p.f32 ? 1024 : 1536) + (p.gated ? 512 : 0);
+}
+
+// Workgroups of the wide form of two sets a wave.
+static int64_t wide_groups(const W4Params& p, int rows) {
+    const int64_t sets = tiles_of(p.gated ? p.N / 2 : p.N), each = p.gated ? 4 : 8;
+    return grid_of(p, (sets + each - 1) / each, rows);
+}
 
 int64_t w4_items(const W4Params& p) {
-    const int64_t sets = tiles_of(p.gated ? p.N / 2 : p.N);
-    if (!takes_wide(p)) return grid_of(p, sets, 16) * 1024;             // at most
-    const int rows = p.rows <= 16 ? 16 : (p.f32 || p.rows <= 32 ? 32 : 64), each = p.gated ? 4 : 8;
-    return grid_of(p, (sets + each - 1) / each, rows) * 512;
+    if (!takes_wide(p)) return grid_of(p, tiles_of(p.gated ? p.N / 2 : p.N), 16) * 1024;
+    return wide_groups(p, p.rows <= 16 ? 16 : (p.f32 || p.rows <= 32 ? 32 : 64)) * 512;
 }
 
 hipError_t launch_w4_linear(const W4Params& p, hipStream_t st) {
     const int64_t chunks = chunks_of(p.K);
     if (takes_wide(p)) {
-        if (p.f32) return p.rows <= 16 ? wide<true, 1, 2, 2>(p, st) : wide<true, 2, 2, 1>(p, st);
+        if (p.f32) {
+            if (p.rows <= 16) return wide<true, 1, 2, 2>(p, st);
+            return wide_groups(p, 32) <= 256 ? wide<true, 2, 2, 2>(p, st) : wide<true, 2, 2, 1>(p, st);
+        }
         if (p.rows <= 16) return wide<false, 1, 2, 2>(p, st);
-        return p.rows <= 32 ? wide<false, 2, 2, 2>(p, st) : wide<false, 4, 2, 2>(p, st);
+        if (p.rows <= 32) return wide<false, 2, 2, 2>(p, st);
+        return wide_groups(p, 64) <= 128 && !p.gated ? wide<false, 4, 1, 2>(p, st) : wide<false, 4, 2, 2>(p, st);
     }
     const int64_t units = row_tiles(p);
     if (p.f32) return units <= 256 && chunks > 8 ? narrow<true, 12>(p, st) : narrow<true, 4>(p, st);

@@ -313,7 +313,7 @@ class W4Weight:
 
     # Rows up to which the product reads the 4-bit weights itself.  For more they are written out for a library
     # product (1,024 rows in bf16: 17,920 outputs of 1,536 inputs 70 us by itself, 26 + 70 written out, 151,936 of
-    # 1,536 553 and 194 + 445, 1,536 of 8,960 50 and 19 + 46; from there on its time doubles with the rows).
+    # 1,536 553 and 194 + 445, 1,536 of 8,960 47 and 18 + 45; from there on its time doubles with the rows).
     MOST_ROWS = 1024
 
     def __init__(self, w):

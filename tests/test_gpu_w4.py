@@ -217,6 +217,7 @@ def test_many_rows():
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("rows,N,K", [(3, 1504, 5000), (70, 1504, 5000), (130, 1504, 5000), (300, 1504, 5000),
+                                      (400, 1504, 1032), (600, 1504, 520), (1500, 1504, 520),
                                       (1, 16_416, 200), (20, 16_416, 200), (50, 16_416, 200), (2, 16_480, 1032)])
 def test_every_form(rows, N, K, dtype):
     """40 tiles of inputs, the last one not whole, for every number of waves that deal them; outputs
