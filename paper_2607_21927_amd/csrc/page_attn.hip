@@ -82,6 +82,10 @@ struct Plan {
     }
 };
 
+// In a piece's fourth number, else 1 where its row attends to something and 0 where not: it does,
+// and its weights were taken at m c (see join_factor).
+constexpr float kApart = 2.f;
+
 // What the second launch needs of a row tile of a KV head: its pieces are the end of part
 // `part` and the beginnings of the parts behind it.
 struct Pieces {
@@ -458,7 +462,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void k_page_attn(Page
         seen &= pos >= 0;
         if (kSplit && (begin > 0 || end < s.n)) {
             const int64_t at = (int64_t)piece * p.part_rows + r;
-            if (lh == 0) *reinterpret_cast<f32x4_t*>(p.part_ml + 4 * at) = f32x4_t{ref.m, ref.mc, l, seen ? 1.f : 0.f};
+            if (lh == 0) *reinterpret_cast<f32x4_t*>(p.part_ml + 4 * at) = f32x4_t{ref.m, ref.mc, l, seen ? (ref.apart ? kApart : 1.f) : 0.f};
             float* to = p.part_o + at * D + 4 * lh;
 #pragma unroll
             for (int d = 0; d < DB; ++d)
@@ -518,19 +522,22 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void k_page_attn(Page
 constexpr int kFewPieces = 16;
 
 struct RowRef {
-    float top, topc;
-    bool far;
-    __device__ __forceinline__ void meet(const f32x4_t& ml) {
-        topc = top < ml[0] ? ml[1] : topc;
-        top = fmaxf(top, ml[0]);
-        far |= far_ref(ml[1]);
+    float top = -INFINITY, topc = 0.f, kind = 0.f;
+    __device__ __forceinline__ void meet(float m, float mc, float k) {
+        kind = top < m ? k : kind;
+        topc = top < m ? mc : topc;
+        top = fmaxf(top, m);
     }
     // Over the wave.
     __device__ __forceinline__ void join() {
         const float all = wave_max(top);
-        topc = __shfl(topc, (int)__builtin_ctzll(__ballot(top == all)));
+        const int at = (int)__builtin_ctzll(__ballot(top == all));
+        topc = __shfl(topc, at);
+        kind = __shfl(kind, at);
         top = all;
-        far = __any(far);
+    }
+    __device__ __forceinline__ float factor(const f32x4_t& ml, float c) const {
+        return join_factor<false>(ml[0], ml[1], ml[3] == kApart, top, topc, kind == kApart, c);
     }
 };
 
@@ -565,10 +572,10 @@ __global__ __launch_bounds__(kPlanThreads) void k_page_join(PageAttnParams p) {
         for (int r = (int)blockIdx.y * kWaves + wave; r < rows; r += (int)gridDim.y * kWaves) {
             f32x4_t ml = {-INFINITY, 0.f, 0.f, 0.f};
             if (lane < n) ml = sums(lane, r);
-            RowRef ref{-INFINITY, 0.f, false};
-            ref.meet(ml);
+            RowRef ref;
+            ref.meet(ml[0], ml[1], ml[3]);
             ref.join();
-            const float a = join_factor<false>(ml[0], ml[1], ref.top, ref.topc, ref.far, p.c);
+            const float a = ref.factor(ml, p.c);
             const float l = wave_sum(ml[2] * a), seen = wave_sum(ml[3]);
             float y[kEach] = {};
 #pragma unroll 4
@@ -589,27 +596,26 @@ __global__ __launch_bounds__(kPlanThreads) void k_page_join(PageAttnParams p) {
         return;
     }
     for (int r = blockIdx.y; r < rows; r += gridDim.y) {
-        RowRef ref{-INFINITY, 0.f, false};
-        for (int i = tid; i < n; i += kPlanThreads) ref.meet(sums(i, r));
+        RowRef ref;
+        for (int i = tid; i < n; i += kPlanThreads) {
+            const f32x4_t ml = sums(i, r);
+            ref.meet(ml[0], ml[1], ml[3]);
+        }
         ref.join();
         __syncthreads();
         if (lane == 0) {
             red[wave][0] = ref.top;
             red[wave][1] = ref.topc;
-            red[wave][2] = ref.far ? 1.f : 0.f;
+            red[wave][2] = ref.kind;
         }
         __syncthreads();
-        ref = RowRef{-INFINITY, 0.f, false};
+        ref = RowRef();
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            ref.topc = ref.top < red[w][0] ? red[w][1] : ref.topc;
-            ref.top = fmaxf(ref.top, red[w][0]);
-            ref.far |= red[w][2] != 0.f;
-        }
+        for (int w = 0; w < kWaves; ++w) ref.meet(red[w][0], red[w][1], red[w][2]);
         float l = 0.f, seen = 0.f;
         for (int i = tid; i < n; i += kPlanThreads) {
             const f32x4_t ml = sums(i, r);
-            const float a = join_factor<false>(ml[0], ml[1], ref.top, ref.topc, ref.far, p.c);
+            const float a = ref.factor(ml, p.c);
             factor[i] = a;
             l = fmaf(ml[2], a, l);
             seen += ml[3];

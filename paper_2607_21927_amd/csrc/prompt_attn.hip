@@ -292,11 +292,12 @@ __global__ __launch_bounds__(64 * kWaves * S, D == 64 ? 3 : 2) void k_prompt_bf1
             uint16_t* const place[4] = {k0s, k1s, v0s, v1s};         // S kKeys D elements each: 64 D floats
 #pragma unroll
             for (int d = 0; d < DB; ++d) mem[d] = reinterpret_cast<float*>(place[d]) + wave * 16 * 64 + lane;
-            __shared__ float ml[kWaves][3][64];
+            __shared__ float ml[kWaves][4][64];
             if (group == 1) {
                 ml[wave][0][lane] = ref.m;
                 ml[wave][1][lane] = ref.mc;
                 ml[wave][2][lane] = l;
+                if (kSafe) ml[wave][3][lane] = ref.apart ? 1.f : 0.f;
 #pragma unroll
                 for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -305,8 +306,9 @@ __global__ __launch_bounds__(64 * kWaves * S, D == 64 ? 3 : 2) void k_prompt_bf1
             __syncthreads();
             if (group == 0) {
                 const float m1 = ml[wave][0][lane], mc1 = ml[wave][1][lane], top = fmaxf(ref.m, m1), topc = ref.m < m1 ? mc1 : ref.mc;
-                const bool far = far_ref(ref.mc) || far_ref(mc1);
-                const float a = join_factor<false>(ref.m, ref.mc, top, topc, far, p.c), a1 = join_factor<false>(m1, mc1, top, topc, far, p.c);
+                const bool apart = kSafe && ref.apart, apart1 = kSafe && ml[wave][3][lane] != 0.f, top_apart = ref.m < m1 ? apart1 : apart;
+                const float a = join_factor<false>(ref.m, ref.mc, apart, top, topc, top_apart, p.c);
+                const float a1 = join_factor<false>(m1, mc1, apart1, top, topc, top_apart, p.c);
                 l = fmaf(ml[wave][2][lane], a1, l * a);
 #pragma unroll
                 for (int d = 0; d < DB; ++d)
@@ -350,6 +352,7 @@ __device__ __forceinline__ void join_waves(const PromptParams& p, float* mem, fl
     ml[wave * kTile] = ref.m;
     ml[wave * kTile + 64] = pair_sum32(l);
     ml[wave * kTile + 192] = ref.mc;
+    if (kSafe) ml[wave * kTile + 128] = ref.apart ? 1.f : 0.f;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -357,17 +360,18 @@ __device__ __forceinline__ void join_waves(const PromptParams& p, float* mem, fl
     __syncthreads();
     if (row >= t.len) return;
     float top = -INFINITY, topc = 0.f, a[kWaves], sum = 0.f;
-    bool far = false;
+    bool apart[kWaves], top_apart = false;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
         const float m = ml[w * kTile], mc = ml[w * kTile + 192];
+        apart[w] = kSafe && ml[w * kTile + 128] != 0.f;
+        top_apart = top < m ? apart[w] : top_apart;
         topc = top < m ? mc : topc;
         top = fmaxf(top, m);
-        far |= kSafe && far_ref(mc);
     }
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-        a[w] = join_factor<kF32>(ml[w * kTile], ml[w * kTile + 192], top, topc, far, p.c);
+        a[w] = join_factor<kF32>(ml[w * kTile], ml[w * kTile + 192], apart[w], top, topc, top_apart, p.c);
         sum = fmaf(a[w], ml[w * kTile + 64], sum);
     }
     const float inv = 1.f / sum;            // every score -inf: 0 / 0, NaN

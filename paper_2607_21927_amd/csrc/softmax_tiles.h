@@ -98,10 +98,14 @@ struct Ref {
     }
 };
 // The factor of a partial sum under the reference m (mc) where partial sums of one row
-// meet under the largest, top (topc); far: one of theirs is.
+// meet under the largest, top (topc).  Weights of a row apart are taken at m c itself, the others
+// at mc, which is up to 2^-1 from it below kNearRef: where the two kinds meet, what an m c is
+// over its mc counts as well (none where mc is infinite, and the other one is 2^24 at most then).
+__device__ __forceinline__ float over(float m, float mc, bool apart, float c) { return apart && isfinite(mc) ? fmaf(m, c, -mc) : 0.f; }
 template <bool kF32>
-__device__ __forceinline__ float join_factor(float m, float mc, float top, float topc, bool far, float c) {
-    return m == -INFINITY ? 0.f : pow2<kF32>(far ? (m - top) * c : mc - topc);
+__device__ __forceinline__ float join_factor(float m, float mc, bool apart, float top, float topc, bool top_apart, float c) {
+    if (m == -INFINITY) return 0.f;
+    return pow2<kF32>(apart && top_apart ? (m - top) * c : (mc - topc) + (over(m, mc, apart, c) - over(top, topc, top_apart, c)));
 }
 
 }  // namespace
