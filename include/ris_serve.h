@@ -291,7 +291,8 @@ int ris_page_attn(const void* Q, const void* Kp, const void* Vp, const int32_t* 
  *      r, byte i hold the inputs 128 k + 32 g + 2 i (low half) and + 2 i + 1 of output
  *      16 n + r;
  *   S: uint8 [ceil(N / 16), ceil(K / 512), 4, 16, 4]: entry (n, q, g, r, i) is the scale
- *      byte of block g of tile k = 4 q + i, 2^(byte - 127), 255 = NaN.
+ *      byte of block g of tile k = 4 q + i, 2^(byte - 127), 255 = NaN (packing writes 3..252
+ *      and 255; under 253 and 254 values from 2^128 on are infinities).
  *
  * Outputs from N on and inputs from K on are zeros.  C must be 16-byte aligned.
  */
@@ -318,7 +319,8 @@ typedef struct {
  * out = x W^T + bias, [rows, N]; gated: out = silu(a) * b, [rows, N / 2], with a and b the
  * first and second half of x W^T + bias (gate above up, as ris_swiglu takes them).
  * bias NULL: none.  Products are exact, sums float32, one rounding at the store: meant for
- * few rows (a decode step), right for any.  out must not overlap the inputs.
+ * few rows (a decode step), right for any.  float32 inputs below 2^-110 in magnitude are cut off to
+ * multiples of 2^-133.  out must not overlap the inputs.
  */
 int ris_w4_linear(const void* x, const uint8_t* C, const uint8_t* S, const void* bias, void* out, const ris_w4_desc* desc,
                   void* stream);

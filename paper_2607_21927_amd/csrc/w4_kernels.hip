@@ -9,7 +9,8 @@
 // l % 16 at the same inputs.  All products are exact, sums are float32.
 //
 // float32 rows are taken as three bf16 parts, cut off and not rounded, whose sum is the
-// float32 value exactly: three products for one.
+// float32 value exactly from 2^-110 on (the matrix unit keeps subnormal numbers; below, the last
+// part lacks bits under 2^-133): three products for one.
 //
 // Two forms.  k_w4_narrow: a workgroup takes one set of 16 outputs and 16 rows, its waves deal the chunks of
 // 128 inputs among them, each reads the rows itself, and meet in LDS: enough workgroups where outputs
