@@ -380,8 +380,8 @@ def _page_map(Kp, table):
 def _need_pages(Kp, Vp):
     if Kp.dtype != torch.bfloat16 or Vp.dtype != torch.bfloat16:
         raise TypeError("pages must be bfloat16")
-    shape = Kp.shape
-    if len(shape) != 4 or Vp.shape != shape or Vp.stride() != Kp.stride():
+    shape, k, v = Kp.shape, Kp.stride(), Vp.stride()
+    if len(shape) != 4 or Vp.shape != shape or v != k and any(n > 1 and a != b for n, a, b in zip(shape, k, v)):
         raise ValueError("Kp and Vp must be [pages, Hkv, page, D], of one shape and strides")
     return shape
 
