@@ -13,14 +13,18 @@
 // may attend to and whose page there is are a mask of 64 bits (`live`); the others are
 // never read: the first live key is loaded in their place.  Rows attend to bits of that
 // mask, so that what lies in unwritten places does not reach an output.
-// Bound by the matrix unit where it is fed: 4 D flops a (query head, key) pair at 0.84 to 0.86 PFLOP/s (2,048 tokens after
-// 30,000, 12/2 heads of 128: 456 us for 390 GFLOP; 16,384 of three sequences under a window of 4,096: 490 for 413), the unit
-// busy 42% and 38% of the time.  A wave's exponentials and its products follow each other, and of two waves a SIMD
+// Bound by the matrix unit where it is fed: 4 D flops a (query head, key) pair at 0.77 to 0.86 PFLOP/s (2,048 tokens after
+// 30,000, 12/2 heads of 128: 453 to 485 us on several machines for 390 GFLOP; 16,384 of three sequences under a window of 4,096:
+// 490 to 537 for 413), the unit busy 42% and 38% of the time.  A wave's exponentials and its products follow each other, and of two waves a SIMD
 // one is often at a barrier for the next tile (in the first case 71% of the requests for K and V miss
-// L2: 2.4 GB of them a pass).  Weights and values of the next 16 keys are made beside a product.
+// L2: 18.5 million of 128 bytes, 2.4 GB, a pass).  Weights and values of the next 16 keys are made beside a product.
 // Measured and not kept: eight waves of 256 rows with three tiles in LDS, half the reads (438 for 475 there, but 537 for
 // 502 under the window and 112 for 92 in a mixed batch); the next tile's scores beside this one's exponentials, with no
-// registers left for it (449 -> 489, 496 -> 598); looking pages up by scalar loads (-2 to -4%).
+// registers left for it (449 -> 489, 496 -> 598); one scalar load of a page for a tile that lies in it
+// (455 -> 464, 508 -> 523, mixed 85.7 -> 88.0).
+// Softmax weights are rounded to bf16 for the PV product, as in the other attention kernels here: in float32 it would
+// run at a sixteenth of the rate, in two bf16 parts at half of it.  An output is off by 2^-8 of the largest value at most for
+// it, 2.3e-3 of itself in the root mean square with its own rounding, which alone is 1.7e-3.
 #include "page_rows.h"
 #include "softmax_tiles.h"
 

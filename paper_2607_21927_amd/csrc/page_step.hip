@@ -208,7 +208,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_page_step(PageAttnParams p) 
                     w[kb][i] = __builtin_amdgcn_exp2f((st[kb][i] - m) * p.c);
                     l += w[kb][i];
                 }
-            // P as the A operand: row l % 16, slots 8 (l / 16) + e hold the keys 4 (l / 16) + e (e < 4) and 16 +
+            // P as the A operand, rounded to bf16 (as the row-tile form's): row l % 16, slots 8 (l / 16) + e hold the keys 4 (l / 16) + e (e < 4) and 16 +
             // 4 (l / 16) + e - 4; V as the B operand with the same key order.
             const u32x4_t pk = {pack_bf16x2(w[0][0], w[0][1]), pack_bf16x2(w[0][2], w[0][3]), pack_bf16x2(w[1][0], w[1][1]),
                                 pack_bf16x2(w[1][2], w[1][3])};
@@ -374,6 +374,13 @@ hipError_t launch_d(const PageAttnParams& p, hipStream_t st) {
 
 }  // namespace
 
+// Tokens of a row tile of the step form where the sequences have so few in the mean that a tile holds them, else 0: the row
+// tiles of 128 rows.  The step form and those, us: one token after 33,000, 12/2 heads of 128, 16.4 and 21.2, 32/4 of 64 14.1 and
+// 17.9; 32 of 41,000 on average 232 and 239; 48 under a window of 1,024, 32/4 of 64, 13.3 and 21.5; 48 of two tokens after 1,000,
+// 12/2 heads 19.7 and 22.3, 32/4 14.3 and 21.5; but 32 of one or two after 3,000 34 to 37 and 29, 8 of two after 9,000 31 and 26,
+// and 32 of two after 65,000 at most 252 and 248.  The host sees the mean alone: one long chunk among single tokens,
+// which the mean hides, is cut into tiles of 16 rows that each read its keys (one of 960 tokens and 63 steps after 9,000, 4/4 heads
+// of 128, 249 and 157, as two calls 187; one of 256 and 63, 12/4 heads, 233 and 154; one of 64 and 63, 24/4 heads, 197 and 155).
 int32_t page_step_tokens(int64_t T, int32_t batch, int32_t G) {
     const int64_t each = (T + batch - 1) / batch;
     return each * G <= kMostRows ? (int32_t)each : 0;

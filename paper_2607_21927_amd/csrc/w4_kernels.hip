@@ -469,9 +469,12 @@ hipError_t wide(const W4Params& p, hipStream_t st) {
 }  // namespace
 
 // The wide form from 1,024 tiles of outputs on, where the narrow one reads the rows for every 16 outputs (us, bf16, narrow
-// and wide: 9,216 outputs of 8,192 inputs, 1 row 12.8, 26, 32 28, 29; 17,920 of 1,536, 1 row 5.8, 6.6, 16 7.5, 6.7,
-// 64 18, 11; 32,768 of 4,096, 1 row 17.3, 18.1, 16 27, 18), and for
-// many rows, where the narrow one reads the weights for every 16 of them (1,536 outputs of 8,960 inputs, 256 rows
+// and wide: 16 rows, 14,336 outputs of 1,536 inputs 6.9, 6.7, of 4,096 11.4, 12.7, of 8,192 26, 27; 17,920 of 1,536 7.6, 6.8, of
+// 4,096 17, 15, of 8,192 32, 28; 64 rows, 17,920 of 1,536 18, 11; float32 16 rows, 14,336 of 4,096 27, 20, 17,920 of 4,096 32, 21).
+// The line looks at outputs alone, and that costs one to four rows just above it, where workgroups of the wide form are fewer
+// than CUs: one row, 17,920 of 1,536 5.9, 6.8, of 4,096 10.4, 15.4, of 8,192 19.4, 27.8, gated 18.8, 28.7, float32 33, 38, gated
+// 24, 38; 28,672 of 4,096 16.3, 17.1, of 8,192 31.8, 32.4; 32,768 of 1,536 8.1, 7.3; 151,936 of 1,536 32, 27, float32 55, 32).
+// And for many rows, where the narrow one reads the weights for every 16 of them (1,536 outputs of 8,960 inputs, 256 rows
 // 29.6, 33, 512 98, 33; 4,096 of 4,096, 96 rows 15.5, 16.4, 128 18.1, 16.4; float32 128 rows 39, 62, 256 77, 62; 4,096 of
 // 4,096, 64 rows 27, 28, 96 36, 28; gated, where a workgroup takes its rows apart for two sets, bf16 128 rows 13.5, 20.8,
 // float32 96 rows 23, 28).  Waves of the narrow form: as many as the chunks keep busy where a CU has one workgroup (1,536 of 8,960, 1 row 5.8

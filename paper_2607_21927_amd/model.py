@@ -311,9 +311,12 @@ def linear(x, w, bias=None):
 class W4Weight:
     """A weight matrix held in 4 bits (codes and scales of ``serve.w4_weight``)."""
 
-    # Rows up to which the product reads the 4-bit weights itself.  For more they are written out for a library
-    # product (1,024 rows in bf16: 17,920 outputs of 1,536 inputs 70 us by itself, 26 + 70 written out, 151,936 of
-    # 1,536 553 and 194 + 445, 1,536 of 8,960 47 and 18 + 45; from there on its time doubles with the rows).
+    # Rows up to which the product reads the 4-bit weights itself.  For more they are written out, in every call, for
+    # a library product.  By itself, and written out + library, us, bf16: 17,920 outputs of 1,536 inputs, 1,024 rows 65 and
+    # 22 + 63, 1,536 101 and 22 + 69, 2,048 141 and 22 + 111; 151,936 of 1,536, 1,024 rows 544 and 189 + 441, 2,048 1,195 and
+    # 189 + 746; 1,536 of 8,960, 1,024 45 and 14 + 42, 2,048 78 and 14 + 59; 2,048 of 1,536, 2,048 21 and 6 + 19.  The library
+    # draws level between 1,024 and 2,048 rows.  float32 has the same line, though the product by itself takes half
+    # as long at every number of rows (17,920 of 1,536, 1,024 rows 168 and 38 + 410, 4,096 720 and 38 + 1,578).
     MOST_ROWS = 1024
 
     def __init__(self, w):
